@@ -53,7 +53,8 @@
  * unimplemented combination returns AQD_ERR_UNSUPPORTED; aqd_last_error()
  * returns a message for the calling thread's last failure.
  *
- * Device pointers must be 16-byte aligned. An output buffer must not overlap
+ * Device pointers must be 16-byte aligned (the 8-bit linear layers' calls ask for
+ * less, see there). An output buffer must not overlap
  * any input buffer of the same call.
  *
  * Thread safety: handles are immutable after creation; concurrent run calls
@@ -309,6 +310,86 @@ typedef struct {
 
 aqd_status_t aqd_maxpool_run(const aqd_maxpool_desc_t *desc, const void *x, void *y,
                              aqd_stream_t stream);
+
+/* ---- 8-bit linear layers: real-valued rows to signed codes, and their product
+ * with 8-bit weights ----------------------------------------------------------
+ * For layers whose outputs are real numbers (the linear layers of a transformer
+ * next to or behind the integer network): activations are rows (tokens) of
+ * signed int8 codes with one fp32 scale per row, weights rows (output channels)
+ * of int8 codes with one fp32 scale per channel; code * scale is the value that
+ * a code stands for. These are inference calls, like the rest of the library.
+ *
+ * Every matrix has a row stride ld in elements, at least its columns (0: its
+ * columns); bytes between a row's end and the next row are never written, and
+ * what they hold does not matter. Pointers need the alignment of their elements only
+ * (int8 any address): rows of 16-byte aligned addresses and strides run
+ * fastest. Two matrices of one call may be column ranges of one buffer (of one
+ * stride); an output must share no element with an input or another output, but
+ * for qnorm's sum. rows == 0 is a no-op. The calls allocate nothing and may be
+ * recorded into a graph. */
+enum { AQD_F32 = 0, AQD_F16 = 1, AQD_BF16 = 2 };   /* types of real-valued tensors */
+
+/* Row quantisation: x [rows][cols] real, per row
+ *   m = max(max_c |x[c]|, 2^-119);  codes[c] = rint(x[c] * (127 / m));  scale = m / 127
+ * in fp32, rint to the nearest even integer: codes lie in [-127, 127], a row of
+ * zeros has codes 0. A row that holds an infinity or a NaN has codes 0 and the
+ * scale NaN. Quantises activations, and offline the weights [n][k] of qlin. */
+typedef struct {
+    int rows, cols; /* cols >= 1 */
+    int type;       /* AQD_F32, AQD_F16 or AQD_BF16 */
+    int64_t ld_x, ld_codes;
+} qrows_desc_t;
+aqd_status_t qrows_run(const qrows_desc_t *desc, const void *x, int8_t *codes, float *scales,
+                       aqd_stream_t stream);
+
+/* Residual addition, root-mean-square norm and row quantisation in one pass:
+ *   s[c] = x[c] + residual[c]             (fp32; without a residual s = x)
+ *   sum[c] = s[c] rounded to `type`       (the next residual; not written if NULL)
+ *   u[c] = s[c] * weight[c]
+ *   codes, m as qrows' of u;  scale = m / sqrt(mean(s^2) + eps) / 127
+ * so that codes * scale is the normalised row: the norm's factor is the same for
+ * the whole row and appears in its scale alone. s is not rounded before the
+ * norm; squares are summed in fp32. A row whose u or sum of squares is not
+ * finite has codes 0 and the scale NaN. All tensors are of `type`; weight has
+ * cols elements. sum may be residual or x (with its stride): in place. */
+typedef struct {
+    int rows, cols; /* cols >= 1 */
+    int type;
+    float eps;      /* finite, >= 0 */
+    int64_t ld_x, ld_residual, ld_sum, ld_codes;
+} qnorm_desc_t;
+aqd_status_t qnorm_run(const qnorm_desc_t *desc, const void *x, const void *residual, const void *weight,
+                       void *sum, int8_t *codes, float *scales, aqd_stream_t stream);
+
+/* Linear layer on 8-bit codes:
+ *   acc[t][j] = sum over c of x[t][c] * w[j][c]                    (int32, exact)
+ *   z[t][j] = acc * x_scales[t] * w_scales[j] + bias[j]            (fp32)
+ *   AQD_QLIN_PLAIN:     y[t][j] = z[t][j], j < n; w has n rows
+ *   AQD_QLIN_SILU_GATE: y[t][j] = z[t][j] / (1 + exp(-z[t][j])) * z[t][n + j]; w has 2n
+ *                       rows, the gate's n first (a gated feed-forward unit)
+ * rounded once to `type`. x: [rows][k] int8, w: [n or 2n][k] int8, all 256 code
+ * values; x_scales [rows], w_scales and bias (NULL: none) one per row of w. NaN and
+ * infinite scales act as in fp32: a row whose scale is NaN gives a row of NaN.
+ * UNSUPPORTED for k > 131071, from where on a sum could leave int32.
+ *
+ * workspace (device, 16-byte aligned, ws_bytes): with it, launches of few output tiles split
+ * the sum over k between workgroups, partial sums (int32, exact) in the workspace.
+ * qlin_workspace gives the size for a call (0: it does not split; never more than
+ * AQD_QLIN_WORKSPACE_BYTES, which therefore serves every call); less than that, or NULL, runs
+ * unsplit with the same result, bit for bit. Calls that share a workspace must not overlap in time.
+ * Its size depends on the description alone. */
+#define AQD_QLIN_WORKSPACE_BYTES (64u << 20)
+enum { AQD_QLIN_PLAIN = 0, AQD_QLIN_SILU_GATE = 1 };
+typedef struct {
+    int rows, n, k; /* n >= 1, k >= 1 */
+    int type;       /* of y */
+    int act;        /* AQD_QLIN_* */
+    int64_t ld_x, ld_w, ld_y;
+} qlin_desc_t;
+aqd_status_t qlin_workspace(const qlin_desc_t *desc, size_t *bytes);
+aqd_status_t qlin_run(const qlin_desc_t *desc, const int8_t *x, const float *x_scales, const int8_t *w,
+                      const float *w_scales, const float *bias, void *y, void *workspace, size_t ws_bytes,
+                      aqd_stream_t stream);
 
 /* Diagnostic for measurements (the benchmark's measured ceiling next to the
  * dense int8 peak figure): launches `workgroups` workgroups of 4 waves,

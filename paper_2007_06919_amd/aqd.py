@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_double, c_int, c_int32, c_int64, c_void_p
+from ctypes import POINTER, c_double, c_float, c_int, c_int32, c_int64, c_void_p
 
 import numpy as np
 
@@ -21,6 +21,9 @@ AQD_OK, AQD_ERR_INVALID, AQD_ERR_UNSUPPORTED, AQD_ERR_NOMEM, AQD_ERR_DEVICE = ra
 WENC_TWOS, WENC_PAPER_ODD = 0, 1
 OUT_CODES, OUT_INT32 = 0, 1
 MAX_SEGS = 16
+F32, F16, BF16 = 0, 1, 2
+QLIN_PLAIN, QLIN_SILU_GATE = 0, 1
+QLIN_WORKSPACE_BYTES = 64 << 20
 
 STATUS_NAMES = {0: "AQD_OK", 1: "AQD_ERR_INVALID", 2: "AQD_ERR_UNSUPPORTED",
                 3: "AQD_ERR_NOMEM", 4: "AQD_ERR_DEVICE"}
@@ -58,6 +61,21 @@ class MaxpoolDesc(ctypes.Structure):
     _fields_ = [(n, c_int) for n in ("n", "h", "w", "c", "bits", "k", "stride", "pad")]
 
 
+class QrowsDesc(ctypes.Structure):
+    _fields_ = [(n, c_int) for n in ("rows", "cols", "type")] + \
+               [(n, c_int64) for n in ("ld_x", "ld_codes")]
+
+
+class QnormDesc(ctypes.Structure):
+    _fields_ = [(n, c_int) for n in ("rows", "cols", "type")] + [("eps", c_float)] + \
+               [(n, c_int64) for n in ("ld_x", "ld_residual", "ld_sum", "ld_codes")]
+
+
+class QlinDesc(ctypes.Structure):
+    _fields_ = [(n, c_int) for n in ("rows", "n", "k", "type", "act")] + \
+               [(n, c_int64) for n in ("ld_x", "ld_w", "ld_y")]
+
+
 class QaddParams(ctypes.Structure):
     _fields_ = [(n, c_void_p) for n in ("skip_c", "skip_d", "skip_side", "mult", "shift")]
 
@@ -87,6 +105,10 @@ def lib():
             "qadd_run": ([POINTER(QaddDesc), vp, vp, vp, POINTER(QaddParams), vp], st),
             "aqd_channel_sums": ([vp, c_int64, i, vp, vp], st),
             "aqd_maxpool_run": ([POINTER(MaxpoolDesc), vp, vp, vp], st),
+            "qrows_run": ([POINTER(QrowsDesc), vp, vp, vp, vp], st),
+            "qnorm_run": ([POINTER(QnormDesc), vp, vp, vp, vp, vp, vp, vp], st),
+            "qlin_workspace": ([POINTER(QlinDesc), POINTER(ctypes.c_size_t)], st),
+            "qlin_run": ([POINTER(QlinDesc), vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp], st),
             "aqd_mfma_probe": ([i, i, vp, vp], st),
             "aqd_graph_begin": ([vp], st),
             "aqd_graph_end": ([vp, POINTER(c_void_p)], st),
@@ -114,7 +136,8 @@ def exported_symbols():
     return ["qconv_create", "qconv_out_shape", "qconv_scales", "qconv_run", "qconv_run_group",
             "qconv_group_workspace", "qconv_run_group_ws", "qconv_run_group_static",
             "qconv_run_proj", "qconv_destroy", "qconv_path",
-            "qadd_run", "aqd_maxpool_run", "aqd_mfma_probe", "aqd_channel_sums", "aqd_graph_begin", "aqd_graph_end",
+            "qadd_run", "aqd_maxpool_run", "qrows_run", "qnorm_run", "qlin_workspace", "qlin_run",
+            "aqd_mfma_probe", "aqd_channel_sums", "aqd_graph_begin", "aqd_graph_end",
             "aqd_graph_launch", "aqd_graph_destroy", "aqd_last_error", "aqd_pack_codes",
             "aqd_unpack_codes", "aqd_approx_ratio", "aqd_normalize_multiplier",
             "aqd_bn_stats_from_sums", "aqd_fold_bn", "aqd_skip_params", "aqd_requant_params"]
@@ -257,6 +280,47 @@ def maxpool_run(n, h, w, c, bits, k, stride, pad, x, y, stream=None):
     """Max-pooling of a code tensor (see aqd.h)."""
     d = MaxpoolDesc(n, h, w, c, bits, k, stride, pad)
     _check(lib().aqd_maxpool_run(ctypes.byref(d), _addr(x), _addr(y), _stream(stream)))
+
+
+# --------------------------------------------------- 8-bit linear layers
+def real_type(t) -> int:
+    """F32, F16 or BF16 of a torch tensor or dtype."""
+    name = str(getattr(t, "dtype", t))
+    try:
+        return {"torch.float32": F32, "torch.float16": F16, "torch.bfloat16": BF16}[name]
+    except KeyError:
+        raise TypeError(f"real-valued tensors are float32, float16 or bfloat16, not {name}") from None
+
+
+def qrows_run(rows, cols, type, x, ld_x, codes, ld_codes, scales, stream=None):
+    """Rows of real numbers to int8 codes and one scale per row (see aqd.h; ld 0: packed)."""
+    d = QrowsDesc(rows, cols, type, ld_x, ld_codes)
+    _check(lib().qrows_run(ctypes.byref(d), _addr(x), _addr(codes), _addr(scales), _stream(stream)))
+
+
+def qnorm_run(rows, cols, type, eps, x, ld_x, residual, ld_residual, weight, sum, ld_sum, codes, ld_codes, scales,
+              stream=None):
+    """Residual addition, root-mean-square norm and row quantisation (see aqd.h). residual
+    and sum may be None; sum may be residual or x."""
+    d = QnormDesc(rows, cols, type, eps, ld_x, ld_residual, ld_sum, ld_codes)
+    _check(lib().qnorm_run(ctypes.byref(d), _addr(x), _addr(residual), _addr(weight), _addr(sum), _addr(codes),
+                           _addr(scales), _stream(stream)))
+
+
+def qlin_workspace(rows, n, k, type, act, ld_x=0, ld_w=0, ld_y=0) -> int:
+    """Workspace bytes with which qlin_run splits the sum over k (0: it does not; at most QLIN_WORKSPACE_BYTES)."""
+    d = QlinDesc(rows, n, k, type, act, ld_x, ld_w, ld_y)
+    b = ctypes.c_size_t(0)
+    _check(lib().qlin_workspace(ctypes.byref(d), ctypes.byref(b)))
+    return b.value
+
+
+def qlin_run(rows, n, k, type, act, x, ld_x, x_scales, w, ld_w, w_scales, bias, y, ld_y, workspace=None, ws_bytes=0,
+             stream=None):
+    """Linear layer on int8 codes with scales per row and channel, plain or gated (see aqd.h)."""
+    d = QlinDesc(rows, n, k, type, act, ld_x, ld_w, ld_y)
+    _check(lib().qlin_run(ctypes.byref(d), _addr(x), _addr(x_scales), _addr(w), _addr(w_scales), _addr(bias), _addr(y),
+                          _addr(workspace), ws_bytes, _stream(stream)))
 
 
 def mfma_probe(workgroups, iters, out, stream=None):

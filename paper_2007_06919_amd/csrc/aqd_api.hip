@@ -1758,6 +1758,195 @@ void aqd_graph_destroy(void *graph_exec)
         (void)hipGraphExecDestroy((hipGraphExec_t)graph_exec);
 }
 
+}  // extern "C"
+
+// ------------------------------------------------------------------ 8-bit linear layers
+namespace {
+
+int real_size(int type) { return type == AQD_F32 ? 4 : type == AQD_F16 || type == AQD_BF16 ? 2 : 0; }
+
+// a matrix as the bytes of its rows
+struct Span {
+    uintptr_t at;
+    long long ld, width, rows;   // bytes
+};
+
+Span span(const void *p, long long rows, long long ld, long long cols, int size)
+{
+    return {(uintptr_t)p, ld * size, cols * size, rows};
+}
+
+// whether two matrices may share a byte: their address ranges meet, unless they are
+// disjoint column ranges of rows of one stride
+bool share(const Span &a, const Span &b)
+{
+    if (!a.at || !b.at || !a.rows || !b.rows)
+        return false;
+    const uintptr_t ea = a.at + (uintptr_t)((a.rows - 1) * a.ld + a.width), eb = b.at + (uintptr_t)((b.rows - 1) * b.ld + b.width);
+    if (a.at >= eb || b.at >= ea)
+        return false;
+    if (a.ld != b.ld)
+        return true;
+    // b's first column, counted from a's within a row
+    const long long d = (long long)((b.at >= a.at ? b.at - a.at : (uintptr_t)a.ld - (a.at - b.at) % (uintptr_t)a.ld) % (uintptr_t)a.ld);
+    return d < a.width || d + b.width > a.ld;
+}
+
+bool aligned_to(const void *p, int size) { return ((uintptr_t)p & (uintptr_t)(size - 1)) == 0; }
+
+// strides: none below the columns, and the matrix inside the address space
+bool stride_ok(int64_t ld, int rows, int cols)
+{
+    return ld >= cols && (rows <= 1 || ld <= (INT64_C(1) << 56) / rows);
+}
+
+aqd_status_t rows_call(RowsArgs &a, int rows, hipStream_t stream)
+{
+    const int size = real_size(a.type);
+    REQUIRE(rows >= 0 && a.cols >= 1, "rows must be at least 0 and cols at least 1");
+    REQUIRE(size, "type must be AQD_F32, AQD_F16 or AQD_BF16");
+    a.rows = rows;
+    for (long long *ld : {&a.ld_x, &a.ld_residual, &a.ld_sum, &a.ld_codes}) {
+        if (!*ld)
+            *ld = a.cols;
+    }
+    REQUIRE(stride_ok(a.ld_x, rows, a.cols) && stride_ok(a.ld_codes, rows, a.cols), "a row stride is below the columns or too large");
+    REQUIRE(!a.residual || stride_ok(a.ld_residual, rows, a.cols), "a row stride is below the columns or too large");
+    REQUIRE(!a.sum || stride_ok(a.ld_sum, rows, a.cols), "a row stride is below the columns or too large");
+    if (rows == 0)
+        return AQD_OK;
+    REQUIRE(a.x && a.codes && a.scales && (!a.norm || a.weight), "null pointer");
+    REQUIRE(aligned_to(a.x, size) && aligned_to(a.residual, size) && aligned_to(a.weight, size) && aligned_to(a.sum, size) &&
+                aligned_to(a.scales, 4),
+            "a pointer is not aligned to its elements");
+    const Span x = span(a.x, rows, a.ld_x, a.cols, size), r = span(a.residual, rows, a.ld_residual, a.cols, size);
+    const Span s = span(a.sum, rows, a.ld_sum, a.cols, size), w = span(a.weight, 1, a.cols, a.cols, size);
+    const Span c = span(a.codes, rows, a.ld_codes, a.cols, 1), q = span(a.scales, 1, rows, rows, 4);
+    const bool on_x = a.sum && a.sum == a.x && a.ld_sum == a.ld_x, on_r = a.sum && a.sum == a.residual && a.ld_sum == a.ld_residual;
+    REQUIRE((on_x || !share(s, x)) && (on_r || !share(s, r)) && !share(s, w), "sum overlaps an input that it is not in place of");
+    REQUIRE(!share(c, x) && !share(c, r) && !share(c, w) && !share(c, s), "codes overlap another tensor");
+    REQUIRE(!share(q, x) && !share(q, r) && !share(q, w) && !share(q, s) && !share(q, c), "scales overlap another tensor");
+    if (launch_qrows(a, stream) != hipSuccess)
+        return fail(AQD_ERR_DEVICE, "row quantisation launch failed");
+    return AQD_OK;
+}
+
+aqd_status_t qlin_args(const qlin_desc_t *d, QlinArgs &a)
+{
+    REQUIRE(d, "null description");
+    REQUIRE(d->rows >= 0 && d->n >= 1 && d->k >= 1, "rows must be at least 0, n and k at least 1");
+    REQUIRE(real_size(d->type), "type must be AQD_F32, AQD_F16 or AQD_BF16");
+    REQUIRE(d->act == AQD_QLIN_PLAIN || d->act == AQD_QLIN_SILU_GATE, "unknown act");
+    a.gate = d->act == AQD_QLIN_SILU_GATE;
+    REQUIRE(d->n <= (a.gate ? INT32_MAX / 2 : INT32_MAX) - 256 && d->rows <= INT32_MAX - 256, "too many rows or channels");
+    a.rows = d->rows;
+    a.n = d->n;
+    a.k = d->k;
+    a.wide = a.gate ? 2 * d->n : d->n;
+    a.type = d->type;
+    a.ld_x = d->ld_x ? d->ld_x : d->k;
+    a.ld_w = d->ld_w ? d->ld_w : d->k;
+    a.ld_y = d->ld_y ? d->ld_y : d->n;
+    REQUIRE(stride_ok(a.ld_x, a.rows, a.k) && stride_ok(a.ld_w, a.wide, a.k) && stride_ok(a.ld_y, a.rows, a.n),
+            "a row stride is below the columns or too large");
+    if (a.k > 131071)
+        return fail(AQD_ERR_UNSUPPORTED, "a sum over k > 131071 could exceed int32");
+    return AQD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+aqd_status_t qrows_run(const qrows_desc_t *d, const void *x, int8_t *codes, float *scales, aqd_stream_t stream)
+{
+    REQUIRE(d, "null description");
+    RowsArgs a = {};
+    a.x = x;
+    a.codes = codes;
+    a.scales = scales;
+    a.ld_x = d->ld_x;
+    a.ld_codes = d->ld_codes;
+    a.cols = d->cols;
+    a.type = d->type;
+    return rows_call(a, d->rows, (hipStream_t)stream);
+}
+
+aqd_status_t qnorm_run(const qnorm_desc_t *d, const void *x, const void *residual, const void *weight, void *sum,
+                       int8_t *codes, float *scales, aqd_stream_t stream)
+{
+    REQUIRE(d, "null description");
+    REQUIRE(std::isfinite(d->eps) && d->eps >= 0.f, "eps must be finite and not negative");
+    RowsArgs a = {};
+    a.x = x;
+    a.residual = residual;
+    a.weight = weight;
+    a.sum = sum;
+    a.codes = codes;
+    a.scales = scales;
+    a.ld_x = d->ld_x;
+    a.ld_residual = d->ld_residual;
+    a.ld_sum = d->ld_sum;
+    a.ld_codes = d->ld_codes;
+    a.cols = d->cols;
+    a.type = d->type;
+    a.norm = 1;
+    a.eps = d->eps;
+    return rows_call(a, d->rows, (hipStream_t)stream);
+}
+
+aqd_status_t qlin_workspace(const qlin_desc_t *d, size_t *bytes)
+{
+    REQUIRE(bytes, "null output pointer");
+    QlinArgs a = {};
+    const aqd_status_t st = qlin_args(d, a);
+    if (st != AQD_OK)
+        return st;
+    *bytes = 0;
+    if (a.rows)
+        (void)qlin_parts(a, bytes);
+    return AQD_OK;
+}
+
+aqd_status_t qlin_run(const qlin_desc_t *d, const int8_t *x, const float *x_scales, const int8_t *w, const float *w_scales,
+                      const float *bias, void *y, void *workspace, size_t ws_bytes, aqd_stream_t stream)
+{
+    QlinArgs a = {};
+    const aqd_status_t st = qlin_args(d, a);
+    if (st != AQD_OK || !a.rows)
+        return st;
+    const int size = real_size(a.type);
+    REQUIRE(x && x_scales && w && w_scales && y, "null pointer");
+    REQUIRE(aligned_to(x_scales, 4) && aligned_to(w_scales, 4) && aligned_to(bias, 4) && aligned_to(y, size),
+            "a pointer is not aligned to its elements");
+    REQUIRE(aligned16(workspace), "the workspace must be 16-byte aligned");
+    const Span out = span(y, a.rows, a.ld_y, a.n, size);
+    const Span in[] = {span(x, a.rows, a.ld_x, a.k, 1), span(w, a.wide, a.ld_w, a.k, 1), span(x_scales, 1, a.rows, a.rows, 4),
+                       span(w_scales, 1, a.wide, a.wide, 4), span(bias, 1, a.wide, a.wide, 4)};
+    for (const Span &s : in)
+        REQUIRE(!share(out, s), "y overlaps an input");
+    a.x = x;
+    a.w = w;
+    a.x_scales = x_scales;
+    a.w_scales = w_scales;
+    a.bias = bias;
+    a.y = y;
+    size_t need = 0;
+    a.ksplit = workspace ? qlin_parts(a, &need) : 1;
+    if (a.ksplit > 1 && ws_bytes >= need) {
+        const Span ws = {(uintptr_t)workspace, (long long)need, (long long)need, 1};
+        REQUIRE(!share(ws, out), "the workspace overlaps y");
+        for (const Span &s : in)
+            REQUIRE(!share(ws, s), "the workspace overlaps an input");
+        a.part = (int32_t *)workspace;
+    } else {
+        a.ksplit = 1;
+    }
+    if (launch_qlin(a, (hipStream_t)stream) != hipSuccess)
+        return fail(AQD_ERR_DEVICE, "linear layer launch failed");
+    return AQD_OK;
+}
+
 // ------------------------------------------------------------------ host helpers
 aqd_status_t aqd_pack_codes(const uint8_t *codes, int64_t rows, int c, int bits, uint8_t *out)
 {

@@ -201,4 +201,33 @@ hipError_t launch_maxpool(const PoolArgs &a, hipStream_t stream);
 hipError_t launch_channel_sums(const int32_t *v, long long rows, int c, long long *sums,
                                hipStream_t stream);
 
+// ---- rows of real numbers to 8-bit codes (qrows.hip) ----------------------------
+struct RowsArgs {
+    const void *x, *residual, *weight;   // residual may be null; weight only with norm
+    void *sum;                           // may be null
+    int8_t *codes;
+    float *scales;
+    long long rows, ld_x, ld_residual, ld_sum, ld_codes;
+    int cols, type, norm;
+    float eps;
+};
+hipError_t launch_qrows(const RowsArgs &a, hipStream_t stream);
+
+// ---- linear layers on 8-bit codes (qlin.hip) --------------------------------------
+struct QlinArgs {
+    const int8_t *x, *w;
+    const float *x_scales, *w_scales, *bias;   // bias may be null
+    void *y;
+    long long ld_x, ld_w, ld_y;
+    int rows, n, k, wide;                      // wide: rows of w (n, or 2n with the gate)
+    int type, gate;
+    int ksplit, kchunk;                        // parts of the K range and their bytes (1: all of k)
+    int32_t *part;                             // [ksplit][rows][1, or 2 with the gate][n_pad] partial sums of a split
+    int n_pad;                                 // n rounded up to 4
+};
+// the parts a launch is split into where it has a workspace (1: it is not split), and the bytes
+// that takes, by the description alone
+int qlin_parts(const QlinArgs &a, size_t *bytes);
+hipError_t launch_qlin(const QlinArgs &a, hipStream_t stream);
+
 }  // namespace aqd

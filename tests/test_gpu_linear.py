@@ -1,0 +1,391 @@
+"""The 8-bit linear layers (qrows, qnorm, qlin) against plain implementations in 64 bits, at the
+edges of their tiles, vectors and types: odd sizes, strides with junk between the rows, addresses
+that are aligned to nothing, rows that are zero or hold no number, the largest sums, offsets past
+32 bits, both acts, with and without the workspace.
+
+Tolerances, from the definitions (u(T): half a unit of T's last place, 2^-24, 2^-11, 2^-8):
+codes: the fp32 steps before the rounding (the division, one product, in qnorm the addition and
+the weight, of the element and of the maximum) err by at most 6 u(F32) of a number up to 127, so a
+code lies within 1/2 + 127 * 6 * 2^-24 (< 1/2 + 5e-5) of the exact number.
+scales: two more roundings; in qnorm the sum of squares, at most 64 additions deep: 64 u(F32).
+y: four roundings of fp32 (int to float, two scales, bias), each at most u(F32) of the product's
+magnitude, and one to T; with the gate the exponential's argument is off by |z| u(F32) and the
+hardware's exponential and reciprocal by one unit each: (|z| + 4) 2^-22 of silu, whose slope is
+at most 1.1."""
+import math
+
+import numpy as np
+import pytest
+
+from paper_2007_06919_amd import aqd
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": aqd.F32, "f16": aqd.F16, "bf16": aqd.BF16}
+HALF = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+LEAST = {"f32": 2.0 ** -150, "f16": 2.0 ** -25, "bf16": 2.0 ** -134}   # half the smallest number
+
+
+def dtype(torch, t):
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[t]
+
+
+def matrix(torch, values, ld, shift=0, junk=None):
+    """`values` [rows][cols] as a device matrix of stride ld, `shift` elements past an aligned address;
+    what lies between the rows and around them is junk."""
+    rows, cols = values.shape
+    buf = torch.full((shift + rows * ld + 64,), junk if junk is not None else 113, dtype=values.dtype, device="cuda:0")
+    view = buf[shift:shift + rows * ld].view(rows, ld)[:, :cols]
+    view.copy_(values)
+    return buf, view
+
+
+def untouched(torch, buf, view, junk):
+    """Nothing of buf outside view was written."""
+    copy = buf.clone()
+    at = view.storage_offset()
+    rows, cols = view.shape
+    copy[at:at + rows * view.stride(0)].view(rows, view.stride(0))[:, :cols] = junk
+    return bool((copy == junk).all())
+
+
+def reals(torch, rng, rows, cols, t, big=1.0):
+    x = rng.standard_normal((rows, cols)) * big
+    if cols > 4:
+        x[:, cols // 3] *= 30
+    return torch.from_numpy(x).to(dtype(torch, t))
+
+
+def check_codes(codes, exact, m):
+    """codes against exact * 127 / m, row by row (all float64 on the host)."""
+    want = exact * (127.0 / np.maximum(m, 2.0 ** -119))[:, None]
+    assert np.abs(codes - want).max(initial=0) <= 0.5 + 5e-5
+    assert np.abs(codes).max(initial=0) <= 127
+
+
+ROWS = [(1, 1, 0, 0), (1, 64, 0, 0), (5, 7, 0, 0), (4, 512, 0, 0), (3, 511, 513, 1), (9, 513, 520, 0), (2, 1024, 1024, 0),
+        (7, 1031, 0, 3), (6, 2048, 2056, 0), (3, 2051, 0, 0), (5, 4096, 0, 0), (2, 4097, 4100, 2), (3, 8192, 0, 0),
+        (2, 9000, 9001, 5), (3, 16384, 0, 0), (2, 16385, 0, 0), (2, 32768, 0, 0), (2, 32771, 32775, 1), (1000, 96, 0, 0)]
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("rows, cols, ld, shift", ROWS)
+def test_rows(rows, cols, ld, shift, t):
+    import torch
+    rng = np.random.Generator(np.random.PCG64(rows * 7919 + cols))
+    x = reals(torch, rng, rows, cols, t, 3.0)
+    if rows > 2:
+        x[1] = 0
+        x[2] *= 1e-3
+    _, xd = matrix(torch, x, ld or cols, shift)
+    cbuf, codes = matrix(torch, torch.zeros(rows, cols, dtype=torch.int8), ld + 3 if ld else cols, shift, junk=99)
+    scales = torch.full((rows,), -1.0, device="cuda:0")
+    aqd.qrows_run(rows, cols, TYPES[t], xd, xd.stride(0) if ld else 0, codes, codes.stride(0) if ld else 0, scales)
+    torch.cuda.synchronize()
+    xe = x.double().numpy()
+    m = np.abs(xe).max(1)
+    check_codes(codes.cpu().numpy().astype(np.float64), xe, m)
+    assert np.allclose(scales.cpu().numpy(), np.maximum(m, 2.0 ** -119) / 127, rtol=2 * 2.0 ** -24, atol=0)
+    assert untouched(torch, cbuf, codes, 99)
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("residual, total", [(True, "own"), (True, "residual"), (True, "x"), (True, None), (False, None),
+                                             (False, "own")])
+@pytest.mark.parametrize("rows, cols, ld, shift", ROWS)
+def test_norm(rows, cols, ld, shift, residual, total, t):
+    import torch
+    rng = np.random.Generator(np.random.PCG64(rows * 104729 + cols))
+    x, r = reals(torch, rng, rows, cols, t, 2.0), reals(torch, rng, rows, cols, t, 0.5)
+    w = torch.from_numpy(1 + 0.3 * rng.standard_normal(cols)).to(dtype(torch, t))
+    if rows > 2:
+        x[1] = 0
+        r[1] = 0
+    _, xd = matrix(torch, x, ld or cols, shift)
+    _, rd = matrix(torch, r, cols + 5, shift)
+    _, wd = matrix(torch, w[None], cols, shift)
+    sbuf, sd = matrix(torch, torch.zeros_like(x), cols + 9, shift, junk=7)
+    cbuf, codes = matrix(torch, torch.zeros(rows, cols, dtype=torch.int8), cols + 1, shift, junk=99)
+    scales = torch.full((rows,), -1.0, device="cuda:0")
+    out = {"own": sd, "residual": rd, "x": xd, None: None}[total]
+    aqd.qnorm_run(rows, cols, TYPES[t], 1e-5, xd, xd.stride(0), rd if residual else None, rd.stride(0), wd, out,
+                  out.stride(0) if total else 0, codes, codes.stride(0), scales)
+    torch.cuda.synchronize()
+    s = x.double() + r.double() if residual else x.double()
+    if total:
+        want = (x.float() + r.float() if residual else x.float()).to(x.dtype)
+        assert torch.equal(out.cpu(), want)
+    s = s.numpy()
+    u = s * w.double().numpy()
+    m = np.abs(u).max(1)
+    check_codes(codes.cpu().numpy().astype(np.float64), u, m)
+    want = np.maximum(m, 2.0 ** -119) / np.sqrt((s * s).mean(1) + float(np.float32(1e-5))) / 127
+    assert np.allclose(scales.cpu().numpy(), want, rtol=64 * 2.0 ** -24, atol=0)
+    assert untouched(torch, cbuf, codes, 99) and (total != "own" or untouched(torch, sbuf, sd, 7))
+
+
+@pytest.mark.parametrize("cols", [100, 3000, 40000])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+def test_rows_without_numbers(cols, value):
+    """One infinity or NaN anywhere gives its own row codes 0 and the scale NaN, and no other row anything."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(5))
+    x = torch.from_numpy(rng.standard_normal((4, cols))).float().cuda()
+    w = torch.ones(cols, device="cuda:0")
+    codes = [torch.full((4, cols), 9, dtype=torch.int8, device="cuda:0") for _ in range(4)]
+    scales = [torch.zeros(4, device="cuda:0") for _ in range(4)]
+
+    def both(x, c, s):
+        aqd.qrows_run(4, cols, aqd.F32, x, 0, codes[c], 0, scales[s])
+        aqd.qnorm_run(4, cols, aqd.F32, 1e-5, x, 0, None, 0, w, None, 0, codes[c + 1], 0, scales[s + 1])
+        torch.cuda.synchronize()
+
+    both(x, 0, 0)
+    bad = x.clone()
+    bad[1, 0], bad[2, cols - 1] = value, value
+    both(bad, 2, 2)
+    for k in (0, 1):
+        assert (codes[k + 2][1:3] == 0).all() and torch.isnan(scales[k + 2][1:3]).all()
+        for row in (0, 3):
+            assert torch.equal(codes[k][row], codes[k + 2][row]) and scales[k][row] == scales[k + 2][row]
+    # squares that leave fp32
+    aqd.qnorm_run(4, cols, aqd.F32, 1e-5, x * 1e25, 0, None, 0, w, None, 0, codes[0], 0, scales[0])
+    assert (codes[0] == 0).all() and torch.isnan(scales[0]).all()
+
+
+def test_rows_near_zero():
+    """Maxima below 2^-119 are taken as that: finite factors, codes that round to at most a few steps."""
+    import torch
+    x = torch.zeros(3, 64)
+    x[0, 5], x[1, 7], x[2, 9] = 2.0 ** -149, 2.0 ** -120, 2.0 ** -100
+    codes, scales = torch.full((3, 64), 9, dtype=torch.int8, device="cuda:0"), torch.zeros(3, device="cuda:0")
+    aqd.qrows_run(3, 64, aqd.F32, x.cuda(), 0, codes, 0, scales)
+    c = codes.cpu()
+    assert c[0].abs().max() == 0 and c[1, 7] == 64 and c[2, 9] == 127 and c.ne(0).sum() == 2
+    assert np.allclose(scales.cpu().numpy(), np.array([2.0 ** -119, 2.0 ** -119, 2.0 ** -100]) / 127, rtol=2.0 ** -22)
+
+
+def lin_case(torch, rng, rows, n, k, t, act, *, ld=(0, 0, 0), shift=(0, 0), bias=True, codes=None, workspace=True, stream=None):
+    """Run one product and compare it; returns the output."""
+    wide = 2 * n if act == aqd.QLIN_SILU_GATE else n
+    if codes is None:
+        x = rng.integers(-128, 128, (rows, k)).astype(np.int8)
+        w = rng.integers(-128, 128, (wide, k)).astype(np.int8)
+    else:
+        x, w = codes
+    sx = (rng.uniform(0.5, 1.5, rows) / 74).astype(np.float32)
+    sw = (rng.uniform(0.5, 1.5, wide) / (74 * math.sqrt(k))).astype(np.float32)
+    b = rng.standard_normal(wide).astype(np.float32)
+    _, xd = matrix(torch, torch.from_numpy(x), ld[0] or k, shift[0], junk=127)
+    _, wd = matrix(torch, torch.from_numpy(w), ld[1] or k, shift[1], junk=-128)
+    ybuf, y = matrix(torch, torch.zeros(rows, n, dtype=dtype(torch, t)), ld[2] or n, 1 if ld[2] else 0, junk=5)
+    sxd, swd, bd = (torch.from_numpy(a).cuda() for a in (sx, sw, b))
+    size = aqd.qlin_workspace(rows, n, k, TYPES[t], act, xd.stride(0), wd.stride(0), y.stride(0))
+    outs = []
+    for use in ([True, False] if workspace and size else [False]):
+        y.fill_(5)
+        work = torch.full((size + 64,), 0x55, dtype=torch.uint8, device="cuda:0") if use else None
+        torch.cuda.synchronize()
+        aqd.qlin_run(rows, n, k, TYPES[t], act, xd, xd.stride(0), sxd, wd, wd.stride(0), swd, bd if bias else None, y,
+                     y.stride(0), work, size if use else 0, stream)
+        torch.cuda.synchronize()
+        assert untouched(torch, ybuf, y, 5)
+        if use:
+            assert (work[size:] == 0x55).all()
+        outs.append(y.clone())
+    if len(outs) == 2:
+        assert torch.equal(outs[0], outs[1]), "the split sum differs from the whole one"
+    acc = x.astype(np.float64) @ w.astype(np.float64).T
+    p = acc * sx[:, None].astype(np.float64) * sw
+    z = p + (b if bias else 0)
+    ez = (4 * np.abs(p) + np.abs(z)) * 2.0 ** -24
+    if act == aqd.QLIN_SILU_GATE:
+        g, v, eg, ev = z[:, :n], z[:, n:], ez[:, :n], ez[:, n:]
+        silu = g / (1 + np.exp(-g))
+        want = silu * v
+        tol = np.abs(v) * (1.1 * eg + np.abs(silu) * (np.abs(g) + 4) * 2.0 ** -22) + np.abs(silu) * ev + np.abs(want) * 2.0 ** -23
+    else:
+        want, tol = z, ez
+    tol = tol * 1.01 + np.abs(want) * HALF[t] * 1.01 + LEAST[t]
+    got = outs[0].double().cpu().numpy()
+    worst = np.abs(got - want) - tol
+    at = np.unravel_index(worst.argmax(), worst.shape)
+    assert worst.max() <= 0, f"{at}: got {got[at]}, want {want[at]}, allowed {tol[at]}; {int((worst > 0).sum())} of {worst.size}"
+    return outs[0]
+
+
+SIZES = [(1, 1, 1), (1, 64, 64), (1, 5, 515), (2, 63, 17), (3, 1003, 100), (15, 64, 4096), (16, 65, 1024), (17, 33, 1040),
+         (31, 130, 16), (32, 256, 256), (33, 100, 127), (48, 96, 640), (63, 64, 128), (64, 64, 129), (65, 65, 65), (77, 1003, 515),
+         (100, 700, 255), (127, 128, 384), (128, 129, 400), (129, 127, 2000), (200, 513, 1100), (255, 256, 128), (257, 300, 300),
+         (300, 720, 256), (513, 260, 512), (1, 700, 9000), (4, 64, 20000), (60, 70, 8192), (140, 130, 6000), (16, 2100, 512),
+         (1, 4096, 1024), (24, 1536, 1536), (130, 1100, 2048), (600, 1030, 640)]
+
+
+@pytest.mark.parametrize("act", [aqd.QLIN_PLAIN, aqd.QLIN_SILU_GATE])
+@pytest.mark.parametrize("rows, n, k", SIZES)
+def test_product_packed(rows, n, k, act):
+    """Packed rows: aligned ones where k is a multiple of 16, any address else."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(rows * 31 + n * 17 + k))
+    t = list(TYPES)[(rows + n + k) % 3]
+    lin_case(torch, rng, rows, n, k, t, act, bias=(rows + k) % 2 == 0)
+
+
+@pytest.mark.parametrize("act", [aqd.QLIN_PLAIN, aqd.QLIN_SILU_GATE])
+@pytest.mark.parametrize("rows, n, k", SIZES)
+def test_product_strided(rows, n, k, act):
+    """Rows of 16-byte aligned strides with junk past k, and outputs in a wider matrix."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(rows * 37 + n * 11 + k))
+    t = list(TYPES)[(rows + n + k + 1) % 3]
+    up = -(-k // 16) * 16
+    lin_case(torch, rng, rows, n, k, t, act, ld=(up + 32, up, n + 3), bias=(rows + k) % 2 == 1)
+
+
+@pytest.mark.parametrize("shift, extra", [((1, 0), (0, 0)), ((0, 5), (0, 0)), ((16, 32), (0, 0)), ((0, 0), (7, 0)),
+                                          ((0, 0), (0, 9)), ((3, 7), (1, 2)), ((0, 0), (8, 4))])
+@pytest.mark.parametrize("rows, n, k", [(1, 100, 320), (9, 200, 2048), (40, 130, 256), (130, 300, 1024), (300, 520, 390)])
+def test_product_at_any_address(rows, n, k, shift, extra):
+    import torch
+    rng = np.random.Generator(np.random.PCG64(rows + sum(shift) + 3 * sum(extra)))
+    for act in (aqd.QLIN_PLAIN, aqd.QLIN_SILU_GATE):
+        lin_case(torch, rng, rows, n, k, "f32", act, ld=(k + extra[0], k + extra[1], 0), shift=shift)
+
+
+@pytest.mark.parametrize("rows, n", [(1, 16), (20, 40), (70, 200), (300, 300)])
+def test_largest_sums(rows, n):
+    """k = 131071 codes of -128 on both sides: the largest sum that int32 holds; and its negative."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(rows))
+    k = 131071
+    x = np.full((rows, k), -128, np.int8)
+    w = np.full((n, k), -128, np.int8)
+    w[::2] = 127
+    lin_case(torch, rng, rows, n, k, "f32", aqd.QLIN_PLAIN, codes=(x, w))
+
+
+@pytest.mark.parametrize("rows, n, k", [(1, 40, 64), (40, 40, 64), (300, 300, 256)])
+def test_scales_that_are_no_numbers(rows, n, k):
+    """A NaN row scale makes its row NaN, an infinite channel scale its column infinite or NaN, and nothing else changes."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(3))
+    x = torch.from_numpy(rng.integers(1, 128, (rows, k)).astype(np.int8)).cuda()
+    w = torch.from_numpy(rng.integers(1, 128, (n, k)).astype(np.int8)).cuda()
+    sx, sw = torch.rand(rows, device="cuda:0") + 0.5, torch.rand(n, device="cuda:0") + 0.5
+
+    def run():
+        y = torch.zeros(rows, n, device="cuda:0")
+        aqd.qlin_run(rows, n, k, aqd.F32, aqd.QLIN_PLAIN, x, 0, sx, w, 0, sw, None, y, 0)
+        return y
+
+    good = run()
+    sx[0], sw[n - 1] = math.nan, math.inf
+    bad = run()
+    torch.cuda.synchronize()
+    assert torch.isnan(bad[0]).all() and torch.isinf(bad[1:, n - 1]).all()
+    assert torch.equal(bad[1:, :n - 1], good[1:, :n - 1])
+
+
+def test_gate_at_its_ends():
+    """Gates far below and above zero: silu is -0 and the identity there, never NaN."""
+    import torch
+    rows, n, k = 2, 64, 64
+    x = torch.ones(rows, k, dtype=torch.int8, device="cuda:0")
+    w = torch.ones(2 * n, k, dtype=torch.int8, device="cuda:0")
+    w[:n // 2] = -1
+    sx = torch.tensor([1.0, 1e30], device="cuda:0")
+    sw = torch.ones(2 * n, device="cuda:0")
+    sw[n:] = 2.0 ** -120
+    y = torch.zeros(rows, n, device="cuda:0")
+    aqd.qlin_run(rows, n, k, aqd.F32, aqd.QLIN_SILU_GATE, x, 0, sx, w, 0, sw, None, y, 0)
+    y = y.cpu()
+    assert torch.isfinite(y).all()
+    assert (y[:, :n // 2].abs() <= 1e-25 * y[:, n // 2:]).all()
+    assert np.allclose(y[0, n // 2:].numpy(), 64.0 * 64 * 2.0 ** -120, rtol=1e-6)
+
+
+@pytest.mark.parametrize("act", [aqd.QLIN_PLAIN, aqd.QLIN_SILU_GATE])
+@pytest.mark.parametrize("rows, n, far", [(3, 40, "x"), (70, 300, "x"), (300, 40, "x"), (70, 300, "w"), (3, 300, "w"),
+                                          (300, 270, "y")])
+def test_offsets_past_32_bits(rows, n, far, act):
+    """Strides that put the last rows more than 2^32 bytes behind the first."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(8))
+    k, wide = 128, 2 * n if act else n
+    big = {"x": rows, "w": wide, "y": rows}[far]
+    ld = {"x": k, "w": k, "y": n}
+    ld[far] = ((1 << 32) + (1 << 28)) // (big - 1) // 16 * 16 // (4 if far == "y" else 1)
+    x = torch.from_numpy(rng.integers(-128, 128, (rows, k)).astype(np.int8)).cuda()
+    w = torch.from_numpy(rng.integers(-128, 128, (wide, k)).astype(np.int8)).cuda()
+    sx, sw = torch.rand(rows, device="cuda:0") / 1000, torch.rand(wide, device="cuda:0") / 1000
+
+    def wider(m, cols, stride):
+        out = torch.empty(m.shape[0] * stride, dtype=m.dtype, device="cuda:0").view(m.shape[0], stride)[:, :cols]
+        out.copy_(m)
+        return out
+
+    near = torch.zeros(rows, n, device="cuda:0")
+    aqd.qlin_run(rows, n, k, aqd.F32, act, x, 0, sx, w, 0, sw, None, near, 0)
+    xf, wf, yf = wider(x, k, ld["x"]), wider(w, k, ld["w"]), wider(torch.zeros_like(near), n, ld["y"])
+    aqd.qlin_run(rows, n, k, aqd.F32, act, xf, ld["x"], sx, wf, ld["w"], sw, None, yf, ld["y"])
+    torch.cuda.synchronize()
+    assert torch.equal(near, yf) and near.abs().max() > 0
+
+
+def test_rows_past_32_bits():
+    import torch
+    rows, cols = 66000, 65536 + 8
+    x = torch.empty(rows * cols, dtype=torch.bfloat16, device="cuda:0").view(rows, cols)[:, :32]
+    x.copy_(torch.randn(rows, 32, device="cuda:0"))
+    codes = torch.empty(rows * cols, dtype=torch.int8, device="cuda:0").view(rows, cols)[:, 16:48]
+    near, scales = torch.zeros(rows, 32, dtype=torch.int8, device="cuda:0"), torch.zeros(2, rows, device="cuda:0")
+    aqd.qrows_run(rows, 32, aqd.BF16, x, cols, codes, cols, scales[0])
+    aqd.qrows_run(rows, 32, aqd.BF16, x.contiguous(), 0, near, 0, scales[1])
+    torch.cuda.synchronize()
+    assert torch.equal(codes, near) and torch.equal(scales[0], scales[1]) and near.ne(0).any(dim=1).all()
+
+
+def test_on_another_stream_and_in_a_graph():
+    """A gated block recorded into a graph and replayed on new inputs, eager work between the replays."""
+    import torch
+    rows, d, n = 20, 640, 384
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x, r = (torch.randn(rows, d, generator=g, device="cuda").bfloat16() for _ in range(2))
+    w1 = torch.randint(-127, 128, (2 * n, d), generator=g, device="cuda", dtype=torch.int8)
+    w2 = torch.randint(-127, 128, (d, n), generator=g, device="cuda", dtype=torch.int8)
+    s1, s2 = torch.rand(2 * n, generator=g, device="cuda") / 2000, torch.rand(d, generator=g, device="cuda") / 2000
+    gain = torch.ones(d, device="cuda").bfloat16()
+    size = max(aqd.qlin_workspace(rows, n, d, aqd.BF16, aqd.QLIN_SILU_GATE), aqd.qlin_workspace(rows, d, n, aqd.BF16, 0), 16)
+
+    def buffers():
+        return {"sum": torch.empty_like(x), "c1": torch.empty(rows, d, dtype=torch.int8, device="cuda"),
+                "s1": torch.empty(rows, device="cuda"), "h": torch.empty(rows, n, dtype=torch.bfloat16, device="cuda"),
+                "c2": torch.empty(rows, n, dtype=torch.int8, device="cuda"), "s2": torch.empty(rows, device="cuda"),
+                "y": torch.empty_like(x), "work": torch.empty(size, dtype=torch.uint8, device="cuda")}
+
+    def block(b, x, stream):
+        aqd.qnorm_run(rows, d, aqd.BF16, 1e-6, x, 0, r, 0, gain, b["sum"], 0, b["c1"], 0, b["s1"], stream)
+        aqd.qlin_run(rows, n, d, aqd.BF16, aqd.QLIN_SILU_GATE, b["c1"], 0, b["s1"], w1, 0, s1, None, b["h"], 0, b["work"], size, stream)
+        aqd.qrows_run(rows, n, aqd.BF16, b["h"], 0, b["c2"], 0, b["s2"], stream)
+        aqd.qlin_run(rows, d, n, aqd.BF16, aqd.QLIN_PLAIN, b["c2"], 0, b["s2"], w2, 0, s2, None, b["y"], 0, b["work"], size, stream)
+
+    side, mine, eager = torch.cuda.Stream(), buffers(), buffers()
+    torch.cuda.synchronize()
+    block(mine, x, side)
+    torch.cuda.synchronize()
+    aqd.graph_begin(side)
+    block(mine, x, side)
+    graph = aqd.graph_end(side)
+    try:
+        for _ in range(4):
+            x.copy_(torch.randn(rows, d, generator=g, device="cuda"))
+            block(eager, x, None)
+            for b in ("sum", "c1", "s1", "h", "c2", "s2", "y"):
+                mine[b].zero_()
+            torch.cuda.synchronize()
+            aqd.graph_launch(graph, side)
+            torch.cuda.synchronize()
+            for b in ("sum", "c1", "s1", "h", "c2", "s2", "y"):
+                assert torch.equal(mine[b], eager[b]), b
+    finally:
+        aqd.graph_destroy(graph)
