@@ -1903,8 +1903,12 @@ aqd_status_t qlin_workspace(const qlin_desc_t *d, size_t *bytes)
     if (st != AQD_OK)
         return st;
     *bytes = 0;
-    if (a.rows)
-        (void)qlin_parts(a, bytes);
+    if (a.rows) {
+        // addresses are not known here, and unaligned ones may want another split: room for both
+        *bytes = qlin_plan(a, AQD_QLIN_WORKSPACE_BYTES).bytes;
+        a.x = (const int8_t *)1;
+        *bytes = std::max(*bytes, qlin_plan(a, AQD_QLIN_WORKSPACE_BYTES).bytes);
+    }
     return AQD_OK;
 }
 
@@ -1931,18 +1935,15 @@ aqd_status_t qlin_run(const qlin_desc_t *d, const int8_t *x, const float *x_scal
     a.w_scales = w_scales;
     a.bias = bias;
     a.y = y;
-    size_t need = 0;
-    a.ksplit = workspace ? qlin_parts(a, &need) : 1;
-    if (a.ksplit > 1 && ws_bytes >= need) {
-        const Span ws = {(uintptr_t)workspace, (long long)need, (long long)need, 1};
+    a.part = (int32_t *)workspace;
+    const QlinPlan plan = qlin_plan(a, workspace ? std::min<size_t>(ws_bytes, AQD_QLIN_WORKSPACE_BYTES) : 0);
+    if (plan.bytes) {
+        const Span ws = {(uintptr_t)workspace, (long long)plan.bytes, (long long)plan.bytes, 1};
         REQUIRE(!share(ws, out), "the workspace overlaps y");
         for (const Span &s : in)
             REQUIRE(!share(ws, s), "the workspace overlaps an input");
-        a.part = (int32_t *)workspace;
-    } else {
-        a.ksplit = 1;
     }
-    if (launch_qlin(a, (hipStream_t)stream) != hipSuccess)
+    if (launch_qlin(a, plan, (hipStream_t)stream) != hipSuccess)
         return fail(AQD_ERR_DEVICE, "linear layer launch failed");
     return AQD_OK;
 }

@@ -225,9 +225,20 @@ struct QlinArgs {
     int32_t *part;                             // [ksplit][rows][1, or 2 with the gate][n_pad] partial sums of a split
     int n_pad;                                 // n rounded up to 4
 };
-// the parts a launch is split into where it has a workspace (1: it is not split), and the bytes
-// that takes, by the description alone
-int qlin_parts(const QlinArgs &a, size_t *bytes);
-hipError_t launch_qlin(const QlinArgs &a, hipStream_t stream);
+// kernel and tile (outputs x tokens) of a launch: _ANY take rows at any address, FEW16 and FEW64 go by
+// 16 outputs and 16 or 64 tokens (qlin_kernels.h)
+enum { QLIN_ANY = 0, QLIN_64x32, QLIN_64x64, QLIN_128x64, QLIN_128x128, QLIN_256x128, QLIN_256x256,
+       QLIN_128x128_ANY, QLIN_256x256_ANY, QLIN_FEW16, QLIN_FEW64 };
+struct QlinPlan {
+    int shape, parts;   // parts of the k range (1: whole)
+    size_t bytes;       // what their sums take
+};
+QlinPlan qlin_plan(const QlinArgs &a, size_t room);
+hipError_t launch_qlin(const QlinArgs &a, const QlinPlan &plan, hipStream_t stream);
+hipError_t launch_qlin_f32(const QlinArgs &a, int shape, hipStream_t stream);
+hipError_t launch_qlin_f16(const QlinArgs &a, int shape, hipStream_t stream);
+hipError_t launch_qlin_bf16(const QlinArgs &a, int shape, hipStream_t stream);
+hipError_t launch_qlin_part(const QlinArgs &a, int shape, hipStream_t stream);      // partial sums only
+hipError_t launch_qlin_combine(const QlinArgs &a, hipStream_t stream);
 
 }  // namespace aqd

@@ -1,249 +1,136 @@
-// Linear layers on signed 8-bit codes: y = (x w^T) * x_scales * w_scales + bias,
-// plain or as the two halves of a gated unit. Definitions: include/aqd.h.
-//
-// Both operands hold their sum's index contiguously, which is what the int8 MFMA
-// wants of both: a lane's 16 bytes are 16 consecutive k of one row. The weights are
-// the MFMA's rows and the tokens its columns, so a lane's accumulators are
-// consecutive channels of one token and leave as one wide store. Sums are int32
-// and exact; so are the partial sums of a split K range, in any order.
+// Linear layers on 8-bit codes: which kernel a launch takes, and whether its k range is split
+// (host code; the kernels: qlin_kernels.h).
+
+#include <algorithm>
 
 #include "internal.h"
-#include "mfma_common.h"
 
 namespace aqd {
 namespace {
 
-// ---- epilogue -----------------------------------------------------------------
-template <typename T>
-struct Four {
-    typedef T type __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+// A tile shape (outputs x tokens; with the gate twice as many rows of w), how many of its workgroups
+// fit a CU, and its time in us per stage of 128 k while few CUs run and while all do, and per round
+// of workgroups apart from the stages (first loads, stores), with the gate that many times as much.
+// Fitted to launches of 640 random sizes (1 to 11000 tokens, 128 to 16384 outputs and k, plain and
+// gated, every shape with 1 to 8 parts): the plan's launch is 1.6% (aligned rows) and 1.2% slower than
+// the fastest of them on average, 6% and 4% at the ninetieth percentile. One shape for all: 2 to 10 times as
+// slow at the other end of the sizes.
+struct Shape {
+    int shape, out, gate_out, tokens, per_cu;
+    double idle, busy, round, gate;
+};
+const Shape copied[] = {
+    {QLIN_64x32, 64, 64, 32, 3, 0.130, 0.170, 1.56, 2.19},    {QLIN_64x64, 64, 0, 64, 2, 0.135, 0.205, 1.68, 0.0},
+    {QLIN_128x64, 128, 64, 64, 2, 0.214, 0.355, 1.86, 1.40},  {QLIN_128x128, 128, 64, 128, 1, 0.272, 0.526, 2.57, 1.24},
+    {QLIN_256x128, 256, 128, 128, 1, 0.363, 0.889, 4.13, 1.07}, {QLIN_256x256, 256, 128, 256, 1, 0.834, 1.616, 8.02, 1.01},
+};
+const Shape anywhere[] = {
+    {QLIN_ANY, 64, 32, 64, 4, 0.812, 0.532, 2.24, 0.98},
+    {QLIN_128x128_ANY, 128, 64, 128, 2, 0.597, 0.828, 4.30, 0.92},
+    {QLIN_256x256_ANY, 256, 128, 256, 1, 1.039, 1.944, 8.98, 0.97},
 };
 
-// z for four consecutive rows of w from row j on (only the first `left` exist)
-__device__ __forceinline__ void scaled4(const QlinArgs &A, const v4i acc, int j, int left, float sx, float *z)
+constexpr int CUS = 256;
+constexpr double LAUNCH = 2.5, MEMORY = 6.3e6;   // us; bytes per us
+
+// how many b hold a
+inline double up(double a, double b)
 {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        z[e] = (float)acc[e] * sx;
-        if (e < left) {
-            z[e] *= A.w_scales[j + e];
-            if (A.bias)
-                z[e] += A.bias[j + e];
-        }
-    }
+    const double q = a / b, whole = (double)(long long)q;
+    return whole + (q > whole ? 1.0 : 0.0);
 }
 
-// z / (1 + exp(-z)): the exponential and the reciprocal are the hardware's (one unit in
-// the last place each); exp(-z) = infinity gives -0
-__device__ __forceinline__ float silu(float z) { return z * __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+double part_bytes(const QlinArgs &a) { return 4.0 * a.rows * (4.0 * up(a.n, 4)) * (a.gate ? 2 : 1); }
 
-// four consecutive outputs of a token from column j on; value: the gated unit's second half
-template <typename T, bool GATE>
-__device__ __forceinline__ void emit4(const QlinArgs &A, long long t, int j, const v4i acc, const v4i value, float sx)
+double time_of(const QlinArgs &a, const Shape &s, int parts)
 {
-    const int left = A.n - j;
-    if (left <= 0)
-        return;
-    float z[4];
-    scaled4(A, acc, j, left, sx, z);
-    if constexpr (GATE) {
-        float v[4];
-        scaled4(A, value, A.n + j, left, sx, v);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            z[e] = silu(z[e]) * v[e];
-    }
-    T *y = (T *)A.y + t * A.ld_y + j;
-    typename Four<T>::type o;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        o[e] = (T)z[e];
-    if (left >= 4) {
-        *(typename Four<T>::type *)y = o;
-    } else {
-#pragma unroll
-        for (int e = 0; e < 3; ++e)
-            if (e < left)
-                y[e] = o[e];
-    }
+    const double groups = up(a.n, a.gate ? s.gate_out : s.out) * up(a.rows, s.tokens) * parts;
+    const double stages = up(up(a.k, parts), 128), each = up(groups, CUS);
+    const double stage = s.idle + (s.busy - s.idle) * std::min(1.0, groups / CUS);
+    const double work = s.round * (a.gate ? s.gate : 1.0) * up(each, s.per_cu) + stages * each * stage;
+    const double memory = ((double)a.rows * a.k + (double)a.wide * a.k + (double)a.rows * a.n * (a.type == AQD_F32 ? 4 : 2)) / MEMORY;
+    // mostly under one another
+    double t = std::max(work, memory) + 0.25 * std::min(work, memory);
+    // the parts are written and read again, by a launch of its own
+    if (parts > 1)
+        t += 2.8 + 2.0 * parts * part_bytes(a) / 9.8e6;
+    return LAUNCH + t;
 }
 
-// ---- partial sums of a split K range ----------------------------------------------
-// four consecutive sums of a token from column j (a multiple of 4) on; half: 1 for the
-// gated unit's second half
-template <bool GATE>
-__device__ __forceinline__ void put4(const QlinArgs &A, int part, long long t, int j, int half, const v4i acc)
+bool aligned_rows(const QlinArgs &a) { return (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.ld_x | (uintptr_t)a.ld_w) & 15) == 0; }
+
+// The small launches' kernel, in the same way: us per round of 256 workgroups, a fixed part and one per
+// 256 k (with the gate `gate` times as much), and the rate it reads weights at, bytes per us.
+double time_of_few(const QlinArgs &a, int tokens, double fixed, double step, double gate, double rate)
 {
-    if (j < A.n_pad)
-        *(v4i *)(A.part + (((long long)part * A.rows + t) * (GATE ? 2 : 1) + half) * A.n_pad + j) = acc;
-}
-
-template <typename T, bool GATE>
-__global__ void __launch_bounds__(256) qlin_combine_kernel(QlinArgs A)
-{
-    const int quads = (A.n + 3) / 4;
-    const long long idx = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (idx >= (long long)A.rows * quads)
-        return;
-    const long long t = idx / quads;
-    const int j = 4 * (int)(idx - t * quads);
-    const long long line = (long long)A.n_pad * (GATE ? 2 : 1), step = A.rows * line;
-    const int32_t *p = A.part + t * line + j;
-    v4i acc = {0, 0, 0, 0}, value = {0, 0, 0, 0};
-    for (int s = 0; s < A.ksplit; ++s) {
-        acc += *(const v4i *)(p + s * step);
-        if constexpr (GATE)
-            value += *(const v4i *)(p + s * step + A.n_pad);
-    }
-    emit4<T, GATE>(A, t, j, acc, value, A.x_scales[t]);
-}
-
-// ---- any strides: 64 rows of w x 64 tokens, both through registers into LDS ----------
-// 16 bytes of a row at c, zeros from k on. Rows start at any byte; the hardware takes an
-// unaligned 16-byte load. Nothing at or past the row's k-th byte is read.
-__device__ __forceinline__ v4i load16(const int8_t *row, int c, int k)
-{
-    typedef int v4u __attribute__((ext_vector_type(4), aligned(1)));
-    if (c + 16 <= k)
-        return *(const v4u *)(row + c);
-    v4i v = {0, 0, 0, 0};
-#pragma unroll
-    for (int e = 0; e < 16; ++e)
-        if (c + e < k)
-            v[e / 4] |= (int)(uint8_t)row[c + e] << (8 * (e % 4));
-    return v;
-}
-
-constexpr int ANY_TILE = 64;
-
-// Wave i: the 64 rows of w by tokens 16i .. 16i+15. With the gate the tile's first 32 rows
-// are gate rows and the others the value rows of the same outputs.
-template <typename T, bool GATE, bool PART>
-__global__ void __launch_bounds__(256) qlin_any_kernel(QlinArgs A, long long tile0)
-{
-    __shared__ v4i lds[2][2][ANY_TILE * 4];   // [buffer][w, x][row][16-byte column, swizzled]
-    constexpr int OUT = GATE ? ANY_TILE / 2 : ANY_TILE;
-    const int tiles_n = (A.n + OUT - 1) / OUT, tiles_t = (A.rows + ANY_TILE - 1) / ANY_TILE;
-    long long tile = tile0 + blockIdx.x;
-    const int tn = (int)(tile % tiles_n);
-    tile /= tiles_n;
-    const int tt = (int)(tile % tiles_t), part = (int)(tile / tiles_t);
-    const int k0 = part * A.kchunk, k1 = A.k - k0 < A.kchunk ? A.k : k0 + A.kchunk;
-
-    const int r = threadIdx.x >> 2, c = threadIdx.x & 3;
-    const int j = tn * OUT + (GATE ? r % OUT : r);
-    const int row_w = (j < A.n ? j : A.n - 1) + (GATE && r >= OUT ? A.n : 0);
-    const long long row_x = (long long)tt * ANY_TILE + r;
-    const int8_t *pw = A.w + row_w * A.ld_w, *px = A.x + (row_x < A.rows ? row_x : A.rows - 1) * A.ld_x;
-    const int slot = r * 4 + (c ^ ((r >> 1) & 3));
-
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, fc = lane >> 4;
-    v4i acc[4] = {};
-    v4i w = load16(pw, k0 + 16 * c, k1), x = load16(px, k0 + 16 * c, k1);
-    int buf = 0;
-    for (int k = k0; k < k1; k += 64, buf ^= 1) {
-        lds[buf][0][slot] = w;
-        lds[buf][1][slot] = x;
-        __syncthreads();
-        w = load16(pw, k + 64 + 16 * c, k1);
-        x = load16(px, k + 64 + 16 * c, k1);
-        const int rb = 16 * wave + fr;
-        const v4i b = lds[buf][1][rb * 4 + (fc ^ ((rb >> 1) & 3))];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int ra = 16 * i + fr;
-            acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(lds[buf][0][ra * 4 + (fc ^ ((ra >> 1) & 3))], b, acc[i], 0, 0, 0);
-        }
-    }
-    const long long t = (long long)tt * ANY_TILE + 16 * wave + fr;
-    if (t >= A.rows)
-        return;
-    if constexpr (PART) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            put4<GATE>(A, part, t, tn * OUT + (16 * i) % OUT + 4 * fc, 16 * i / OUT, acc[i]);
-    } else {
-        const float sx = A.x_scales[t];
-        if constexpr (GATE) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                emit4<T, true>(A, t, tn * OUT + 16 * i + 4 * fc, acc[i], acc[i + 2], sx);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                emit4<T, false>(A, t, tn * OUT + 16 * i + 4 * fc, acc[i], acc[i], sx);
-        }
-    }
-}
-
-// ---- launches -------------------------------------------------------------------------
-constexpr long long MOST_GROUPS = 1 << 23;   // workgroups of one launch
-
-template <typename T, bool GATE>
-void launch_combine(const QlinArgs &a, hipStream_t stream)
-{
-    const long long items = (long long)a.rows * ((a.n + 3) / 4);   // a split's workspace keeps this small
-    hipLaunchKernelGGL((qlin_combine_kernel<T, GATE>), dim3((unsigned)((items + 255) / 256)), dim3(256), 0, stream, a);
-}
-
-template <typename T, bool GATE>
-void launch_any(const QlinArgs &a, hipStream_t stream)
-{
-    constexpr int OUT = GATE ? ANY_TILE / 2 : ANY_TILE;
-    const long long total = (long long)((a.n + OUT - 1) / OUT) * ((a.rows + ANY_TILE - 1) / ANY_TILE) * a.ksplit;
-    for (long long at = 0; at < total; at += MOST_GROUPS) {
-        const dim3 grid((unsigned)(total - at < MOST_GROUPS ? total - at : MOST_GROUPS));
-        if (a.ksplit > 1)
-            hipLaunchKernelGGL((qlin_any_kernel<T, GATE, true>), grid, dim3(256), 0, stream, a, at);
-        else
-            hipLaunchKernelGGL((qlin_any_kernel<T, GATE, false>), grid, dim3(256), 0, stream, a, at);
-    }
-    if (a.ksplit > 1)
-        launch_combine<T, GATE>(a, stream);
-}
-
-template <typename T>
-void launch_gate(const QlinArgs &a, hipStream_t stream)
-{
-    if (a.gate)
-        launch_any<T, true>(a, stream);
-    else
-        launch_any<T, false>(a, stream);
+    const double groups = up(a.n, 16) * up(a.rows, tokens), steps = up(a.k, 256) * (a.gate ? gate : 1.0);
+    return LAUNCH + std::max((fixed + step * steps) * std::max(1.0, groups / CUS), (double)a.wide * a.k / rate);
 }
 
 }  // namespace
 
-int qlin_parts(const QlinArgs &a, size_t *bytes)
+// The plan of a launch: the fastest shape and split by the times above. `room`: bytes for partial sums.
+QlinPlan qlin_plan(const QlinArgs &a, size_t room)
 {
-    const int out = a.gate ? ANY_TILE / 2 : ANY_TILE;
-    const long long tiles = (long long)((a.n + out - 1) / out) * ((a.rows + ANY_TILE - 1) / ANY_TILE);
-    const int steps = (a.k + 63) / 64;
-    const size_t one = (size_t)a.rows * (size_t)((a.n + 3) & ~3) * (a.gate ? 2 : 1) * sizeof(int32_t);
-    long long parts = 512 / tiles;
-    if (parts > steps / 8)
-        parts = steps / 8;
-    while (parts > 1 && one * parts > AQD_QLIN_WORKSPACE_BYTES)
-        --parts;
-    *bytes = parts > 1 ? one * parts : 0;
-    return parts > 1 ? (int)parts : 1;
+    QlinPlan best = {QLIN_ANY, 1, 0};
+    // offsets inside a tile have 32 bits
+    if (std::max(a.ld_x, a.ld_w) >= 1 << 23)
+        return best;
+    double least = 1e30;
+    const bool aligned = aligned_rows(a);
+    const double one = part_bytes(a);
+    auto consider = [&](const Shape &s) {
+        if (a.gate && !s.gate_out)
+            return;
+        for (int parts : {1, 2, 3, 4, 5, 6, 8}) {
+            if (parts > 1 && (one * parts > (double)room || a.k / parts < 512))
+                break;
+            const double t = time_of(a, s, parts);
+            if (t < least) {
+                least = t;
+                best = {s.shape, parts, parts > 1 ? (size_t)(one * parts) : 0};
+            }
+        }
+    };
+    if (aligned)
+        for (const Shape &s : copied)
+            consider(s);
+    else
+        for (const Shape &s : anywhere)
+            consider(s);
+    // (its workgroups' second grid dimension ends at 65535)
+    auto consider_few = [&](int shape, int tokens, double t) {
+        if (t < least && up(a.rows, tokens) <= 65535) {
+            least = t;
+            best = {shape, 1, 0};
+        }
+    };
+    if (aligned) {
+        if (a.rows <= 16)
+            consider_few(QLIN_FEW16, 16, time_of_few(a, 16, 1.2, 0.09, 2.5, 4.1e6));
+    } else {
+        consider_few(QLIN_FEW16, 16, time_of_few(a, 16, 1.6, 0.26, 1.96, 2.6e6));
+        consider_few(QLIN_FEW64, 64, time_of_few(a, 64, 1.8, 0.41, 1.82, 3.5e6));
+    }
+    return best;
 }
 
-hipError_t launch_qlin(const QlinArgs &args, hipStream_t stream)
+hipError_t launch_qlin(const QlinArgs &args, const QlinPlan &plan, hipStream_t stream)
 {
     QlinArgs a = args;
     a.n_pad = (a.n + 3) & ~3;
-    const int steps = (a.k + 63) / 64;
-    a.kchunk = 64 * ((steps + a.ksplit - 1) / a.ksplit);
+    // whole stages per part
+    const int stages = a.k / 128 + (a.k % 128 != 0);
+    a.kchunk = 128 * ((stages + plan.parts - 1) / plan.parts);
     a.ksplit = (a.k + a.kchunk - 1) / a.kchunk;
-    if (a.ksplit <= 1)
-        a.kchunk = a.k;
-    if (a.type == AQD_F32)
-        launch_gate<float>(a, stream);
-    else if (a.type == AQD_F16)
-        launch_gate<_Float16>(a, stream);
-    else
-        launch_gate<__bf16>(a, stream);
-    return hipGetLastError();
+    if (a.ksplit > 1) {
+        const hipError_t e = launch_qlin_part(a, plan.shape, stream);
+        return e != hipSuccess ? e : launch_qlin_combine(a, stream);
+    }
+    a.kchunk = a.k;
+    return a.type == AQD_F32   ? launch_qlin_f32(a, plan.shape, stream)
+           : a.type == AQD_F16 ? launch_qlin_f16(a, plan.shape, stream)
+                               : launch_qlin_bf16(a, plan.shape, stream);
 }
 
 }  // namespace aqd

@@ -1,0 +1,846 @@
+// Kernels of the linear layers on signed 8-bit codes: y = (x w^T) * x_scales * w_scales
+// + bias, plain or as the two halves of a gated unit (definitions: include/aqd.h). Included by the
+// sources that instantiate them, one for each type of y.
+//
+// Both operands hold their sum's index contiguously, which is what the int8 MFMA
+// wants of both: a lane's 16 bytes are 16 consecutive k of one row. The weights are
+// the MFMA's rows and the tokens its columns, so a lane's accumulators are
+// consecutive channels of one token. Sums are int32 and exact; so are the partial sums of
+// a split k range, in any order: every kernel gives the same bits.
+#pragma once
+
+#include "internal.h"
+#include "mfma_common.h"
+
+namespace aqd {
+namespace {
+
+// ---- epilogue -----------------------------------------------------------------
+template <typename T>
+struct Four {
+    typedef T type __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+};
+
+// z for four consecutive rows of w from row j on (only the first `left` exist)
+__device__ __forceinline__ void scaled4(const QlinArgs &A, const v4i acc, int j, int left, float sx, float *z)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        z[e] = (float)acc[e] * sx;
+        if (e < left) {
+            z[e] *= A.w_scales[j + e];
+            if (A.bias)
+                z[e] += A.bias[j + e];
+        }
+    }
+}
+
+// z / (1 + exp(-z)): the exponential and the reciprocal are the hardware's (one unit in
+// the last place each); exp(-z) = infinity gives -0
+__device__ __forceinline__ float silu(float z) { return z * __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+
+// four consecutive outputs of a token from column j on; value: the gated unit's second half
+template <typename T, bool GATE>
+__device__ __forceinline__ void emit4(const QlinArgs &A, long long t, int j, const v4i acc, const v4i value, float sx)
+{
+    const int left = A.n - j;
+    if (left <= 0)
+        return;
+    float z[4];
+    scaled4(A, acc, j, left, sx, z);
+    if constexpr (GATE) {
+        float v[4];
+        scaled4(A, value, A.n + j, left, sx, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            z[e] = silu(z[e]) * v[e];
+    }
+    T *y = (T *)A.y + t * A.ld_y + j;
+    typename Four<T>::type o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        o[e] = (T)z[e];
+    if (left >= 4) {
+        *(typename Four<T>::type *)y = o;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < left)
+                y[e] = o[e];
+    }
+}
+
+// ---- partial sums of a split K range ----------------------------------------------
+// four consecutive sums of a token from column j (a multiple of 4) on; half: 1 for the
+// gated unit's second half
+template <bool GATE>
+__device__ __forceinline__ void put4(const QlinArgs &A, int part, long long t, int j, int half, const v4i acc)
+{
+    if (j < A.n_pad)
+        *(v4i *)(A.part + (((long long)part * A.rows + t) * (GATE ? 2 : 1) + half) * A.n_pad + j) = acc;
+}
+
+template <typename T, bool GATE>
+__global__ void __launch_bounds__(256) qlin_combine_kernel(QlinArgs A)
+{
+    const int quads = (A.n + 3) / 4;
+    const long long idx = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (idx >= (long long)A.rows * quads)
+        return;
+    const long long t = idx / quads;
+    const int j = 4 * (int)(idx - t * quads);
+    const long long line = (long long)A.n_pad * (GATE ? 2 : 1), step = A.rows * line;
+    const int32_t *p = A.part + t * line + j;
+    v4i acc = {0, 0, 0, 0}, value = {0, 0, 0, 0};
+    for (int s = 0; s < A.ksplit; ++s) {
+        acc += *(const v4i *)(p + s * step);
+        if constexpr (GATE)
+            value += *(const v4i *)(p + s * step + A.n_pad);
+    }
+    emit4<T, GATE>(A, t, j, acc, value, A.x_scales[t]);
+}
+
+// ---- loads ------------------------------------------------------------------------------
+// Rows may start at any byte. The hardware takes 16-byte loads at multiples of 4 at full speed, at
+// other addresses at about a third (16 x 4096 x 4096 with rows of 4097 bytes: 19.7 us, of 4100:
+// 7.1); those are loaded as five whole words and shifted. The fifth holds bytes of the
+// 16, or is the fourth again: no load leaves the words that hold the row.
+typedef int v4u __attribute__((ext_vector_type(4), aligned(1)));
+
+struct Words {
+    v4i v;
+    int more;
+};
+// 16 bytes at a wave-uniform base (kept in scalar registers) and a lane's offset. The base is moved
+// down to a word first: an offset of 0 has no room for the shift.
+template <bool BYTES>
+__device__ __forceinline__ Words load_words(const int8_t *base, uint32_t off)
+{
+    typedef int v4w __attribute__((ext_vector_type(4), aligned(4)));
+    const uint32_t low = BYTES ? (uint32_t)(uintptr_t)base & 3 : 0;
+    auto p = (const __attribute__((address_space(1))) int8_t *)(base - low);
+    asm("" : "+s"(p));
+    Words r = {};
+    const uint32_t o = (off + low) & ~3u;
+    if constexpr (BYTES) {
+        r.v = *(const __attribute__((address_space(1))) v4w *)(p + o);
+        r.more = *(const __attribute__((address_space(1))) int *)(p + (o + ((off + low) & 3 ? 16u : 12u)));
+    } else {
+        r.v = *(const __attribute__((address_space(1))) v4w *)(p + off);
+    }
+    return r;
+}
+// the 16 bytes of what was loaded; shift: the last two bits of their address
+template <bool BYTES>
+__device__ __forceinline__ v4i shifted(const Words &r, int shift)
+{
+    if constexpr (!BYTES)
+        return r.v;
+    return v4i{(int)__builtin_amdgcn_alignbyte((unsigned)r.v[1], (unsigned)r.v[0], (unsigned)shift),
+               (int)__builtin_amdgcn_alignbyte((unsigned)r.v[2], (unsigned)r.v[1], (unsigned)shift),
+               (int)__builtin_amdgcn_alignbyte((unsigned)r.v[3], (unsigned)r.v[2], (unsigned)shift),
+               (int)__builtin_amdgcn_alignbyte((unsigned)r.more, (unsigned)r.v[3], (unsigned)shift)};
+}
+
+// The 16 bytes of a row from c on where the row may end (at k) inside them or before them: nothing
+// past it is read. A sum's terms have no order, so the 16 bytes then are the row's last, and
+// the terms that another lane or step has too are zeros in the tokens (TOKEN).
+template <bool TOKEN>
+__device__ __forceinline__ v4i load16(const int8_t *row, int c, int k)
+{
+    v4i v = {0, 0, 0, 0};
+    if (k < 16) {
+#pragma unroll
+        for (int e = 0; e < 15; ++e)
+            if (c + e < k)
+                v[e / 4] |= (int)(uint8_t)row[c + e] << (8 * (e % 4));
+        return v;
+    }
+    const int at = c < k - 16 ? c : k - 16, gone = c - at;
+    v = *(const v4u *)(row + at);
+    if constexpr (TOKEN)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int z = gone - 4 * e;
+            v[e] = z >= 4 ? 0 : z > 0 ? (int)((uint32_t)v[e] >> (8 * z) << (8 * z)) : v[e];
+        }
+    return v;
+}
+
+// ---- tiles of rows at any address ----------------------------------------------------------
+// 64 rows of w x 64 tokens, both through registers into LDS, 128 k a stage, loaded a stage and
+// a half before they are used. Wave i: the 64 rows of w by tokens 16i .. 16i+15. With the gate the
+// tile's first 32 rows are gate rows and the others the value rows of the same outputs. Takes every
+// stride (64-bit addresses).
+constexpr int KS = 128;   // k of a stage
+
+// XOR of the 16-byte columns of LDS row r (128 bytes): 16-byte reads of consecutive rows at one column
+// hit every bank once whether 8 or 16 lanes are served per cycle
+__device__ __forceinline__ int swz(int r) { return (r ^ (r >> 3 & 1)) & 7; }
+
+constexpr int ANY_TILE = 64;
+
+template <typename T, bool GATE, bool PART>
+__global__ void __launch_bounds__(256) qlin_any_kernel(QlinArgs A, long long tile0)
+{
+    __shared__ v4i lds[2][2][ANY_TILE * 8];   // [buffer][w, x][row][16-byte column, swizzled]
+    constexpr int OUT = GATE ? ANY_TILE / 2 : ANY_TILE;
+    const int tiles_n = (A.n + OUT - 1) / OUT, tiles_t = (A.rows + ANY_TILE - 1) / ANY_TILE;
+    long long tile = tile0 + blockIdx.x;
+    const int tn = (int)(tile % tiles_n);
+    tile /= tiles_n;
+    const int tt = (int)(tile % tiles_t), part = (int)(tile / tiles_t);
+    const int k0 = part * A.kchunk, k1 = A.k - k0 < A.kchunk ? A.k : k0 + A.kchunk;
+
+    const int r = threadIdx.x >> 2, c = threadIdx.x & 3;   // this thread copies columns c and c + 4 of row r
+    const int j = tn * OUT + (GATE ? r % OUT : r);
+    const long long row_w = (j < A.n ? j : A.n - 1) + (GATE && r >= OUT ? (long long)A.n : 0);
+    const long long row_x = (long long)tt * ANY_TILE + r;
+    const int8_t *pw = A.w + row_w * A.ld_w + k0, *px = A.x + (row_x < A.rows ? row_x : A.rows - 1) * A.ld_x + k0;
+    const int kn = k1 - k0;
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, fc = lane >> 4;
+    v4i acc[4] = {};
+    Words w[2] = {}, x[2] = {};
+    const int shift_w = (int)((uintptr_t)pw & 3), shift_x = (int)((uintptr_t)px & 3);
+    int sw = 0, sx = 0;   // the shifts of what is held
+    auto words = [](const int8_t *p, int shift) {
+        const int *q = (const int *)(p - shift);
+        return Words{v4i{q[0], q[1], q[2], q[3]}, q[shift ? 4 : 3]};
+    };
+    auto load = [&](int k) {
+        if (k + KS <= kn) {
+            sw = shift_w;
+            sx = shift_x;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                w[h] = words(pw + k + 16 * c + 64 * h, shift_w);
+                x[h] = words(px + k + 16 * c + 64 * h, shift_x);
+            }
+        } else if (k < kn) {
+            sw = sx = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                w[h].v = load16<false>(pw, k + 16 * c + 64 * h, kn);
+                x[h].v = load16<true>(px, k + 16 * c + 64 * h, kn);
+            }
+        }
+    };
+    auto store = [&](int buf) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            lds[buf][0][r * 8 + ((c + 4 * h) ^ swz(r))] = shifted<true>(w[h], sw);
+            lds[buf][1][r * 8 + ((c + 4 * h) ^ swz(r))] = shifted<true>(x[h], sx);
+        }
+    };
+    load(0);
+    store(0);
+    load(KS);
+    __syncthreads();
+    int buf = 0;
+    for (int k = 0; k < kn; k += KS, buf ^= 1) {
+        if (k + KS < kn) {
+            store(buf ^ 1);
+            load(k + 2 * KS);
+        }
+        const int rb = 16 * wave + fr;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const v4i b = lds[buf][1][rb * 8 + ((fc + 4 * h) ^ swz(rb))];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int ra = 16 * i + fr;
+                acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(lds[buf][0][ra * 8 + ((fc + 4 * h) ^ swz(ra))], b, acc[i], 0, 0, 0);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    const long long t = (long long)tt * ANY_TILE + 16 * wave + fr;
+    if (t >= A.rows)
+        return;
+    if constexpr (PART) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            put4<GATE>(A, part, t, tn * OUT + (16 * i) % OUT + 4 * fc, 16 * i / OUT, acc[i]);
+    } else {
+        const float sx = A.x_scales[t];
+        if constexpr (GATE) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                emit4<T, true>(A, t, tn * OUT + 16 * i + 4 * fc, acc[i], acc[i + 2], sx);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                emit4<T, false>(A, t, tn * OUT + 16 * i + 4 * fc, acc[i], acc[i], sx);
+        }
+    }
+}
+
+// ---- small launches: both operands straight into registers ----------------------------
+// One workgroup per 16 outputs and 16 NB tokens, its waves splitting k, 64 at a time, and adding
+// their sums in LDS: no LDS and no barrier in the loop, and the shortest chain from launch to
+// store. Rows start at any byte, their 16 (tokens: 16 NB) within 32 bits of offset.
+constexpr int FEW_WAVES = 4;
+
+template <typename T, bool GATE, bool BYTES, int NB, int U>
+__global__ void __launch_bounds__(64 * FEW_WAVES) qlin_few_kernel(QlinArgs A)
+{
+    constexpr int H = GATE ? 2 : 1;   // row tiles: with the gate, the gate rows and the value rows
+    __shared__ v4i sums[FEW_WAVES][H * NB][64];
+    // (uniform, so that every condition on it is a scalar branch: MFMAs ignore the execution mask)
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, fr = lane & 15, fc = lane >> 4;
+    const int j0 = blockIdx.x * 16;
+    const long long t0 = (long long)blockIdx.y * 16 * NB;
+    const int8_t *pw[2] = {A.w + j0 * A.ld_w, A.w + ((long long)A.n + j0) * A.ld_w}, *px = A.x + t0 * A.ld_x;
+    const int left = A.n - 1 - j0;
+    const uint32_t vw = (uint32_t)(fr < left ? fr : left) * (uint32_t)A.ld_w + 16 * fc;
+    uint32_t vx[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const long long t = 16 * b + fr, most = A.rows - 1 - t0;
+        vx[b] = (uint32_t)(t < most ? t : most) * (uint32_t)A.ld_x + 16 * fc;
+    }
+    const int steps = A.k / 64, from = (int)((long long)steps * wave / FEW_WAVES), to = (int)((long long)steps * (wave + 1) / FEW_WAVES);
+    v4i acc[H][NB] = {};
+    Words a[2][U][H], b[2][U][NB];
+    int shift_w[2], shift_x[NB];   // of a lane's rows (their 16-byte pieces are 16 apart: the same for all)
+    shift_w[0] = (int)(((uintptr_t)pw[0] + vw) & 3);
+    shift_w[1] = (int)(((uintptr_t)pw[1] + vw) & 3);
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+        shift_x[i] = (int)(((uintptr_t)px + vx[i]) & 3);
+    auto mfma = [&](const v4i (&fa)[H], const v4i (&fb)[NB]) {
+#pragma unroll
+        for (int i = 0; i < H; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[i], fb[j], acc[i][j], 0, 0, 0);
+    };
+    auto step = [&](const Words (&wa)[H], const Words (&wb)[NB]) {
+        v4i fa[H], fb[NB];
+#pragma unroll
+        for (int i = 0; i < H; ++i)
+            fa[i] = shifted<BYTES>(wa[i], shift_w[i]);
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+            fb[i] = shifted<BYTES>(wb[i], shift_x[i]);
+        mfma(fa, fb);
+    };
+    // two sets of U steps in turn: one in flight, one in the MFMAs; loads past the range read its last step
+    // again and are not used
+    if (int s = from; s < to) {
+        auto fill = [&](int set, int s) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int c = 64 * (s + u < to ? s + u : to - 1);
+#pragma unroll
+                for (int i = 0; i < H; ++i)
+                    a[set][u][i] = load_words<BYTES>(pw[i] + c, vw);
+#pragma unroll
+                for (int i = 0; i < NB; ++i)
+                    b[set][u][i] = load_words<BYTES>(px + c, vx[i]);
+            }
+        };
+        auto use = [&](int set, int s) {
+            if (s + U <= to) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    step(a[set][u], b[set][u]);
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (s + u < to)
+                        step(a[set][u], b[set][u]);
+            }
+        };
+        fill(0, s);
+        for (;;) {
+            fill(1, s + U);
+            use(0, s);
+            s += U;
+            if (s >= to)
+                break;
+            fill(0, s + U);
+            use(1, s);
+            s += U;
+            if (s >= to)
+                break;
+        }
+    }
+    if (64 * steps < A.k && wave == FEW_WAVES - 1) {   // the last k
+        const int k = 64 * steps + 16 * fc;
+        v4i fa[H], fb[NB];
+#pragma unroll
+        for (int i = 0; i < H; ++i)
+            fa[i] = load16<false>(pw[i] + vw - 16 * fc, k, A.k);
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+            fb[i] = load16<true>(px + vx[i] - 16 * fc, k, A.k);
+        mfma(fa, fb);
+    }
+#pragma unroll
+    for (int i = 0; i < H; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+            sums[wave][i * NB + j][lane] = acc[i][j];
+    __syncthreads();
+    for (int j = wave; j < NB; j += FEW_WAVES) {
+        const long long t = t0 + 16 * j + fr;
+        v4i c[H] = {};
+#pragma unroll
+        for (int w = 0; w < FEW_WAVES; ++w)
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+                c[h] += sums[w][h * NB + j][lane];
+        if (t < A.rows)
+            emit4<T, GATE>(A, t, j0 + 4 * fc, c[0], c[H - 1], A.x_scales[t]);
+    }
+}
+
+// ---- tiles through LDS -------------------------------------------------------------------
+// A workgroup computes TN rows of w by TM tokens; the next 128 k of both operands (one stage) go
+// into LDS ahead of the MFMAs, a ring of RING stages. Wave (i, j) of WN x WM holds TN / WN rows by
+// TM / WM tokens in accumulators of 32 x 32; a stage is four steps of 32 k.
+//
+// COPY: rows start at multiples of 16 bytes and are copied straight into LDS, 16 bytes a lane.
+// Otherwise they start anywhere and pass through registers, loaded one stage before they
+// are written (RING 2).
+//
+// While the MFMAs of one step run, the fragments of the next are read; in the last step, after the
+// first few MFMAs, the workgroup meets: by then each wave has read all of its stage (so its place
+// may be refilled) and its own part of the next one is in LDS. With one or two MFMAs a step that is
+// too short a time, and a whole stage's fragments are read ahead (DEEP).
+//
+// The 16-byte columns of LDS row r (128 bytes) sit XORed with swz(r), which is done by permuting the
+// lanes' source columns; fragment reads hit every bank once (no conflict in the counters).
+typedef int v16i __attribute__((ext_vector_type(16)));
+typedef uint32_t v4u32 __attribute__((ext_vector_type(4)));
+
+// 16 bytes per lane from rsrc's base + voff + soff to LDS address la + 16 * lane. Not
+// tracked by the compiler: every wait for it is an explicit wait_vmcnt.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void copy16(v4u32 rsrc, uint32_t voff, uint32_t soff, uint32_t la)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 ::"s"(la), "v"(voff), "s"(rsrc), "s"(soff) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+__device__ __forceinline__ v4u32 raw_rsrc(const void *p)
+{
+    const uint64_t a = (uint64_t)(uintptr_t)p;
+    return v4u32{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xFFFFu)), 0xFFFFFFFFu, 0x00020000u};
+}
+
+// position of tile `id` of `total`: workgroups go round the 8 XCDs, so each XCD takes a
+// contiguous range, in strips of up to 4 token tiles along the rows of w: the tiles that
+// run at once on an XCD share their operands in its L2
+struct Place {
+    int tn, tt, part;
+};
+__device__ __forceinline__ Place place(unsigned id, unsigned total, int tiles_n, int tiles_t)
+{
+    const unsigned x = id & 7, i = id >> 3, q = total >> 3, r = total & 7;
+    unsigned t = x * q + (x < r ? x : r) + i;
+    const unsigned per = (unsigned)tiles_n * (unsigned)tiles_t;
+    Place p;
+    p.part = (int)(t / per);
+    t -= p.part * per;
+    const unsigned strip = t / (4u * tiles_n), first = 4 * strip, high = tiles_t - first < 4 ? tiles_t - first : 4;
+    t -= strip * 4u * tiles_n;
+    p.tn = (int)(t / high);
+    p.tt = (int)(first + t % high);
+    return p;
+}
+
+// The sums of a wave to y (or the partial sums): 32 tokens at a time through the wave's own
+// 32 x (32 NA) int32 of LDS, so that stores are whole lines of consecutive outputs, and a
+// lane keeps the scales of its channels. A lane holds token lane % 32, rows 8 g + 4 (lane / 32)
+// .. + 3 of each 32 x 32; the 16-byte columns of a staged token are XORed with the token. With the gate
+// the value rows follow the gate rows.
+template <typename T, bool GATE, bool PART, int NA, int NB>
+__device__ __forceinline__ void store_tile(const QlinArgs &A, const v16i (&acc)[NA][NB], int8_t *stage, int part, long long t0, int j0)
+{
+    constexpr int WIDE = 32 * NA, SLOTS = WIDE / 4, OUT = GATE && !PART ? WIDE / 2 : WIDE;
+    constexpr int V = PART ? 4 : 16 / (int)sizeof(T), LANES = OUT / V;   // outputs per lane, lanes per token
+    const int lane = threadIdx.x & 63, o = lane % LANES * V;
+    typedef T vecT __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+    const int j = j0 + o, left = A.n - j;
+    float ws[V] = {}, wb[V] = {}, vs[V] = {}, vb[V] = {};
+    if constexpr (!PART) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const int c = j + e < A.n ? j + e : A.n - 1;
+            ws[e] = A.w_scales[c];
+            if (A.bias)
+                wb[e] = A.bias[c];
+            if constexpr (GATE) {
+                vs[e] = A.w_scales[A.n + c];
+                if (A.bias)
+                    vb[e] = A.bias[A.n + c];
+            }
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int tw = lane & 31;
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int row = GATE ? 32 * (i / 2) + (i & 1) * (WIDE / 2) : 32 * i;
+                const int slot = (row / 4 + 2 * g + (lane >> 5)) ^ (tw & (SLOTS - 1));
+                *(v4i *)(stage + (tw * SLOTS + slot) * 16) = v4i{acc[i][b][4 * g], acc[i][b][4 * g + 1], acc[i][b][4 * g + 2], acc[i][b][4 * g + 3]};
+            }
+#pragma unroll
+        for (int it = 0; it < 32 * LANES / 64; ++it) {
+            const int tr = it * (64 / LANES) + lane / LANES;
+            const long long t = t0 + 32 * b + tr;
+            auto sums = [&](int row, int e) {
+                return *(const v4i *)(stage + (tr * SLOTS + (((row + e) / 4) ^ (tr & (SLOTS - 1)))) * 16);
+            };
+            if constexpr (PART) {
+                if (t < A.rows) {
+                    // with the gate the staged rows are both halves: j0 counts outputs, o staged rows
+                    if constexpr (GATE)
+                        put4<true>(A, part, t, j0 + o % (WIDE / 2), o / (WIDE / 2), sums(o, 0));
+                    else
+                        put4<false>(A, part, t, j, 0, sums(o, 0));
+                }
+            } else if (t < A.rows) {
+                const float sx = A.x_scales[t];
+                vecT y;
+#pragma unroll
+                for (int e = 0; e < V; e += 4) {
+                    const v4i c = sums(o, e);
+                    v4i d = {};
+                    if constexpr (GATE)
+                        d = sums(WIDE / 2 + o, e);
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) {
+                        float z = (float)c[f] * sx * ws[e + f];
+                        if (A.bias)
+                            z += wb[e + f];
+                        if constexpr (GATE) {
+                            float v = (float)d[f] * sx * vs[e + f];
+                            if (A.bias)
+                                v += vb[e + f];
+                            z = silu(z) * v;
+                        }
+                        y[e + f] = (T)z;
+                    }
+                }
+                T *out = (T *)A.y + t * A.ld_y + j;
+                if (left >= V) {
+                    *(vecT *)out = y;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        if (e < left)
+                            out[e] = y[e];
+                }
+            }
+        }
+    }
+}
+
+template <typename T, bool GATE, bool PART, bool COPY, int TN, int TM, int WN, int WM, int RING>
+__global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, unsigned tile0, unsigned total)
+{
+    constexpr int WAVES = WN * WM, NA = TN / WN / 32, NB = TM / WM / 32, OUT = GATE ? TN / 2 : TN;
+    constexpr int STAGE = (TN + TM) * KS, STEPS = KS / 32;
+    // a copy is 8 rows of 128 bytes: COPIES per wave and stage, the first WCOPIES of rows of w
+    constexpr int WCOPIES = TN / 8 / WAVES, COPIES = (TN + TM) / 8 / WAVES;
+    constexpr int M = NA * NB, R = NA + NB;   // MFMAs and fragments of a step
+    constexpr bool DEEP = M <= 2;
+    static_assert(WCOPIES * 8 * WAVES == TN && COPIES * 8 * WAVES == TN + TM, "whole copies per wave");
+    static_assert(!GATE || NA % 2 == 0, "a wave holds gate and value");
+    static_assert(RING * STAGE >= WAVES * 32 * 32 * NA * 4 && RING * STAGE <= 160 << 10, "the outputs are staged in the ring");
+    static_assert((RING - 1) * COPIES < 64, "waits count to 63");
+    static_assert(COPY || (RING == 2 && !DEEP), "through registers: two places, stages of many MFMAs");
+    __shared__ __attribute__((aligned(16))) int8_t ring[RING * STAGE];
+    const int tiles_n = (A.n + OUT - 1) / OUT, tiles_t = (int)((A.rows + (long long)TM - 1) / TM);
+    const Place at = place(tile0 + blockIdx.x, total, tiles_n, tiles_t);
+    const int k0 = at.part * A.kchunk, k1 = A.k - k0 < A.kchunk ? A.k : k0 + A.kchunk;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t base = lds_addr(ring);
+
+    // Copy q of a wave moves LDS rows 8 (wave + WAVES q) .. + 7; the rows of w come first. With the
+    // gate, 32 gate rows and the 32 value rows of the same outputs take turns, so that a wave
+    // holds both halves of its outputs.
+    const int8_t *wbase = A.w + (long long)at.tn * OUT * A.ld_w, *xbase = A.x + (long long)at.tt * TM * A.ld_x;
+    const int8_t *vbase = wbase + (GATE ? A.n * A.ld_w : 0);
+    uint32_t voff[COPIES];
+#pragma unroll
+    for (int q = 0; q < COPIES; ++q) {
+        const int r = 8 * (wave + WAVES * q) + (lane >> 3), c = (lane & 7) ^ swz(r);
+        if (q < WCOPIES) {
+            const int j = GATE ? 32 * (r >> 6) + (r & 31) : r, left = A.n - 1 - at.tn * OUT;
+            voff[q] = (uint32_t)(j < left ? j : left) * (uint32_t)A.ld_w + 16 * c;
+        } else {
+            const int t = r - TN;
+            const long long left = A.rows - 1 - (long long)at.tt * TM;
+            voff[q] = (uint32_t)(t < left ? t : left) * (uint32_t)A.ld_x + 16 * c;
+        }
+    }
+    auto source = [&](int q) { return q >= WCOPIES ? xbase : GATE && (8 * (wave + WAVES * q) & 32) ? vbase : wbase; };
+    const v4u32 rw = raw_rsrc(wbase + k0), rv = raw_rsrc(vbase + k0), rx = raw_rsrc(xbase + k0);
+    // copy q of stage `stage` into place `place` of the ring
+    auto copy = [&](int q, int stage, int place) {
+        copy16(q >= WCOPIES ? rx : GATE && (8 * (wave + WAVES * q) & 32) ? rv : rw, voff[q], (uint32_t)KS * stage,
+               __builtin_amdgcn_readfirstlane(base + (uint32_t)place * STAGE + 1024u * (wave + WAVES * q)));
+    };
+    // The other way in: the next HOLD copies are on their way through registers. Half a stage of them where
+    // the accumulators leave no room for more (and a stage is long).
+    constexpr int HOLD = TN * TM >= 256 * 256 ? COPIES / 2 : COPIES;
+    Words held[COPY ? 1 : HOLD];
+    auto load = [&](int q, int stage) { held[q % HOLD] = load_words<true>(source(q) + k0 + KS * stage, voff[q]); };
+    auto store = [&](int q, int place) {
+        const int shift = (int)(((uintptr_t)source(q) + voff[q]) & 3);
+        *(v4i *)(ring + place * STAGE + 1024 * (wave + WAVES * q) + 16 * lane) = shifted<true>(held[q % HOLD], shift);
+    };
+
+    const int wn = wave / WM, wm = wave % WM, fr = lane & 31;
+    const int8_t *fa = ring + (wn * (TN / WN) + fr) * KS, *fb = ring + (TN + wm * (TM / WM) + fr) * KS;
+    int col[STEPS];   // where a lane finds its 16 bytes of each step in a row
+#pragma unroll
+    for (int p = 0; p < STEPS; ++p)
+        col[p] = ((2 * p + (lane >> 5)) ^ swz(fr)) * 16;
+    v16i acc[NA][NB] = {};
+    v4i a[DEEP ? 2 * STEPS : 2][NA], b[DEEP ? 2 * STEPS : 2][NB];
+    auto read = [&](int set, int i, int off) {
+        if (i < NA)
+            a[set][i] = *(const v4i *)(fa + off + i * 32 * KS);
+        else
+            b[set][i - NA] = *(const v4i *)(fb + off + (i - NA) * 32 * KS);
+    };
+    auto mfma = [&](int set, int m) {
+        const int i = m / NB, j = m % NB;
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[set][i], b[set][j], acc[i][j], 0, 0, 0);
+    };
+
+    // (copies and loads past the last stage take the last stage again, into a place that nothing reads, so
+    // that the counts of copies in flight hold)
+    const int stages = (k1 - k0) / KS, last = stages - 1;
+    if (DEEP && stages) {
+#pragma unroll
+        for (int s = 0; s < RING; ++s)
+#pragma unroll
+            for (int q = 0; q < COPIES; ++q)
+                copy(q, s < last ? s : last, s);
+        wait_vmcnt<(RING - 1) * COPIES>();
+        asm volatile("s_barrier" ::: "memory");
+        static_for<STEPS * R>([&](auto i) { read(i.value / R, i.value % R, col[i.value / R]); });
+        int place = 0;
+        auto stage = [&](auto P, int s) {
+            // every wave has read stage s, whose place may be refilled, and stage s + 1 has landed
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((RING - 2) * COPIES) : "memory");
+            const int next = place + 1 == RING ? 0 : place + 1;
+            static_for<STEPS * R>([&](auto i) {
+                read((1 - P.value) * STEPS + i.value / R, i.value % R, next * STAGE + col[i.value / R]);
+            });
+#pragma unroll
+            for (int q = 0; q < COPIES; ++q)
+                copy(q, s + RING < last ? s + RING : last, place);
+            static_for<STEPS * M>([&](auto m) { mfma(P.value * STEPS + m.value / M, m.value % M); });
+            place = next;
+        };
+        for (int s = 0; s < stages; s += 2) {
+            stage(std::integral_constant<int, 0>{}, s);
+            if (s + 1 == stages)
+                break;
+            stage(std::integral_constant<int, 1>{}, s + 1);
+        }
+    }
+    if (!DEEP && stages) {
+        if constexpr (COPY) {
+#pragma unroll
+            for (int s = 0; s < RING - 1; ++s)
+#pragma unroll
+                for (int q = 0; q < COPIES; ++q)
+                    copy(q, s < last ? s : last, s);
+            wait_vmcnt<(RING - 2) * COPIES>();
+            asm volatile("s_barrier" ::: "memory");
+        } else {
+#pragma unroll
+            for (int q = 0; q < HOLD; ++q)
+                load(q, 0);
+#pragma unroll
+            for (int q = 0; q < COPIES; ++q) {
+                store(q, 0);
+                if (q + HOLD < COPIES)
+                    load(q + HOLD, 0);
+                else
+                    load(q + HOLD - COPIES, 1 < last ? 1 : last);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            read(0, i, col[0]);
+        constexpr int MEET = M >= 16 ? 4 : M >= 8 ? 2 : 1;   // MFMAs of the last step before the workgroup meets
+        constexpr int SPREAD = M * (STEPS - 1);              // MFMAs that the copies are spread over
+        int off = 0;
+        for (int s = 0; s < stages; ++s) {
+            const int ahead = s + RING - 1 < last ? s + RING - 1 : last, into = (s + RING - 1) % RING;
+            const int after = s + 2 < last ? s + 2 : last;   // (through registers: ahead is the stage s + 1)
+            static_for<STEPS - 1>([&](auto p) {
+                static_for<M>([&](auto m) {
+                    static_for<R>([&](auto i) {
+                        if constexpr (i.value * (M < R ? M : R) / R == m.value)
+                            read((p.value + 1) & 1, i.value, off + col[p.value + 1]);
+                    });
+                    mfma(p.value & 1, m.value);
+                    static_for<COPIES>([&](auto q) {
+                        if constexpr (q.value * SPREAD / COPIES == p.value * M + m.value) {
+                            if constexpr (COPY) {
+                                copy(q.value, ahead, into);
+                            } else {
+                                store(q.value, into);
+                                if constexpr (q.value + HOLD < COPIES)
+                                    load(q.value + HOLD, ahead);
+                                else
+                                    load(q.value + HOLD - COPIES, after);
+                            }
+                        }
+                    });
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            });
+            const int next = s == last ? off : (s + 1) % RING * STAGE;
+            static_for<M>([&](auto m) {
+                if constexpr (m.value == MEET) {
+                    if constexpr (COPY)
+                        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((RING - 2) * COPIES) : "memory");
+                    else
+                        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                static_for<R>([&](auto i) {
+                    if constexpr (MEET + i.value * (M - MEET < R ? M - MEET : R) / R == m.value)
+                        read(0, i.value, next + col[0]);
+                });
+                mfma((STEPS - 1) & 1, m.value);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            off = next;
+        }
+    }
+    // the last k, where 128 does not divide them, through registers
+    wait_vmcnt<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (const int k = k0 + KS * stages; k < k1) {
+#pragma unroll
+        for (int q = 0; q < COPIES; ++q) {
+            const int c = (lane & 7) ^ swz(8 * (wave + WAVES * q) + (lane >> 3));
+            *(v4i *)(ring + 1024 * (wave + WAVES * q) + 16 * lane) =
+                q < WCOPIES ? load16<false>(source(q) + k0 + (voff[q] - 16 * c), k - k0 + 16 * c, k1 - k0)
+                            : load16<true>(source(q) + k0 + (voff[q] - 16 * c), k - k0 + 16 * c, k1 - k0);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int p = 0; p < STEPS; ++p) {
+            if (k + 32 * p >= k1)
+                break;
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                read(p & 1, i, col[p]);
+#pragma unroll
+            for (int m = 0; m < M; ++m)
+                mfma(p & 1, m);
+        }
+    }
+
+    __syncthreads();   // every wave is done with the ring, which now stages the outputs
+    const int j0 = at.tn * OUT + wn * (OUT / WN);
+    const long long t0 = (long long)at.tt * TM + wm * (TM / WM);
+    store_tile<T, GATE, PART, NA, NB>(A, acc, ring + wave * 32 * NA * 32 * 4, at.part, t0, j0);
+}
+
+// ---- launches ---------------------------------------------------------------------------
+constexpr unsigned MOST_GROUPS = 1u << 22;   // workgroups of one launch (a multiple of 8: XCDs keep their turns)
+
+template <typename T, bool GATE, bool PART>
+void launch_any(const QlinArgs &a, hipStream_t stream)
+{
+    constexpr int OUT = GATE ? ANY_TILE / 2 : ANY_TILE;
+    const long long total = (long long)((a.n + OUT - 1) / OUT) * ((a.rows + ANY_TILE - 1) / ANY_TILE) * a.ksplit;
+    for (long long at = 0; at < total; at += MOST_GROUPS) {
+        const dim3 grid((unsigned)(total - at < MOST_GROUPS ? total - at : MOST_GROUPS));
+        hipLaunchKernelGGL((qlin_any_kernel<T, GATE, PART>), grid, dim3(256), 0, stream, a, at);
+    }
+}
+
+template <typename T, bool GATE, bool BYTES, int NB, int U>
+void launch_few(const QlinArgs &a, hipStream_t stream)
+{
+    const dim3 grid((unsigned)((a.n + 15) / 16), (unsigned)((a.rows + 16 * NB - 1) / (16 * NB)));
+    hipLaunchKernelGGL((qlin_few_kernel<T, GATE, BYTES, NB, U>), grid, dim3(64 * FEW_WAVES), 0, stream, a);
+}
+
+template <typename T, bool GATE, bool PART, bool COPY, int TN, int TM, int WN, int WM, int RING>
+void launch_tile(const QlinArgs &a, hipStream_t stream)
+{
+    constexpr int OUT = GATE ? TN / 2 : TN;
+    const unsigned total = (unsigned)((a.n + OUT - 1) / OUT) * (unsigned)((a.rows + TM - 1) / TM) * (unsigned)a.ksplit;
+    for (unsigned at = 0; at < total; at += MOST_GROUPS) {
+        const dim3 grid(total - at < MOST_GROUPS ? total - at : MOST_GROUPS), block(64 * WN * WM);
+        hipLaunchKernelGGL((qlin_tile_kernel<T, GATE, PART, COPY, TN, TM, WN, WM, RING>), grid, block, 0, stream, a, at, total);
+    }
+}
+
+// rows of w (with the gate: of both halves) x tokens; a gated tile's waves hold pairs of row tiles
+template <typename T, bool GATE, bool PART>
+void launch_shape(const QlinArgs &a, int shape, hipStream_t stream)
+{
+    switch (shape) {
+    case QLIN_ANY: return launch_any<T, GATE, PART>(a, stream);
+    case QLIN_64x32:
+        if constexpr (GATE)
+            return launch_tile<T, GATE, PART, true, 128, 32, 2, 1, 4>(a, stream);
+        else
+            return launch_tile<T, GATE, PART, true, 64, 32, 2, 1, 4>(a, stream);
+    case QLIN_64x64:   // plain only: the gated 128x64 has the same tile
+        if constexpr (!GATE)
+            return launch_tile<T, GATE, PART, true, 64, 64, 2, 2, 4>(a, stream);
+        break;
+    case QLIN_128x64:
+        if constexpr (GATE)
+            return launch_tile<T, GATE, PART, true, 128, 64, 2, 2, 3>(a, stream);
+        else
+            return launch_tile<T, GATE, PART, true, 128, 64, 4, 2, 3>(a, stream);
+    case QLIN_128x128:
+        if constexpr (GATE)
+            return launch_tile<T, GATE, PART, true, 128, 128, 2, 4, 3>(a, stream);
+        else
+            return launch_tile<T, GATE, PART, true, 128, 128, 4, 2, 3>(a, stream);
+    case QLIN_256x128: return launch_tile<T, GATE, PART, true, 256, 128, 4, 2, 3>(a, stream);
+    case QLIN_256x256: return launch_tile<T, GATE, PART, true, 256, 256, 2, 4, 2>(a, stream);
+    case QLIN_128x128_ANY: return launch_tile<T, GATE, PART, false, 128, 128, 2, 2, 2>(a, stream);
+    case QLIN_256x256_ANY: return launch_tile<T, GATE, PART, false, 256, 256, 2, 4, 2>(a, stream);
+    default: break;
+    }
+    if constexpr (!PART) {
+        const bool bytes = (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.ld_x | (uintptr_t)a.ld_w) & 3) != 0;
+        if (shape == QLIN_FEW16)
+            return bytes ? launch_few<T, GATE, true, 1, 4>(a, stream) : launch_few<T, GATE, false, 1, 4>(a, stream);
+        if (shape == QLIN_FEW64)
+            return bytes ? launch_few<T, GATE, true, 4, 2>(a, stream) : launch_few<T, GATE, false, 4, 2>(a, stream);
+    }
+}
+
+template <typename T>
+hipError_t launch_typed(const QlinArgs &a, int shape, hipStream_t stream)
+{
+    if (a.gate)
+        launch_shape<T, true, false>(a, shape, stream);
+    else
+        launch_shape<T, false, false>(a, shape, stream);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace aqd
