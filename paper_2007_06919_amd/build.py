@@ -18,7 +18,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libaqd.so")
 SOURCES = ["aqd_api.hip", "qconv_mfma.hip", "qconv_wv.hip", "qconv_wvs.hip", "qconv_b8.hip", "qconv_gf.hip", "qconv_fx.hip", "qconv_stem.hip", "qconv_splitk.hip", "qconv_direct.hip",
            "qadd.hip", "qpool.hip", "qrows.hip", "qlin.hip", "qlin_f32.hip", "qlin_f16.hip", "qlin_bf16.hip",
-           "qlin_part.hip", "mfma_probe.hip"]
+           "mfma_probe.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -238,7 +238,5 @@ hipError_t launch_qlin(const QlinArgs &a, const QlinPlan &plan, hipStream_t stre
 hipError_t launch_qlin_f32(const QlinArgs &a, int shape, hipStream_t stream);
 hipError_t launch_qlin_f16(const QlinArgs &a, int shape, hipStream_t stream);
 hipError_t launch_qlin_bf16(const QlinArgs &a, int shape, hipStream_t stream);
-hipError_t launch_qlin_part(const QlinArgs &a, int shape, hipStream_t stream);      // partial sums only
-hipError_t launch_qlin_combine(const QlinArgs &a, hipStream_t stream);
 
 }  // namespace aqd

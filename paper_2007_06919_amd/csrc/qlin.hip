@@ -1,9 +1,9 @@
-// Linear layers on 8-bit codes: which kernel a launch takes, and whether its k range is split
-// (host code; the kernels: qlin_kernels.h).
+// Linear layers on 8-bit codes: which kernel a launch takes, whether its k range is split, and
+// the launches of a split one: partial sums, then the sum of those.
 
 #include <algorithm>
 
-#include "internal.h"
+#include "qlin_kernels.h"
 
 namespace aqd {
 namespace {
@@ -115,6 +115,41 @@ QlinPlan qlin_plan(const QlinArgs &a, size_t room)
     return best;
 }
 
+namespace {
+
+hipError_t launch_part(const QlinArgs &a, int shape, hipStream_t stream)
+{
+    if (a.gate)
+        launch_shape<float, true, true>(a, shape, stream);
+    else
+        launch_shape<float, false, true>(a, shape, stream);
+    return hipGetLastError();
+}
+
+template <typename T>
+void combine(const QlinArgs &a, hipStream_t stream)
+{
+    const long long items = (long long)a.rows * (a.n_pad / 4);   // few: their sums fit the workspace
+    const dim3 grid((unsigned)((items + 255) / 256));
+    if (a.gate)
+        hipLaunchKernelGGL((qlin_combine_kernel<T, true>), grid, dim3(256), 0, stream, a);
+    else
+        hipLaunchKernelGGL((qlin_combine_kernel<T, false>), grid, dim3(256), 0, stream, a);
+}
+
+hipError_t launch_combine(const QlinArgs &a, hipStream_t stream)
+{
+    if (a.type == AQD_F32)
+        combine<float>(a, stream);
+    else if (a.type == AQD_F16)
+        combine<_Float16>(a, stream);
+    else
+        combine<__bf16>(a, stream);
+    return hipGetLastError();
+}
+
+}  // namespace
+
 hipError_t launch_qlin(const QlinArgs &args, const QlinPlan &plan, hipStream_t stream)
 {
     QlinArgs a = args;
@@ -124,8 +159,8 @@ hipError_t launch_qlin(const QlinArgs &args, const QlinPlan &plan, hipStream_t s
     a.kchunk = 128 * ((stages + plan.parts - 1) / plan.parts);
     a.ksplit = (a.k + a.kchunk - 1) / a.kchunk;
     if (a.ksplit > 1) {
-        const hipError_t e = launch_qlin_part(a, plan.shape, stream);
-        return e != hipSuccess ? e : launch_qlin_combine(a, stream);
+        const hipError_t e = launch_part(a, plan.shape, stream);
+        return e != hipSuccess ? e : launch_combine(a, stream);
     }
     a.kchunk = a.k;
     return a.type == AQD_F32   ? launch_qlin_f32(a, plan.shape, stream)
