@@ -302,6 +302,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) qlin_few_kernel(QlinArgs A)
         vx[b] = (uint32_t)(t < most ? t : most) * (uint32_t)A.ld_x + 16 * fc;
     }
     const int steps = A.k / 64, from = (int)((long long)steps * wave / FEW_WAVES), to = (int)((long long)steps * (wave + 1) / FEW_WAVES);
+    const int start = gridDim.y == 1 && to > from ? (int)(blockIdx.x % (unsigned)(to - from)) : 0;   // as in qlin_tile_kernel
     v4i acc[H][NB] = {};
     Words a[2][U][H], b[2][U][NB];
     int shift_w[2], shift_x[NB];   // of a lane's rows (their 16-byte pieces are 16 apart: the same for all)
@@ -333,7 +334,8 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) qlin_few_kernel(QlinArgs A)
         auto fill = [&](int set, int s) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int c = 64 * (s + u < to ? s + u : to - 1);
+                const int at = s + u < to ? s + u : to - 1, turn = at + start < to ? at + start : at + start - (to - from);
+                const int c = 64 * turn;
 #pragma unroll
                 for (int i = 0; i < H; ++i)
                     a[set][u][i] = load_words<BYTES>(pw[i] + c, vw);
@@ -625,12 +627,17 @@ __global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, uns
     // (copies and loads past the last stage take the last stage again, into a place that nothing reads, so
     // that the counts of copies in flight hold)
     const int stages = (k1 - k0) / KS, last = stages - 1;
+    // Where this workgroup starts: a sum's terms have no order. With rows of a power of two of bytes, workgroups that
+    // all read the same columns meet on a few memory channels; where each row of w is read by one of them
+    // (one token tile) they start apart: 16 x 16384 x 4096 gated 33.3 -> 28.9 us.
+    const int start = stages && tiles_t == 1 ? at.tn % stages : 0;
+    auto turned = [&](int s) { return s + start < stages ? s + start : s + start - stages; };
     if (DEEP && stages) {
 #pragma unroll
         for (int s = 0; s < RING; ++s)
 #pragma unroll
             for (int q = 0; q < COPIES; ++q)
-                copy(q, s < last ? s : last, s);
+                copy(q, turned(s < last ? s : last), s);
         wait_vmcnt<(RING - 1) * COPIES>();
         asm volatile("s_barrier" ::: "memory");
         static_for<STEPS * R>([&](auto i) { read(i.value / R, i.value % R, col[i.value / R]); });
@@ -638,13 +645,13 @@ __global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, uns
         auto stage = [&](auto P, int s) {
             // every wave has read stage s, whose place may be refilled, and stage s + 1 has landed
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((RING - 2) * COPIES) : "memory");
-            const int next = place + 1 == RING ? 0 : place + 1;
+            const int next = place + 1 == RING ? 0 : place + 1, ahead = turned(s + RING < last ? s + RING : last);
             static_for<STEPS * R>([&](auto i) {
                 read((1 - P.value) * STEPS + i.value / R, i.value % R, next * STAGE + col[i.value / R]);
             });
 #pragma unroll
             for (int q = 0; q < COPIES; ++q)
-                copy(q, s + RING < last ? s + RING : last, place);
+                copy(q, ahead, place);
             static_for<STEPS * M>([&](auto m) { mfma(P.value * STEPS + m.value / M, m.value % M); });
             place = next;
         };
@@ -661,20 +668,20 @@ __global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, uns
             for (int s = 0; s < RING - 1; ++s)
 #pragma unroll
                 for (int q = 0; q < COPIES; ++q)
-                    copy(q, s < last ? s : last, s);
+                    copy(q, turned(s < last ? s : last), s);
             wait_vmcnt<(RING - 2) * COPIES>();
             asm volatile("s_barrier" ::: "memory");
         } else {
 #pragma unroll
             for (int q = 0; q < HOLD; ++q)
-                load(q, 0);
+                load(q, turned(0));
 #pragma unroll
             for (int q = 0; q < COPIES; ++q) {
                 store(q, 0);
                 if (q + HOLD < COPIES)
-                    load(q + HOLD, 0);
+                    load(q + HOLD, turned(0));
                 else
-                    load(q + HOLD - COPIES, 1 < last ? 1 : last);
+                    load(q + HOLD - COPIES, turned(1 < last ? 1 : last));
             }
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         }
@@ -685,8 +692,8 @@ __global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, uns
         constexpr int SPREAD = M * (STEPS - 1);              // MFMAs that the copies are spread over
         int off = 0;
         for (int s = 0; s < stages; ++s) {
-            const int ahead = s + RING - 1 < last ? s + RING - 1 : last, into = (s + RING - 1) % RING;
-            const int after = s + 2 < last ? s + 2 : last;   // (through registers: ahead is the stage s + 1)
+            const int ahead = turned(s + RING - 1 < last ? s + RING - 1 : last), into = (s + RING - 1) % RING;
+            const int after = turned(s + 2 < last ? s + 2 : last);   // (through registers: ahead is the stage s + 1)
             static_for<STEPS - 1>([&](auto p) {
                 static_for<M>([&](auto m) {
                     static_for<R>([&](auto i) {
