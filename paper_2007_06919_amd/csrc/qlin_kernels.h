@@ -92,10 +92,23 @@ __global__ void __launch_bounds__(256) qlin_combine_kernel(QlinArgs A)
     const long long line = (long long)A.n_pad * (GATE ? 2 : 1), step = A.rows * line;
     const int32_t *p = A.part + t * line + j;
     v4i acc = {0, 0, 0, 0}, value = {0, 0, 0, 0};
-    for (int s = 0; s < A.ksplit; ++s) {
-        acc += *(const v4i *)(p + s * step);
-        if constexpr (GATE)
-            value += *(const v4i *)(p + s * step + A.n_pad);
+    // four parts' loads in flight at once; past the last part it is read again and not added
+    for (int s = 0; s < A.ksplit; s += 4) {
+        v4i v[4], w[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int32_t *q = p + (s + u < A.ksplit ? s + u : A.ksplit - 1) * step;
+            v[u] = *(const v4i *)q;
+            if constexpr (GATE)
+                w[u] = *(const v4i *)(q + A.n_pad);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (s + u < A.ksplit) {
+                acc += v[u];
+                if constexpr (GATE)
+                    value += w[u];
+            }
     }
     emit4<T, GATE>(A, t, j, acc, value, A.x_scales[t]);
 }
