@@ -228,7 +228,7 @@ struct QlinArgs {
 // kernel and tile (outputs x tokens) of a launch: _ANY take rows at any address, FEW16 and FEW64 go by
 // 16 outputs and 16 or 64 tokens (qlin_kernels.h)
 enum { QLIN_ANY = 0, QLIN_64x32, QLIN_64x64, QLIN_128x64, QLIN_128x128, QLIN_256x128, QLIN_256x256,
-       QLIN_128x128_ANY, QLIN_256x256_ANY, QLIN_FEW16, QLIN_FEW64 };
+       QLIN_128x128_ANY, QLIN_256x256_ANY, QLIN_FEW16, QLIN_FEW64, QLIN_128x128_TWO };
 struct QlinPlan {
     int shape, parts;   // parts of the k range (1: whole)
     size_t bytes;       // what their sums take

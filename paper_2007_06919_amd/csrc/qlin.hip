@@ -11,10 +11,11 @@ namespace {
 // A tile shape (outputs x tokens; with the gate twice as many rows of w), how many of its workgroups
 // fit a CU, and its time in us per stage of 128 k while few CUs run and while all do, and per round
 // of workgroups apart from the stages (first loads, stores), with the gate that many times as much.
-// Fitted to launches of 640 random sizes (1 to 11000 tokens, 128 to 16384 outputs and k, plain and
-// gated, every shape with 1 to 8 parts): the plan's launch is 1.6% (aligned rows) and 1.2% slower than
-// the fastest of them on average, 6% and 4% at the ninetieth percentile. One shape for all: 2 to 10 times as
-// slow at the other end of the sizes.
+// Fitted to launches of 1140 random sizes (1 to 11000 tokens, 128 to 16384 outputs and k, plain and
+// gated, every shape with 1 to 8 parts): the plan's launch is 2% (aligned rows) and 1.2% slower than
+// the fastest of them on average, 7% and 4% at the ninetieth percentile. Without one of the shapes the
+// fastest is 0.3% (128x128_TWO; 32% at worst, many tiles and a short k) to 1.8% slower on average; one shape
+// for all, 2 to 10 times at the other end of the sizes.
 struct Shape {
     int shape, out, gate_out, tokens, per_cu;
     double idle, busy, round, gate;
@@ -22,7 +23,8 @@ struct Shape {
 const Shape copied[] = {
     {QLIN_64x32, 64, 64, 32, 3, 0.130, 0.170, 1.56, 2.19},    {QLIN_64x64, 64, 0, 64, 2, 0.135, 0.205, 1.68, 0.0},
     {QLIN_128x64, 128, 64, 64, 2, 0.214, 0.355, 1.86, 1.40},  {QLIN_128x128, 128, 64, 128, 1, 0.272, 0.526, 2.57, 1.24},
-    {QLIN_256x128, 256, 128, 128, 1, 0.363, 0.889, 4.13, 1.07}, {QLIN_256x256, 256, 128, 256, 1, 0.834, 1.616, 8.02, 1.01},
+    {QLIN_128x128_TWO, 128, 64, 128, 2, 0.380, 0.540, 3.40, 1.35}, {QLIN_256x128, 256, 128, 128, 1, 0.363, 0.889, 4.13, 1.07},
+    {QLIN_256x256, 256, 128, 256, 1, 0.834, 1.616, 8.02, 1.01},
 };
 const Shape anywhere[] = {
     {QLIN_ANY, 64, 32, 64, 4, 0.812, 0.532, 2.24, 0.98},
@@ -64,7 +66,7 @@ bool aligned_rows(const QlinArgs &a) { return (((uintptr_t)a.x | (uintptr_t)a.w 
 double time_of_few(const QlinArgs &a, int tokens, double fixed, double step, double gate, double rate)
 {
     const double groups = up(a.n, 16) * up(a.rows, tokens), steps = up(a.k, 256) * (a.gate ? gate : 1.0);
-    return LAUNCH + std::max((fixed + step * steps) * std::max(1.0, groups / CUS), (double)a.wide * a.k / rate);
+    return LAUNCH + std::max((fixed + step * steps) * up(groups, CUS), (double)a.wide * a.k / rate);
 }
 
 }  // namespace
@@ -107,7 +109,7 @@ QlinPlan qlin_plan(const QlinArgs &a, size_t room)
     };
     if (aligned) {
         if (a.rows <= 16)
-            consider_few(QLIN_FEW16, 16, time_of_few(a, 16, 1.2, 0.09, 2.5, 4.1e6));
+            consider_few(QLIN_FEW16, 16, time_of_few(a, 16, 2.0, 0.09, 2.0, 4.1e6));
     } else {
         consider_few(QLIN_FEW16, 16, time_of_few(a, 16, 1.6, 0.26, 1.96, 2.6e6));
         consider_few(QLIN_FEW64, 64, time_of_few(a, 64, 1.8, 0.41, 1.82, 3.5e6));

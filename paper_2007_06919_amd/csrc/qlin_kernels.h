@@ -837,6 +837,11 @@ void launch_shape(const QlinArgs &a, int shape, hipStream_t stream)
             return launch_tile<T, GATE, PART, true, 128, 128, 2, 4, 3>(a, stream);
         else
             return launch_tile<T, GATE, PART, true, 128, 128, 4, 2, 3>(a, stream);
+    case QLIN_128x128_TWO:   // two stages of LDS: two workgroups to a CU
+        if constexpr (GATE)
+            return launch_tile<T, GATE, PART, true, 128, 128, 2, 4, 2>(a, stream);
+        else
+            return launch_tile<T, GATE, PART, true, 128, 128, 4, 2, 2>(a, stream);
     case QLIN_256x128: return launch_tile<T, GATE, PART, true, 256, 128, 4, 2, 3>(a, stream);
     case QLIN_256x256: return launch_tile<T, GATE, PART, true, 256, 256, 2, 4, 2>(a, stream);
     case QLIN_128x128_ANY: return launch_tile<T, GATE, PART, false, 128, 128, 2, 2, 2>(a, stream);

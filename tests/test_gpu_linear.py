@@ -389,3 +389,38 @@ def test_on_another_stream_and_in_a_graph():
                 assert torch.equal(mine[b], eager[b]), b
     finally:
         aqd.graph_destroy(graph)
+
+
+# sizes at which each of the kernels is the fastest, or nearly (rows at any address: k odd)
+LARGE = [(2100, 2200, 640), (4000, 1300, 1100), (2500, 4100, 2048), (1300, 1500, 1000), (520, 2100, 512), (9000, 330, 200),
+         (300, 1000, 6000), (140, 520, 16000), (1700, 900, 333), (2300, 2100, 1001), (90, 4000, 2001), (700, 300, 7777)]
+
+
+@pytest.mark.parametrize("act", [aqd.QLIN_PLAIN, aqd.QLIN_SILU_GATE])
+@pytest.mark.parametrize("rows, n, k", LARGE)
+def test_large_products(rows, n, k, act):
+    """Against 64-bit sums on the GPU (exact: integers below 2^53); every element of y, and the workspace's split against none."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(rows + n + k)
+    wide = 2 * n if act else n
+    x = torch.randint(-128, 128, (rows, k), generator=g, device="cuda", dtype=torch.int8)
+    w = torch.randint(-128, 128, (wide, k), generator=g, device="cuda", dtype=torch.int8)
+    sx = (torch.rand(rows, generator=g, device="cuda") + 0.5) / 74
+    sw = (torch.rand(wide, generator=g, device="cuda") + 0.5) / (74 * math.sqrt(k))
+    b = torch.randn(wide, generator=g, device="cuda")
+    work = torch.empty(aqd.QLIN_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+    y = [torch.zeros(rows, n, device="cuda") for _ in range(2)]
+    for i, ws in enumerate((work, None)):
+        aqd.qlin_run(rows, n, k, aqd.F32, act, x, 0, sx, w, 0, sw, b, y[i], 0, ws, work.numel() if ws is not None else 0)
+    p = torch.mm(x.double(), w.double().t().contiguous()) * sx.double()[:, None] * sw.double()
+    z = p + b.double()
+    ez = (4 * p.abs() + z.abs()) * 2.0 ** -24
+    want, tol = z, ez
+    if act:
+        gate, v = z[:, :n], z[:, n:]
+        silu = gate / (1 + torch.exp(-gate))
+        want = silu * v
+        tol = v.abs() * (1.1 * ez[:, :n] + silu.abs() * (gate.abs() + 4) * 2.0 ** -22) + silu.abs() * ez[:, n:] + want.abs() * 2.0 ** -23
+    tol = tol * 1.01 + want.abs() * 2.0 ** -24 + 2.0 ** -150
+    assert torch.equal(y[0], y[1])
+    assert bool(((y[0].double() - want).abs() <= tol).all())
