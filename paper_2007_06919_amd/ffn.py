@@ -1,0 +1,148 @@
+"""A gated feed-forward block on 8-bit weights, the four launches that serve it:
+
+    sum, codes, scales = qnorm(x + residual)              residual's addition, norm, 8-bit codes
+    h                  = qlin(codes, gate and up rows)    silu(gate) * up in the product's epilogue
+    codes, scales      = qrows(h)                         8-bit codes of the hidden units
+    y                  = qlin(codes, down rows)
+
+Weights are quantised once, one scale per output channel, by the same row quantisation
+that makes the activations' codes. All buffers are allocated at set-up for the most
+rows of a call, so a pass allocates nothing and can be captured in a HIP graph
+(``capture``, ``replay``). PyTorch provides device memory and the stream; all
+arithmetic is in ``libaqd.so``.
+
+    python -m paper_2007_06919_amd.ffn [hidden] [units]
+
+times a block of random weights at 1 to 4096 rows, eager and replayed, and prints how
+far its outputs are from the same block in fp32 on the unquantised weights.
+"""
+from __future__ import annotations
+
+import sys
+
+from . import aqd
+
+
+def quantize_rows(w, stream=None):
+    """(codes, scales) of a real matrix, one scale per row; rows of codes start at multiples of 16 bytes."""
+    import torch
+    rows, cols = w.shape
+    codes = torch.zeros(rows, -(-cols // 16) * 16, dtype=torch.int8, device=w.device)[:, :cols]
+    scales = torch.empty(rows, dtype=torch.float32, device=w.device)
+    aqd.qrows_run(rows, cols, aqd.real_type(w), w, w.stride(0), codes, codes.stride(0), scales, stream)
+    return codes, scales
+
+
+class GatedFfn:
+    """norm_weight [hidden], gate and up [units][hidden], down [hidden][units]: device tensors of one real type."""
+
+    def __init__(self, norm_weight, gate, up, down, eps=1e-5, max_rows=4096):
+        import torch
+        units, hidden = gate.shape
+        if up.shape != gate.shape or down.shape != (hidden, units) or norm_weight.shape != (hidden,):
+            raise ValueError(f"shapes do not make a block: norm {tuple(norm_weight.shape)}, gate {tuple(gate.shape)}, "
+                             f"up {tuple(up.shape)}, down {tuple(down.shape)}")
+        if max_rows < 1:
+            raise ValueError("max_rows must be at least 1")
+        self.hidden, self.units, self.eps, self.max_rows = hidden, units, float(eps), max_rows
+        self.dtype, self.type = gate.dtype, aqd.real_type(gate)
+        self.norm_weight = norm_weight.contiguous()
+        self.w1, self.s1 = quantize_rows(torch.cat([gate, up]))
+        self.w2, self.s2 = quantize_rows(down)
+        dev = gate.device
+
+        def codes(cols):
+            return torch.empty(max_rows, -(-cols // 16) * 16, dtype=torch.int8, device=dev)
+
+        self.c1, self.q1 = codes(hidden), torch.empty(max_rows, device=dev)
+        self.h = torch.empty(max_rows, units, dtype=self.dtype, device=dev)
+        self.c2, self.q2 = codes(units), torch.empty(max_rows, device=dev)
+        # the bound serves every call; the block's launches follow one another on one stream
+        self.workspace = torch.empty(aqd.QLIN_WORKSPACE_BYTES, dtype=torch.uint8, device=dev)
+        self._graph = None
+
+    def forward(self, x, residual, y, total, stream=None):
+        """y = block(norm(x + residual)), total = x + residual; all [rows][hidden] with contiguous rows. total may be
+        residual. On one stream at a time."""
+        rows = x.shape[0]
+        if rows > self.max_rows:
+            raise ValueError(f"{rows} rows, and buffers for {self.max_rows}")
+        for t in (x, residual, y, total):
+            if t.shape != (rows, self.hidden) or t.dtype != self.dtype or t.stride(1) != 1:
+                raise ValueError(f"tensors must be [{rows}][{self.hidden}] {self.dtype} with contiguous rows")
+        ws = self.workspace
+        aqd.qnorm_run(rows, self.hidden, self.type, self.eps, x, x.stride(0), residual, residual.stride(0), self.norm_weight,
+                      total, total.stride(0), self.c1, self.c1.stride(0), self.q1, stream)
+        aqd.qlin_run(rows, self.units, self.hidden, self.type, aqd.QLIN_SILU_GATE, self.c1, self.c1.stride(0), self.q1, self.w1,
+                     self.w1.stride(0), self.s1, None, self.h, self.units, ws, ws.numel(), stream)
+        aqd.qrows_run(rows, self.units, self.type, self.h, self.units, self.c2, self.c2.stride(0), self.q2, stream)
+        aqd.qlin_run(rows, self.hidden, self.units, self.type, aqd.QLIN_PLAIN, self.c2, self.c2.stride(0), self.q2, self.w2,
+                     self.w2.stride(0), self.s2, None, y, y.stride(0), ws, ws.numel(), stream)
+        return y
+
+    def capture(self, x, residual, y, total, stream):
+        """Record a pass on these tensors into a HIP graph (`stream`: not the null stream)."""
+        self.close()
+        aqd.graph_begin(stream)
+        try:
+            self.forward(x, residual, y, total, stream)
+        finally:
+            self._graph = aqd.graph_end(stream)
+
+    def replay(self, stream):
+        aqd.graph_launch(self._graph, stream)
+
+    def close(self):
+        if self._graph is not None:
+            aqd.graph_destroy(self._graph)
+            self._graph = None
+
+
+def reference(x, residual, norm_weight, gate, up, down, eps):
+    """The block in fp32 on the unquantised weights."""
+    import torch
+    s = x.float() + residual.float()
+    n = s * torch.rsqrt((s * s).mean(1, keepdim=True) + eps) * norm_weight.float()
+    g = n @ gate.float().t()
+    return (g * torch.sigmoid(g) * (n @ up.float().t())) @ down.float().t()
+
+
+def main(hidden=4096, units=11264):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(0)
+
+    def randn(*shape, scale=1.0):
+        return (torch.randn(*shape, generator=g, device="cuda") * scale).bfloat16()
+
+    w = (1 + 0.1 * randn(hidden), randn(units, hidden, scale=hidden ** -0.5), randn(units, hidden, scale=hidden ** -0.5),
+         randn(hidden, units, scale=units ** -0.5))
+    ffn = GatedFfn(*w)
+    stream = torch.cuda.Stream()
+    for rows in (1, 16, 128, 1024, 4096):
+        x, r = randn(rows, hidden), randn(rows, hidden)
+        y, total = torch.empty_like(x), torch.empty_like(x)
+        torch.cuda.synchronize()
+        ffn.forward(x, r, y, total, stream)
+        torch.cuda.synchronize()
+        want = reference(x, r, *w, ffn.eps)
+        off = float((y.float() - want).norm() / want.norm())
+        ffn.capture(x, r, y, total, stream)
+        line = f"{rows:5d} rows: {100 * off:.2f}% off fp32"
+        ops = 6 * rows * hidden * units
+        for name, run in (("eager", lambda: ffn.forward(x, r, y, total, stream)), ("replayed", lambda: ffn.replay(stream))):
+            for _ in range(10):
+                run()
+            begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            begin.record(stream)
+            for _ in range(50):
+                run()
+            end.record(stream)
+            torch.cuda.synchronize()
+            us = begin.elapsed_time(end) / 50 * 1e3
+            line += f", {name} {us:.1f} us ({ops / us / 1e6:.0f} TOPS)"
+        print(line, flush=True)
+    ffn.close()
+
+
+if __name__ == "__main__":
+    main(*(int(a) for a in sys.argv[1:3]))

@@ -1,0 +1,85 @@
+"""The gated feed-forward block (ffn.GatedFfn) against its own steps in 64 bits, and its graph against eager passes.
+
+The steps are taken on the codes and scales that the block itself made (their own tests hold them to their
+definitions), so the tolerances are those of one product each: four roundings of fp32, the gate's
+exponential, and one rounding to bf16 (2^-8 of the value)."""
+import pytest
+
+from paper_2007_06919_amd import aqd, ffn
+
+pytestmark = pytest.mark.gpu
+
+
+def block(torch, hidden, units, rows, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def randn(*shape, scale=1.0):
+        return (torch.randn(*shape, generator=g, device="cuda") * scale).bfloat16()
+
+    w = (1 + 0.1 * randn(hidden), randn(units, hidden, scale=hidden ** -0.5), randn(units, hidden, scale=hidden ** -0.5),
+         randn(hidden, units, scale=units ** -0.5))
+    return ffn.GatedFfn(*w, max_rows=rows), w, randn
+
+
+@pytest.mark.parametrize("rows, hidden, units", [(1, 256, 640), (3, 250, 333), (40, 512, 1000), (300, 1024, 768)])
+def test_block(rows, hidden, units):
+    import torch
+    f, w, randn = block(torch, hidden, units, rows)
+    x, r = randn(rows, hidden), randn(rows, hidden)
+    y, total = torch.empty_like(x), torch.empty_like(x)
+    f.forward(x, r, y, total)
+    torch.cuda.synchronize()
+    assert torch.equal(total, (x.float() + r.float()).bfloat16())
+
+    def product(c, q, w, s, k):
+        return torch.mm(c[:, :k].double() * q.double()[:, None], (w.double() * s.double()[:, None]).t().contiguous())
+
+    z = product(f.c1, f.q1, f.w1, f.s1, hidden)
+    h = z[:, :units] * torch.sigmoid(z[:, :units]) * z[:, units:]
+    tol = h.abs() * (2.0 ** -8 + 2.0 ** -18) + (z[:, units:].abs() + z[:, :units].abs()) * 2.0 ** -20
+    assert bool(((f.h[:rows].double() - h).abs() <= tol).all())
+    want = product(f.c2, f.q2, f.w2, f.s2, units)
+    assert bool(((y.double() - want).abs() <= want.abs() * 2.0 ** -8 + want.abs().max() * 2.0 ** -20).all())
+    # and near the block on the unquantised weights: codes of 8 bits are off by 1 part in 250 of the row's largest
+    real = ffn.reference(x, r, *w, f.eps)
+    assert float((y.float() - real).norm() / real.norm()) < 0.05
+
+
+def test_graph_and_in_place_residual():
+    import torch
+    rows, hidden = 24, 768
+    f, _, randn = block(torch, hidden, 1280, rows)
+    stream = torch.cuda.Stream()
+    x, r, y = randn(rows, hidden), randn(rows, hidden), torch.empty(rows, hidden, device="cuda").bfloat16()
+    torch.cuda.synchronize()
+    f.capture(x, r, y, r, stream)
+    try:
+        for _ in range(3):
+            x.copy_(randn(rows, hidden))
+            before, eager, total = r.clone(), torch.empty_like(y), torch.empty_like(r)
+            f.forward(x, before, eager, total)
+            torch.cuda.synchronize()
+            f.replay(stream)
+            torch.cuda.synchronize()
+            assert torch.equal(y, eager) and torch.equal(r, total)
+    finally:
+        f.close()
+
+
+def test_refusals():
+    import torch
+    f, w, randn = block(torch, 64, 96, 4)
+    x = randn(4, 64)
+    with pytest.raises(ValueError):
+        ffn.GatedFfn(w[0], w[1], w[2], w[1])
+    with pytest.raises(ValueError):
+        ffn.GatedFfn(*w, max_rows=0)
+    with pytest.raises(ValueError):
+        f.forward(randn(5, 64), randn(5, 64), randn(5, 64), randn(5, 64))
+    with pytest.raises(ValueError):
+        f.forward(x, x.float(), x.clone(), x.clone())
+    with pytest.raises(ValueError):
+        f.forward(x, x.clone(), x.clone(), randn(64, 4).t())
+    wider = randn(5, 64)
+    with pytest.raises(aqd.AqdError):   # total is x, shifted by one element
+        f.forward(wider[:4], x, x.clone(), wider.view(-1)[1:257].view(4, 64))
