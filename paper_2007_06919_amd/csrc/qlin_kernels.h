@@ -484,8 +484,13 @@ __device__ __forceinline__ void store_tile(const QlinArgs &A, const v16i (&acc)[
     const int lane = threadIdx.x & 63, o = lane % LANES * V;
     typedef T vecT __attribute__((ext_vector_type(V), aligned(sizeof(T))));
     const int j = j0 + o, left = A.n - j;
-    float ws[V] = {}, wb[V] = {}, vs[V] = {}, vb[V] = {};
+    // All scales are loaded before the first store (a load after one could not be moved up, and would be waited for
+    // in every round): lane l keeps the scale of token t0 + l, shuffled to the lanes that want it.
+    static_assert(NB <= 2, "a lane per token");
+    float ws[V] = {}, wb[V] = {}, vs[V] = {}, vb[V] = {}, xs = 0.f;
     if constexpr (!PART) {
+        if (lane < 32 * NB && t0 + lane < A.rows)
+            xs = A.x_scales[t0 + lane];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const int c = j + e < A.n ? j + e : A.n - 1;
@@ -525,8 +530,7 @@ __device__ __forceinline__ void store_tile(const QlinArgs &A, const v16i (&acc)[
                     else
                         put4<false>(A, part, t, j, 0, sums(o, 0));
                 }
-            } else if (t < A.rows) {
-                const float sx = A.x_scales[t];
+            } else if (const float sx = __shfl(xs, 32 * b + tr); t < A.rows) {
                 vecT y;
 #pragma unroll
                 for (int e = 0; e < V; e += 4) {
