@@ -224,6 +224,7 @@ struct QlinArgs {
     int ksplit, kchunk;                        // parts of the K range and their bytes (1: all of k)
     int32_t *part;                             // [ksplit][rows][1, or 2 with the gate][n_pad] partial sums of a split
     int n_pad;                                 // n rounded up to 4
+    int whole_lines;                           // stores of y are whole lines of 128 bytes, and pass the L2 by
 };
 // kernel and tile (outputs x tokens) of a launch: _ANY take rows at any address, FEW16 and FEW64 go by
 // 16 outputs and 16 or 64 tokens (qlin_kernels.h)

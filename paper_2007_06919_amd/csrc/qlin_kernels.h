@@ -450,11 +450,13 @@ __device__ __forceinline__ v4u32 raw_rsrc(const void *p)
                  (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xFFFFu)), 0xFFFFFFFFu, 0x00020000u};
 }
 
-// position of tile `id` of `total`: workgroups go round the 8 XCDs, so each XCD takes a
-// contiguous range, in strips of up to 4 token tiles along the rows of w: the tiles that
-// run at once on an XCD share their operands in its L2
+// Position of tile `id` of `total`. Workgroups go round the 8 XCDs, so each XCD takes a contiguous range, in
+// strips of up to 4 token tiles along the rows of w: the tiles that run at once on an XCD share their
+// operands in its L2. Each eighth of the strips starts an eighth further along (`tn`): where y's rows are a
+// power of two of bytes, XCDs that all write the same columns meet on a few memory channels (134 MB of y
+// 30.4 us together, 24.6 apart; 8192 x 8192 x 2048 155 -> 148 us).
 struct Place {
-    int tn, tt, part;
+    int tn, tt, part, xcd;
 };
 __device__ __forceinline__ Place place(unsigned id, unsigned total, int tiles_n, int tiles_t)
 {
@@ -462,12 +464,15 @@ __device__ __forceinline__ Place place(unsigned id, unsigned total, int tiles_n,
     unsigned t = x * q + (x < r ? x : r) + i;
     const unsigned per = (unsigned)tiles_n * (unsigned)tiles_t;
     Place p;
+    p.xcd = (int)x;
     p.part = (int)(t / per);
     t -= p.part * per;
     const unsigned strip = t / (4u * tiles_n), first = 4 * strip, high = tiles_t - first < 4 ? tiles_t - first : 4;
     t -= strip * 4u * tiles_n;
-    p.tn = (int)(t / high);
     p.tt = (int)(first + t % high);
+    const unsigned strips = (tiles_t + 3u) / 4, eighth = 8 * strip / strips;
+    t = t / high + (unsigned)((unsigned long long)eighth * tiles_n / 8);
+    p.tn = (int)(t < (unsigned)tiles_n ? t : t - tiles_n);
     return p;
 }
 
@@ -515,54 +520,64 @@ __device__ __forceinline__ void store_tile(const QlinArgs &A, const v16i (&acc)[
                 const int slot = (row / 4 + 2 * g + (lane >> 5)) ^ (tw & (SLOTS - 1));
                 *(v4i *)(stage + (tw * SLOTS + slot) * 16) = v4i{acc[i][b][4 * g], acc[i][b][4 * g + 1], acc[i][b][4 * g + 2], acc[i][b][4 * g + 3]};
             }
+        // (past: past the L2; a choice within a round would be lost where the compiler joins the stores again)
+        auto rounds = [&](auto past) {
 #pragma unroll
-        for (int it = 0; it < 32 * LANES / 64; ++it) {
-            const int tr = it * (64 / LANES) + lane / LANES;
-            const long long t = t0 + 32 * b + tr;
-            auto sums = [&](int row, int e) {
-                return *(const v4i *)(stage + (tr * SLOTS + (((row + e) / 4) ^ (tr & (SLOTS - 1)))) * 16);
-            };
-            if constexpr (PART) {
-                if (t < A.rows) {
-                    // with the gate the staged rows are both halves: j0 counts outputs, o staged rows
-                    if constexpr (GATE)
-                        put4<true>(A, part, t, j0 + o % (WIDE / 2), o / (WIDE / 2), sums(o, 0));
-                    else
-                        put4<false>(A, part, t, j, 0, sums(o, 0));
-                }
-            } else if (const float sx = __shfl(xs, 32 * b + tr); t < A.rows) {
-                vecT y;
+            for (int it = 0; it < 32 * LANES / 64; ++it) {
+                const int tr = it * (64 / LANES) + lane / LANES;
+                const long long t = t0 + 32 * b + tr;
+                auto sums = [&](int row, int e) {
+                    return *(const v4i *)(stage + (tr * SLOTS + (((row + e) / 4) ^ (tr & (SLOTS - 1)))) * 16);
+                };
+                if constexpr (PART) {
+                    if (t < A.rows) {
+                        // with the gate the staged rows are both halves: j0 counts outputs, o staged rows
+                        if constexpr (GATE)
+                            put4<true>(A, part, t, j0 + o % (WIDE / 2), o / (WIDE / 2), sums(o, 0));
+                        else
+                            put4<false>(A, part, t, j, 0, sums(o, 0));
+                    }
+                } else if (const float sx = __shfl(xs, 32 * b + tr); t < A.rows) {
+                    vecT y;
 #pragma unroll
-                for (int e = 0; e < V; e += 4) {
-                    const v4i c = sums(o, e);
-                    v4i d = {};
-                    if constexpr (GATE)
-                        d = sums(WIDE / 2 + o, e);
+                    for (int e = 0; e < V; e += 4) {
+                        const v4i c = sums(o, e);
+                        v4i d = {};
+                        if constexpr (GATE)
+                            d = sums(WIDE / 2 + o, e);
 #pragma unroll
-                    for (int f = 0; f < 4; ++f) {
-                        float z = (float)c[f] * sx * ws[e + f];
-                        if (A.bias)
-                            z += wb[e + f];
-                        if constexpr (GATE) {
-                            float v = (float)d[f] * sx * vs[e + f];
+                        for (int f = 0; f < 4; ++f) {
+                            float z = (float)c[f] * sx * ws[e + f];
                             if (A.bias)
-                                v += vb[e + f];
-                            z = silu(z) * v;
+                                z += wb[e + f];
+                            if constexpr (GATE) {
+                                float v = (float)d[f] * sx * vs[e + f];
+                                if (A.bias)
+                                    v += vb[e + f];
+                                z = silu(z) * v;
+                            }
+                            y[e + f] = (T)z;
                         }
-                        y[e + f] = (T)z;
+                    }
+                    T *out = (T *)A.y + t * A.ld_y + j;
+                    if (left >= V) {
+                        if constexpr (past.value)
+                            __builtin_nontemporal_store(y, (vecT *)out);
+                        else
+                            *(vecT *)out = y;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < V; ++e)
+                            if (e < left)
+                                out[e] = y[e];
                     }
                 }
-                T *out = (T *)A.y + t * A.ld_y + j;
-                if (left >= V) {
-                    *(vecT *)out = y;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < V; ++e)
-                        if (e < left)
-                            out[e] = y[e];
-                }
             }
-        }
+        };
+        if (!PART && A.whole_lines)
+            rounds(std::true_type{});
+        else
+            rounds(std::false_type{});
     }
 }
 
@@ -645,9 +660,10 @@ __global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, uns
     // that the counts of copies in flight hold)
     const int stages = (k1 - k0) / KS, last = stages - 1;
     // Where this workgroup starts: a sum's terms have no order. With rows of a power of two of bytes, workgroups that
-    // all read the same columns meet on a few memory channels; where each row of w is read by one of them
-    // (one token tile) they start apart: 16 x 16384 x 4096 gated 33.3 -> 28.9 us.
-    const int start = stages && tiles_t == 1 ? at.tn % stages : 0;
+    // all read the same columns meet on a few memory channels. Where each row of w is read by one of them
+    // (one token tile) all start apart (16 x 16384 x 4096 gated 33.3 -> 28.9 us), else the XCDs do, whose
+    // workgroups share their reads (8192 x 8192 x 8192 482 -> 470 us).
+    const int start = !stages ? 0 : tiles_t == 1 ? at.tn % stages : (int)((long long)stages * at.xcd / 8);
     auto turned = [&](int s) { return s + start < stages ? s + start : s + start - stages; };
     if (DEEP && stages) {
 #pragma unroll
