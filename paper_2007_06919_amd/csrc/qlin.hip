@@ -75,8 +75,8 @@ double time_of_few(const QlinArgs &a, int tokens, double fixed, double step, dou
 QlinPlan qlin_plan(const QlinArgs &a, size_t room)
 {
     QlinPlan best = {QLIN_ANY, 1, 0};
-    // offsets inside a tile have 32 bits
-    if (std::max(a.ld_x, a.ld_w) >= 1 << 23)
+    // offsets inside a tile have 32 bits, and the other kernels' loads 16 bytes
+    if (std::max(a.ld_x, a.ld_w) >= 1 << 23 || a.k < 16)
         return best;
     double least = 1e30;
     const bool aligned = aligned_rows(a);
@@ -156,12 +156,11 @@ hipError_t launch_qlin(const QlinArgs &args, const QlinPlan &plan, hipStream_t s
 {
     QlinArgs a = args;
     a.n_pad = (a.n + 3) & ~3;
-    // Stores of whole lines pass the L2 by where y is larger than the caches would keep for its reader: 8192 x 8192 x 2048
-    // (134 MB) 148 -> 138 us; a feed-forward block of 1024 rows, whose hidden units (23 MB) are read at once, is
-    // 162 us with them in the caches and 171 past them. Parts of lines, which the L2 joins, do not
-    // (22300 x 720 x 256 19.4 us, and 23.1 past it).
+    // Stores of whole lines pass the L2 by: 8192 x 8192 x 2048 148 -> 138 us, 2048 x 11264 x 4096 gated 191 -> 183, and
+    // a feed-forward block of 2048 rows that reads its hidden units at once 297 -> 290. Parts of lines, which the
+    // L2 joins, do not (22300 x 720 x 256 19.4 us, and 23.1 past it), nor do small outputs.
     const int size = a.type == AQD_F32 ? 4 : 2;
-    a.whole_lines = (((uintptr_t)a.y | (uintptr_t)a.ld_y * size) & 127) == 0 && (double)a.rows * a.n * size >= 64e6;
+    a.whole_lines = (((uintptr_t)a.y | (uintptr_t)a.ld_y * size) & 127) == 0 && (double)a.rows * a.n * size >= 4e6;
     // whole stages per part
     const int stages = a.k / 128 + (a.k % 128 != 0);
     a.kchunk = 128 * ((stages + plan.parts - 1) / plan.parts);

@@ -155,28 +155,30 @@ __device__ __forceinline__ v4i shifted(const Words &r, int shift)
                (int)__builtin_amdgcn_alignbyte((unsigned)r.more, (unsigned)r.v[3], (unsigned)shift)};
 }
 
-// The 16 bytes of a row from c on where the row may end (at k) inside them or before them: nothing
+// The 16 bytes of a row from c on where the row may end (at k >= 16) inside them or before them: nothing
 // past it is read. A sum's terms have no order, so the 16 bytes then are the row's last, and
 // the terms that another lane or step has too are zeros in the tokens (TOKEN).
 template <bool TOKEN>
 __device__ __forceinline__ v4i load16(const int8_t *row, int c, int k)
 {
-    v4i v = {0, 0, 0, 0};
-    if (k < 16) {
-#pragma unroll
-        for (int e = 0; e < 15; ++e)
-            if (c + e < k)
-                v[e / 4] |= (int)(uint8_t)row[c + e] << (8 * (e % 4));
-        return v;
-    }
     const int at = c < k - 16 ? c : k - 16, gone = c - at;
-    v = *(const v4u *)(row + at);
+    v4i v = *(const v4u *)(row + at);
     if constexpr (TOKEN)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int z = gone - 4 * e;
             v[e] = z >= 4 ? 0 : z > 0 ? (int)((uint32_t)v[e] >> (8 * z) << (8 * z)) : v[e];
         }
+    return v;
+}
+// the same where k may be less than 16: byte by byte, zeros from k on
+__device__ __forceinline__ v4i load_bytes(const int8_t *row, int c, int k)
+{
+    v4i v = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 15; ++e)
+        if (c + e < k)
+            v[e / 4] |= (int)(uint8_t)row[c + e] << (8 * (e % 4));
     return v;
 }
 
@@ -234,8 +236,9 @@ __global__ void __launch_bounds__(256) qlin_any_kernel(QlinArgs A, long long til
             sw = sx = 0;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                w[h].v = load16<false>(pw, k + 16 * c + 64 * h, kn);
-                x[h].v = load16<true>(px, k + 16 * c + 64 * h, kn);
+                const int at = k0 + k + 16 * c + 64 * h;   // (a part may be shorter than 16, all of k rarely)
+                w[h].v = k1 < 16 ? load_bytes(pw - k0, at, k1) : load16<false>(pw - k0, at, k1);
+                x[h].v = k1 < 16 ? load_bytes(px - k0, at, k1) : load16<true>(px - k0, at, k1);
             }
         }
     };
@@ -456,22 +459,29 @@ __device__ __forceinline__ v4u32 raw_rsrc(const void *p)
 // power of two of bytes, XCDs that all write the same columns meet on a few memory channels (134 MB of y
 // 30.4 us together, 24.6 apart; 8192 x 8192 x 2048 155 -> 148 us).
 struct Place {
-    int tn, tt, part, xcd;
+    int tn, tt, part, eighth;
 };
+template <bool PART>
 __device__ __forceinline__ Place place(unsigned id, unsigned total, int tiles_n, int tiles_t)
 {
     const unsigned x = id & 7, i = id >> 3, q = total >> 3, r = total & 7;
     unsigned t = x * q + (x < r ? x : r) + i;
-    const unsigned per = (unsigned)tiles_n * (unsigned)tiles_t;
-    Place p;
-    p.xcd = (int)x;
-    p.part = (int)(t / per);
-    t -= p.part * per;
+    Place p = {0, 0, 0, 0};
+    if constexpr (PART) {
+        const unsigned per = (unsigned)tiles_n * (unsigned)tiles_t;
+        p.part = (int)(t / per);
+        t -= p.part * per;
+    }
+    if (tiles_t <= 4) {   // one strip
+        p.tn = (int)(t / (unsigned)tiles_t);
+        p.tt = (int)(t - p.tn * (unsigned)tiles_t);
+        return p;
+    }
     const unsigned strip = t / (4u * tiles_n), first = 4 * strip, high = tiles_t - first < 4 ? tiles_t - first : 4;
     t -= strip * 4u * tiles_n;
+    p.eighth = (int)(8 * strip / ((tiles_t + 3u) / 4));
     p.tt = (int)(first + t % high);
-    const unsigned strips = (tiles_t + 3u) / 4, eighth = 8 * strip / strips;
-    t = t / high + (unsigned)((unsigned long long)eighth * tiles_n / 8);
+    t = t / high + (unsigned)((unsigned long long)p.eighth * tiles_n / 8);
     p.tn = (int)(t < (unsigned)tiles_n ? t : t - tiles_n);
     return p;
 }
@@ -481,7 +491,7 @@ __device__ __forceinline__ Place place(unsigned id, unsigned total, int tiles_n,
 // lane keeps the scales of its channels. A lane holds token lane % 32, rows 8 g + 4 (lane / 32)
 // .. + 3 of each 32 x 32; the 16-byte columns of a staged token are XORed with the token. With the gate
 // the value rows follow the gate rows.
-template <typename T, bool GATE, bool PART, int NA, int NB>
+template <typename T, bool GATE, bool PART, bool PAST, int NA, int NB>
 __device__ __forceinline__ void store_tile(const QlinArgs &A, const v16i (&acc)[NA][NB], int8_t *stage, int part, long long t0, int j0)
 {
     constexpr int WIDE = 32 * NA, SLOTS = WIDE / 4, OUT = GATE && !PART ? WIDE / 2 : WIDE;
@@ -520,7 +530,8 @@ __device__ __forceinline__ void store_tile(const QlinArgs &A, const v16i (&acc)[
                 const int slot = (row / 4 + 2 * g + (lane >> 5)) ^ (tw & (SLOTS - 1));
                 *(v4i *)(stage + (tw * SLOTS + slot) * 16) = v4i{acc[i][b][4 * g], acc[i][b][4 * g + 1], acc[i][b][4 * g + 2], acc[i][b][4 * g + 3]};
             }
-        // (past: past the L2; a choice within a round would be lost where the compiler joins the stores again)
+        // (past: past the L2, in tiles of large outputs; a choice within a round would be lost where the compiler joins
+        // the stores again)
         auto rounds = [&](auto past) {
 #pragma unroll
             for (int it = 0; it < 32 * LANES / 64; ++it) {
@@ -574,10 +585,13 @@ __device__ __forceinline__ void store_tile(const QlinArgs &A, const v16i (&acc)[
                 }
             }
         };
-        if (!PART && A.whole_lines)
-            rounds(std::true_type{});
-        else
-            rounds(std::false_type{});
+        if constexpr (PAST && !PART) {
+            if (A.whole_lines) {
+                rounds(std::true_type{});
+                continue;
+            }
+        }
+        rounds(std::false_type{});
     }
 }
 
@@ -597,7 +611,7 @@ __global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, uns
     static_assert(COPY || (RING == 2 && !DEEP), "through registers: two places, stages of many MFMAs");
     __shared__ __attribute__((aligned(16))) int8_t ring[RING * STAGE];
     const int tiles_n = (A.n + OUT - 1) / OUT, tiles_t = (int)((A.rows + (long long)TM - 1) / TM);
-    const Place at = place(tile0 + blockIdx.x, total, tiles_n, tiles_t);
+    const Place at = place<PART>(tile0 + blockIdx.x, total, tiles_n, tiles_t);
     const int k0 = at.part * A.kchunk, k1 = A.k - k0 < A.kchunk ? A.k : k0 + A.kchunk;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t base = lds_addr(ring);
@@ -661,9 +675,9 @@ __global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, uns
     const int stages = (k1 - k0) / KS, last = stages - 1;
     // Where this workgroup starts: a sum's terms have no order. With rows of a power of two of bytes, workgroups that
     // all read the same columns meet on a few memory channels. Where each row of w is read by one of them
-    // (one token tile) all start apart (16 x 16384 x 4096 gated 33.3 -> 28.9 us), else the XCDs do, whose
-    // workgroups share their reads (8192 x 8192 x 8192 482 -> 470 us).
-    const int start = !stages ? 0 : tiles_t == 1 ? at.tn % stages : (int)((long long)stages * at.xcd / 8);
+    // (one token tile) all start apart (16 x 16384 x 4096 gated 33.3 -> 28.9 us); of many token tiles each eighth
+    // does, whose workgroups share their reads (8192 x 8192 x 8192 482 -> 470 us).
+    const int start = !stages ? 0 : tiles_t == 1 ? at.tn % stages : (int)((long long)stages * at.eighth / 8);
     auto turned = [&](int s) { return s + start < stages ? s + start : s + start - stages; };
     if (DEEP && stages) {
 #pragma unroll
@@ -777,8 +791,8 @@ __global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, uns
         for (int q = 0; q < COPIES; ++q) {
             const int c = (lane & 7) ^ swz(8 * (wave + WAVES * q) + (lane >> 3));
             *(v4i *)(ring + 1024 * (wave + WAVES * q) + 16 * lane) =
-                q < WCOPIES ? load16<false>(source(q) + k0 + (voff[q] - 16 * c), k - k0 + 16 * c, k1 - k0)
-                            : load16<true>(source(q) + k0 + (voff[q] - 16 * c), k - k0 + 16 * c, k1 - k0);
+                q < WCOPIES ? load16<false>(source(q) + (voff[q] - 16 * c), k + 16 * c, k1)
+                            : load16<true>(source(q) + (voff[q] - 16 * c), k + 16 * c, k1);
         }
         __syncthreads();
 #pragma unroll
@@ -797,7 +811,7 @@ __global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, uns
     __syncthreads();   // every wave is done with the ring, which now stages the outputs
     const int j0 = at.tn * OUT + wn * (OUT / WN);
     const long long t0 = (long long)at.tt * TM + wm * (TM / WM);
-    store_tile<T, GATE, PART, NA, NB>(A, acc, ring + wave * 32 * NA * 32 * 4, at.part, t0, j0);
+    store_tile<T, GATE, PART, (TN * TM >= 256 * 128), NA, NB>(A, acc, ring + wave * 32 * NA * 32 * 4, at.part, t0, j0);
 }
 
 // ---- launches ---------------------------------------------------------------------------
