@@ -322,8 +322,8 @@ aqd_status_t aqd_maxpool_run(const aqd_maxpool_desc_t *desc, const void *x, void
  * Every matrix has a row stride ld in elements, at least its columns (0: its
  * columns); bytes between a row's end and the next row are never written, and
  * what they hold does not matter. Pointers need the alignment of their elements only
- * (int8 any address): rows of 16-byte aligned addresses and strides run
- * fastest. Two matrices of one call may be column ranges of one buffer (of one
+ * (int8 any address): rows that start at whole lines of 128 bytes run fastest,
+ * then those at multiples of 4. Two matrices of one call may be column ranges of one buffer (of one
  * stride); an output must share no element with an input or another output, but
  * for qnorm's sum. rows == 0 is a no-op. The calls allocate nothing and may be
  * recorded into a graph. */

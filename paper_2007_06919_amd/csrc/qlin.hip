@@ -59,7 +59,8 @@ double time_of(const QlinArgs &a, const Shape &s, int parts)
     return LAUNCH + t;
 }
 
-bool aligned_rows(const QlinArgs &a) { return (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.ld_x | (uintptr_t)a.ld_w) & 15) == 0; }
+// the copies into LDS take whole words
+bool aligned_rows(const QlinArgs &a) { return (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.ld_x | (uintptr_t)a.ld_w) & 3) == 0; }
 
 // The small launches' kernel, in the same way: us per round of 256 workgroups, a fixed part and one per
 // 256 k (with the gate `gate` times as much), and the rate it reads weights at, bytes per us.
@@ -108,8 +109,7 @@ QlinPlan qlin_plan(const QlinArgs &a, size_t room)
         }
     };
     if (aligned) {
-        if (a.rows <= 16)
-            consider_few(QLIN_FEW16, 16, time_of_few(a, 16, 2.0, 0.09, 2.0, 4.1e6));
+        consider_few(QLIN_FEW16, 16, time_of_few(a, 16, 2.0, 0.09, 2.0, 4.1e6));
     } else {
         consider_few(QLIN_FEW16, 16, time_of_few(a, 16, 1.6, 0.26, 1.96, 2.6e6));
         consider_few(QLIN_FEW64, 64, time_of_few(a, 64, 1.8, 0.41, 1.82, 3.5e6));
