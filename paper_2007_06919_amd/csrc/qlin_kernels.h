@@ -27,11 +27,8 @@ __device__ __forceinline__ void scaled4(const QlinArgs &A, const v4i acc, int j,
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         z[e] = (float)acc[e] * sx;
-        if (e < left) {
-            z[e] *= A.w_scales[j + e];
-            if (A.bias)
-                z[e] += A.bias[j + e];
-        }
+        if (e < left)
+            z[e] = __builtin_fmaf(z[e], A.w_scales[j + e], A.bias ? A.bias[j + e] : 0.f);
     }
 }
 
@@ -425,6 +422,8 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) qlin_few_kernel(QlinArgs A)
 // they straddle cost 10 to 25%: 1000 x 4096 x 4096 21.5 us at multiples of 128, 26.4 at others).
 // Otherwise they start anywhere and pass through registers, loaded one stage before they
 // are written (RING 2).
+// The k that no whole stage has are copied as one more stage, after the others (5264 x 6912 x 560 47.7 us, 51.5
+// where they passed through registers after the last MFMA).
 //
 // While the MFMAs of one step run, the fragments of the next are read; in the last step, after the
 // first few MFMAs, the workgroup meets: by then each wave has read all of its stage (so its place
@@ -559,15 +558,9 @@ __device__ __forceinline__ void store_tile(const QlinArgs &A, const v16i (&acc)[
                             d = sums(WIDE / 2 + o, e);
 #pragma unroll
                         for (int f = 0; f < 4; ++f) {
-                            float z = (float)c[f] * sx * ws[e + f];
-                            if (A.bias)
-                                z += wb[e + f];
-                            if constexpr (GATE) {
-                                float v = (float)d[f] * sx * vs[e + f];
-                                if (A.bias)
-                                    v += vb[e + f];
-                                z = silu(z) * v;
-                            }
+                            float z = __builtin_fmaf((float)c[f] * sx, ws[e + f], wb[e + f]);
+                            if constexpr (GATE)
+                                z = silu(z) * __builtin_fmaf((float)d[f] * sx, vs[e + f], vb[e + f]);
                             y[e + f] = (T)z;
                         }
                     }
@@ -597,7 +590,7 @@ __device__ __forceinline__ void store_tile(const QlinArgs &A, const v16i (&acc)[
 }
 
 template <typename T, bool GATE, bool PART, bool COPY, int TN, int TM, int WN, int WM, int RING>
-__global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, unsigned tile0, unsigned total)
+__global__ void __launch_bounds__(64 * WN * WM, RING * (TN + TM) * KS <= 80 << 10 ? (WN * WM + 1) / 2 : 1) qlin_tile_kernel(QlinArgs A, unsigned tile0, unsigned total)
 {
     constexpr int WAVES = WN * WM, NA = TN / WN / 32, NB = TM / WM / 32, OUT = GATE ? TN / 2 : TN;
     constexpr int STAGE = (TN + TM) * KS, STEPS = KS / 32;
@@ -636,10 +629,13 @@ __global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, uns
         }
     }
     auto source = [&](int q) { return q >= WCOPIES ? xbase : GATE && (8 * (wave + WAVES * q) & 32) ? vbase : wbase; };
-    const v4u32 rw = raw_rsrc(wbase + k0), rv = raw_rsrc(vbase + k0), rx = raw_rsrc(xbase + k0);
-    // copy q of stage `stage` into place `place` of the ring
-    auto copy = [&](int q, int stage, int place) {
-        copy16(q >= WCOPIES ? rx : GATE && (8 * (wave + WAVES * q) & 32) ? rv : rw, voff[q], (uint32_t)KS * stage,
+    const v4u32 rw = raw_rsrc(wbase), rv = raw_rsrc(vbase), rx = raw_rsrc(xbase);
+    // copy q of the stage at `from` into place `place` of the ring
+    struct From {
+        uint32_t soff, slide;
+    };
+    auto copy = [&](int q, From from, int place) {
+        copy16(q >= WCOPIES ? rx : GATE && (8 * (wave + WAVES * q) & 32) ? rv : rw, voff[q] + from.slide, from.soff,
                __builtin_amdgcn_readfirstlane(base + (uint32_t)place * STAGE + 1024u * (wave + WAVES * q)));
     };
     // The other way in: the next HOLD copies are on their way through registers. Half a stage of them where
@@ -673,27 +669,43 @@ __global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, uns
 
     // (copies and loads past the last stage take the last stage again, into a place that nothing reads, so
     // that the counts of copies in flight hold)
-    const int stages = (k1 - k0) / KS, last = stages - 1;
+    const int stages = (k1 - k0) / KS, last = stages - 1, rest = k0 + KS * stages;   // rest: the k that no whole stage has
     // Where this workgroup starts: a sum's terms have no order. With rows of a power of two of bytes, workgroups that
     // all read the same columns meet on a few memory channels. Where each row of w is read by one of them
     // (one token tile) all start apart (16 x 16384 x 4096 gated 33.3 -> 28.9 us); of many token tiles each eighth
     // does, whose workgroups share their reads (8192 x 8192 x 8192 482 -> 470 us).
     const int start = !stages ? 0 : tiles_t == 1 ? at.tn % stages : (int)((long long)stages * at.eighth / 8);
     auto turned = [&](int s) { return s + start < stages ? s + start : s + start - stages; };
+    // Where the copies of the s-th stage start. The k that no whole stage has are one more; a row ends inside it, and
+    // a lane whose 16 bytes would pass the row's last word takes the 16 bytes up to there (load16 does the same).
+    const int end = (k1 + 3) & ~3;   // (of whole words; k >= 16)
+    auto first = [&](int c) { return rest + 16 * c < end - 16 ? rest + 16 * c : end - 16; };
+    const int mine = (lane & 7) ^ swz(8 * wave + (lane >> 3));   // this lane's column in each of its copies
+    const uint32_t slide = (uint32_t)(first(mine) - 16 * mine);
+    static_assert(WAVES % 2 == 0, "swz is the same in all copies of a wave");
+    auto from = [&](int s) {
+        return s == stages && rest < k1 ? From{0, slide} : From{(uint32_t)(k0 + KS * turned(s < last ? s : last)), 0};
+    };
+    int place = 0;
+    if (COPY && !stages) {
+#pragma unroll
+        for (int q = 0; q < COPIES; ++q)
+            copy(q, from(0), 0);
+    }
     if (DEEP && stages) {
 #pragma unroll
         for (int s = 0; s < RING; ++s)
 #pragma unroll
             for (int q = 0; q < COPIES; ++q)
-                copy(q, turned(s < last ? s : last), s);
+                copy(q, from(s), s);
         wait_vmcnt<(RING - 1) * COPIES>();
         asm volatile("s_barrier" ::: "memory");
         static_for<STEPS * R>([&](auto i) { read(i.value / R, i.value % R, col[i.value / R]); });
-        int place = 0;
         auto stage = [&](auto P, int s) {
             // every wave has read stage s, whose place may be refilled, and stage s + 1 has landed
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((RING - 2) * COPIES) : "memory");
-            const int next = place + 1 == RING ? 0 : place + 1, ahead = turned(s + RING < last ? s + RING : last);
+            const int next = place + 1 == RING ? 0 : place + 1;
+            const From ahead = from(s + RING);
             static_for<STEPS * R>([&](auto i) {
                 read((1 - P.value) * STEPS + i.value / R, i.value % R, next * STAGE + col[i.value / R]);
             });
@@ -716,7 +728,7 @@ __global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, uns
             for (int s = 0; s < RING - 1; ++s)
 #pragma unroll
                 for (int q = 0; q < COPIES; ++q)
-                    copy(q, turned(s < last ? s : last), s);
+                    copy(q, from(s), s);
             wait_vmcnt<(RING - 2) * COPIES>();
             asm volatile("s_barrier" ::: "memory");
         } else {
@@ -740,8 +752,10 @@ __global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, uns
         constexpr int SPREAD = M * (STEPS - 1);              // MFMAs that the copies are spread over
         int off = 0;
         for (int s = 0; s < stages; ++s) {
-            const int ahead = turned(s + RING - 1 < last ? s + RING - 1 : last), into = (s + RING - 1) % RING;
-            const int after = turned(s + 2 < last ? s + 2 : last);   // (through registers: ahead is the stage s + 1)
+            const int into = (s + RING - 1) % RING;
+            const From ahead = from(s + RING - 1);
+            // (through registers)
+            const int next_load = turned(s + 1 < last ? s + 1 : last), after = turned(s + 2 < last ? s + 2 : last);
             static_for<STEPS - 1>([&](auto p) {
                 static_for<M>([&](auto m) {
                     static_for<R>([&](auto i) {
@@ -756,7 +770,7 @@ __global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, uns
                             } else {
                                 store(q.value, into);
                                 if constexpr (q.value + HOLD < COPIES)
-                                    load(q.value + HOLD, ahead);
+                                    load(q.value + HOLD, next_load);
                                 else
                                     load(q.value + HOLD - COPIES, after);
                             }
@@ -784,25 +798,41 @@ __global__ void __launch_bounds__(64 * WN * WM) qlin_tile_kernel(QlinArgs A, uns
             off = next;
         }
     }
-    // the last k, where 128 does not divide them, through registers
+    // the last k, where 128 does not divide them
     wait_vmcnt<0>();
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (const int k = k0 + KS * stages; k < k1) {
+    if (rest < k1) {
+        const int off = COPY ? stages % RING * STAGE : 0;
+        if constexpr (!COPY) {
 #pragma unroll
-        for (int q = 0; q < COPIES; ++q) {
-            const int c = (lane & 7) ^ swz(8 * (wave + WAVES * q) + (lane >> 3));
-            *(v4i *)(ring + 1024 * (wave + WAVES * q) + 16 * lane) =
-                q < WCOPIES ? load16<false>(source(q) + (voff[q] - 16 * c), k + 16 * c, k1)
-                            : load16<true>(source(q) + (voff[q] - 16 * c), k + 16 * c, k1);
+            for (int q = 0; q < COPIES; ++q) {
+                const int c = (lane & 7) ^ swz(8 * (wave + WAVES * q) + (lane >> 3));
+                *(v4i *)(ring + 1024 * (wave + WAVES * q) + 16 * lane) =
+                    q < WCOPIES ? load16<false>(source(q) + (voff[q] - 16 * c), rest + 16 * c, k1)
+                                : load16<true>(source(q) + (voff[q] - 16 * c), rest + 16 * c, k1);
+            }
+            __syncthreads();
         }
-        __syncthreads();
 #pragma unroll
         for (int p = 0; p < STEPS; ++p) {
-            if (k + 32 * p >= k1)
+            if (rest + 32 * p >= k1)
                 break;
 #pragma unroll
             for (int i = 0; i < R; ++i)
-                read(p & 1, i, col[p]);
+                read(p & 1, i, off + col[p]);
+            if constexpr (COPY) {   // zeros in the tokens for what is past the row, or in another lane or stage too
+                const int c = 2 * p + (lane >> 5), gone = rest + 16 * c - first(c), over = end - k1;
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int z = gone - 4 * e;
+                        uint32_t mask = z >= 4 ? 0u : z > 0 ? ~0u << (8 * z) : ~0u;
+                        if (e == 3 && first(c) == end - 16)
+                            mask &= ~0u >> (8 * over);
+                        b[p & 1][j][e] &= (int)mask;
+                    }
+            }
 #pragma unroll
             for (int m = 0; m < M; ++m)
                 mfma(p & 1, m);

@@ -424,3 +424,27 @@ def test_large_products(rows, n, k, act):
     tol = tol * 1.01 + want.abs() * 2.0 ** -24 + 2.0 ** -150
     assert torch.equal(y[0], y[1])
     assert bool(((y[0].double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("rows, n", [(20, 70), (70, 200), (130, 600), (600, 1030), (1200, 2300)])
+@pytest.mark.parametrize("k", [16, 17, 19, 66, 127, 129, 130, 143, 255, 387, 1021, 2050, 4097])
+def test_rows_that_end_inside_a_stage(rows, n, k):
+    """Rows at multiples of 4 bytes with junk behind any number of codes: exact sums (below 2^24), alone and split, and the
+    gated unit on them (the multiplications by powers of two are exact: silu's units and the product's rounding are left)."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(rows + k)
+    codes = [torch.randint(-15, 16, (r, k), generator=g, device="cuda", dtype=torch.int8) for r in (rows, 2 * n)]
+    lds = [-(-k // 4) * 4 + 4 * e for e in (0, 1)]
+    (_, x), (_, w) = (matrix(torch, c.cpu(), ld, 4, junk=-128) for c, ld in zip(codes, lds))
+    one = torch.ones(2 * max(rows, n), device="cuda")
+    work = torch.empty(aqd.QLIN_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+    sums = torch.mm(codes[0].double(), codes[1].double().t().contiguous())
+    for ws in (work, None):
+        y = torch.zeros(rows, n, device="cuda")
+        aqd.qlin_run(rows, n, k, aqd.F32, aqd.QLIN_PLAIN, x, lds[0], one, w, lds[1], one, None, y, 0, ws, work.numel() if ws is not None else 0)
+        assert torch.equal(y.double(), sums[:, :n])
+        aqd.qlin_run(rows, n, k, aqd.F32, aqd.QLIN_SILU_GATE, x, lds[0], one / 64, w, lds[1], one / 64, None, y, 0, ws,
+                     work.numel() if ws is not None else 0)
+        z, v = sums[:, :n] / 4096, sums[:, n:] / 4096
+        want = z / (1 + torch.exp(-z)) * v
+        assert bool(((y.double() - want).abs() <= want.abs() * ((z.abs() + 4) * 2.0 ** -22 + 2.0 ** -23) + 2.0 ** -149).all())
