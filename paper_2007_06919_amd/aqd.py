@@ -153,11 +153,13 @@ def _check(status):
 
 
 def _addr(t):
+    if t is None:
+        return None
     try:
         return t.data_ptr()
     except AttributeError:
         pass
-    if t is None or isinstance(t, int):
+    if isinstance(t, int):
         return t
     return t.ctypes.data
 
