@@ -549,7 +549,7 @@ __device__ __forceinline__ void store_tile(const QlinArgs &A, const v16i (&acc)[
                             put4<false>(A, part, t, j, 0, sums(o, 0));
                     }
                 } else if (const float sx = __shfl(xs, 32 * b + tr); t < A.rows) {
-                    vecT y;
+                    float zs __attribute__((ext_vector_type(V)));
 #pragma unroll
                     for (int e = 0; e < V; e += 4) {
                         const v4i c = sums(o, e);
@@ -561,9 +561,10 @@ __device__ __forceinline__ void store_tile(const QlinArgs &A, const v16i (&acc)[
                             float z = __builtin_fmaf((float)c[f] * sx, ws[e + f], wb[e + f]);
                             if constexpr (GATE)
                                 z = silu(z) * __builtin_fmaf((float)d[f] * sx, vs[e + f], vb[e + f]);
-                            y[e + f] = (T)z;
+                            zs[e + f] = z;
                         }
                     }
+                    const vecT y = __builtin_convertvector(zs, vecT);
                     T *out = (T *)A.y + t * A.ld_y + j;
                     if (left >= V) {
                         if constexpr (past.value)
