@@ -156,7 +156,7 @@ hipError_t launch_qlin(const QlinArgs &args, const QlinPlan &plan, hipStream_t s
 {
     QlinArgs a = args;
     a.n_pad = (a.n + 3) & ~3;
-    // Stores of whole lines pass the L2 by: 8192 x 8192 x 2048 148 -> 138 us, 2048 x 11264 x 4096 gated 191 -> 183, and
+    // Stores of whole lines pass the L2 by: 8192 x 8192 x 2048 148 -> 138 us (135 now), 2048 x 11264 x 4096 gated 191 -> 183 (180), and
     // a feed-forward block of 2048 rows that reads its hidden units at once 297 -> 290. Parts of lines, which the
     // L2 joins, do not (22300 x 720 x 256 19.4 us, and 23.1 past it), nor do small outputs.
     const int size = a.type == AQD_F32 ? 4 : 2;

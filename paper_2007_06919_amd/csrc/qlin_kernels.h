@@ -77,6 +77,8 @@ __device__ __forceinline__ void put4(const QlinArgs &A, int part, long long t, i
         *(v4i *)(A.part + (((long long)part * A.rows + t) * (GATE ? 2 : 1) + half) * A.n_pad + j) = acc;
 }
 
+// The parts' sums, scaled and stored: bound by its launch and one round of loads from the L2
+// (192 x 4096 in four parts, 12.6 MB, 3.9 us).
 template <typename T, bool GATE>
 __global__ void __launch_bounds__(256) qlin_combine_kernel(QlinArgs A)
 {
@@ -183,7 +185,8 @@ __device__ __forceinline__ v4i load_bytes(const int8_t *row, int c, int k)
 // 64 rows of w x 64 tokens, both through registers into LDS, 128 k a stage, loaded a stage and
 // a half before they are used. Wave i: the 64 rows of w by tokens 16i .. 16i+15. With the gate the
 // tile's first 32 rows are gate rows and the others the value rows of the same outputs. Takes every
-// stride (64-bit addresses).
+// stride (64-bit addresses) and any k. For small launches whose rows start at odd bytes, where it is bound by the
+// chain from load to LDS to MFMA (200 x 2000 x 501 packed 7.3 us, 300 x 3000 x 301 6.8), and for what no other takes.
 constexpr int KS = 128;   // k of a stage
 
 // XOR of the 16-byte columns of LDS row r (128 bytes): 16-byte reads of consecutive rows at one column
@@ -293,6 +296,8 @@ __global__ void __launch_bounds__(256) qlin_any_kernel(QlinArgs A, long long til
 // One workgroup per 16 outputs and 16 NB tokens, its waves splitting k, 64 at a time, and adding
 // their sums in LDS: no LDS and no barrier in the loop, and the shortest chain from launch to
 // store. Rows start at any byte, their 16 (tokens: 16 NB) within 32 bits of offset.
+// Bound by the launch and the first loads' latency (77 x 1003 x 515 packed 6.2 us), then by the
+// weights' stream (1 x 4096 x 4096 6.6 us, 16.8 MB; at most 4.1 TB/s, where the tiles below reach 4.5).
 constexpr int FEW_WAVES = 4;
 
 template <typename T, bool GATE, bool BYTES, int NB, int U>
@@ -432,6 +437,10 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) qlin_few_kernel(QlinArgs A)
 //
 // The 16-byte columns of LDS row r (128 bytes) sit XORed with swz(r), which is done by permuting the
 // lanes' source columns; fragment reads hit every bank once (no conflict in the counters).
+//
+// Large products are bound by power: 8192 x 8192 x 8192 takes 450 to 466 us (2360 to 2440 TOPS), its matrix cores busy
+// for 63% of the cycles of a clock that falls to 1.7 GHz (on codes of zero 404 us). Small tiles are bound by their
+// copies (about 47 bytes a clock and CU) and their first and last microseconds.
 typedef int v16i __attribute__((ext_vector_type(16)));
 typedef uint32_t v4u32 __attribute__((ext_vector_type(4)));
 
@@ -457,7 +466,7 @@ __device__ __forceinline__ v4u32 raw_rsrc(const void *p)
 // strips of up to 4 token tiles along the rows of w: the tiles that run at once on an XCD share their
 // operands in its L2. Each eighth of the strips starts an eighth further along (`tn`): where y's rows are a
 // power of two of bytes, XCDs that all write the same columns meet on a few memory channels (134 MB of y
-// 30.4 us together, 24.6 apart; 8192 x 8192 x 2048 155 -> 148 us).
+// 30.4 us together, 24.6 apart; 8192 x 8192 x 2048 155 -> 148 us when it came in).
 struct Place {
     int tn, tt, part, eighth;
 };
@@ -591,7 +600,8 @@ __device__ __forceinline__ void store_tile(const QlinArgs &A, const v16i (&acc)[
 }
 
 template <typename T, bool GATE, bool PART, bool COPY, int TN, int TM, int WN, int WM, int RING>
-__global__ void __launch_bounds__(64 * WN * WM, RING * (TN + TM) * KS <= 80 << 10 ? (WN * WM + 1) / 2 : 1) qlin_tile_kernel(QlinArgs A, unsigned tile0, unsigned total)
+__global__ void __launch_bounds__(64 * WN * WM, RING * (TN + TM) * KS <= 80 << 10 ? (WN * WM + 1) / 2 : 1)
+qlin_tile_kernel(QlinArgs A, unsigned tile0, unsigned total)   // (waves per SIMD: registers for two workgroups where LDS has room for them)
 {
     constexpr int WAVES = WN * WM, NA = TN / WN / 32, NB = TM / WM / 32, OUT = GATE ? TN / 2 : TN;
     constexpr int STAGE = (TN + TM) * KS, STEPS = KS / 32;
@@ -673,8 +683,8 @@ __global__ void __launch_bounds__(64 * WN * WM, RING * (TN + TM) * KS <= 80 << 1
     const int stages = (k1 - k0) / KS, last = stages - 1, rest = k0 + KS * stages;   // rest: the k that no whole stage has
     // Where this workgroup starts: a sum's terms have no order. With rows of a power of two of bytes, workgroups that
     // all read the same columns meet on a few memory channels. Where each row of w is read by one of them
-    // (one token tile) all start apart (16 x 16384 x 4096 gated 33.3 -> 28.9 us); of many token tiles each eighth
-    // does, whose workgroups share their reads (8192 x 8192 x 8192 482 -> 470 us).
+    // (one token tile) all start apart (16 x 16384 x 4096 gated 34.3 -> 30.1 us); of many token tiles each eighth
+    // does, whose workgroups share their reads (2048 x 11264 x 4096 gated 186 -> 180 us, 8192 x 8192 x 8192 the same).
     const int start = !stages ? 0 : tiles_t == 1 ? at.tn % stages : (int)((long long)stages * at.eighth / 8);
     auto turned = [&](int s) { return s + start < stages ? s + start : s + start - stages; };
     // Where the copies of the s-th stage start. The k that no whole stage has are one more; a row ends inside it, and
