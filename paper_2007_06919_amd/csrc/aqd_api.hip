@@ -1797,7 +1797,7 @@ bool aligned_to(const void *p, int size) { return ((uintptr_t)p & (uintptr_t)(si
 // strides: none below the columns, and the matrix inside the address space
 bool stride_ok(int64_t ld, int rows, int cols)
 {
-    return ld >= cols && (rows <= 1 || ld <= (INT64_C(1) << 56) / rows);
+    return ld >= cols && ld <= (INT64_C(1) << 56) / std::max(rows, 1);
 }
 
 aqd_status_t rows_call(RowsArgs &a, int rows, hipStream_t stream)

@@ -111,3 +111,12 @@ def test_real_types():
     assert aqd.real_type(torch.float16) == aqd.F16
     with pytest.raises(TypeError):
         aqd.real_type(torch.empty(0, dtype=torch.int8))
+
+
+@pytest.mark.parametrize("call, bad", [
+    (rows_call, dict(ld_x=1 << 62)), (rows_call, dict(ld_codes=1 << 60)), (norm_call, dict(ld_x=1 << 61, ld_sum=1 << 61, sum=A + 8)),
+    (norm_call, dict(type=aqd.F32, ld_x=1 << 62, ld_sum=1 << 62, sum=A + 64)), (lin_call, dict(ld_x=1 << 62)), (lin_call, dict(ld_y=1 << 62)),
+])
+def test_a_single_row_has_a_bounded_stride_too(call, bad):
+    """2^62 elements of 4 bytes are 0 bytes in 64 bits, which no overlap check may divide by."""
+    refused(call, rows=1, **bad)
