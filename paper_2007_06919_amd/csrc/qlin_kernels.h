@@ -292,6 +292,9 @@ __global__ void __launch_bounds__(256) qlin_any_kernel(QlinArgs A, long long til
     }
 }
 
+// one of n < 2^16 places for workgroup `id`, evenly and neighbours far apart: fractions of the golden ratio
+__device__ __forceinline__ int scattered(unsigned id, int n) { return (int)((id * 0x9E3779B1u >> 16) * (unsigned)n >> 16); }
+
 // ---- small launches: both operands straight into registers ----------------------------
 // One workgroup per 16 outputs and 16 NB tokens, its waves splitting k, 64 at a time, and adding
 // their sums in LDS: no LDS and no barrier in the loop, and the shortest chain from launch to
@@ -320,7 +323,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) qlin_few_kernel(QlinArgs A)
         vx[b] = (uint32_t)(t < most ? t : most) * (uint32_t)A.ld_x + 16 * fc;
     }
     const int steps = A.k / 64, from = (int)((long long)steps * wave / FEW_WAVES), to = (int)((long long)steps * (wave + 1) / FEW_WAVES);
-    const int start = gridDim.y == 1 && to > from ? (int)(blockIdx.x % (unsigned)(to - from)) : 0;   // as in qlin_tile_kernel
+    const int start = gridDim.y == 1 && to > from ? scattered(blockIdx.x, to - from) : 0;   // as in qlin_tile_kernel
     v4i acc[H][NB] = {};
     Words a[2][U][H], b[2][U][NB];
     int shift_w[2], shift_x[NB];   // of a lane's rows (their 16-byte pieces are 16 apart: the same for all)
@@ -683,9 +686,10 @@ qlin_tile_kernel(QlinArgs A, unsigned tile0, unsigned total)   // (waves per SIM
     const int stages = (k1 - k0) / KS, last = stages - 1, rest = k0 + KS * stages;   // rest: the k that no whole stage has
     // Where this workgroup starts: a sum's terms have no order. With rows of a power of two of bytes, workgroups that
     // all read the same columns meet on a few memory channels. Where each row of w is read by one of them
-    // (one token tile) all start apart (16 x 16384 x 4096 gated 34.3 -> 30.1 us); of many token tiles each eighth
+    // (one token tile) all start apart (16 x 16384 x 4096 gated all at 0 34.3 us, each a stage after the last 30.1,
+    // scattered 26.5; 32 x 8192 x 4096 gated 15.3 by stages, 15.9 scattered, the worst found); of many token tiles each eighth
     // does, whose workgroups share their reads (2048 x 11264 x 4096 gated 186 -> 180 us, 8192 x 8192 x 8192 the same).
-    const int start = !stages ? 0 : tiles_t == 1 ? at.tn % stages : (int)((long long)stages * at.eighth / 8);
+    const int start = !stages ? 0 : tiles_t == 1 ? scattered(tile0 + blockIdx.x, stages) : (int)((long long)stages * at.eighth / 8);
     auto turned = [&](int s) { return s + start < stages ? s + start : s + start - stages; };
     // Where the copies of the s-th stage start. The k that no whole stage has are one more; a row ends inside it, and
     // a lane whose 16 bytes would pass the row's last word takes the 16 bytes up to there (load16 does the same).
