@@ -300,7 +300,7 @@ __device__ __forceinline__ int scattered(unsigned id, int n) { return (int)((id 
 // their sums in LDS: no LDS and no barrier in the loop, and the shortest chain from launch to
 // store. Rows start at any byte, their 16 (tokens: 16 NB) within 32 bits of offset.
 // Bound by the launch and the first loads' latency (77 x 1003 x 515 packed 6.2 us), then by the
-// weights' stream (1 x 4096 x 4096 6.6 us, 16.8 MB; at most 4.1 TB/s, where the tiles below reach 4.5).
+// weights' stream (1 x 4096 x 4096 6.6 us, 16.8 MB; at most 4.1 TB/s, where the tiles below reach 5.1).
 constexpr int FEW_WAVES = 4;
 
 template <typename T, bool GATE, bool BYTES, int NB, int U>
