@@ -299,8 +299,8 @@ __device__ __forceinline__ int scattered(unsigned id, int n) { return (int)((id 
 // One workgroup per 16 outputs and 16 NB tokens, its waves splitting k, 64 at a time, and adding
 // their sums in LDS: no LDS and no barrier in the loop, and the shortest chain from launch to
 // store. Rows start at any byte, their 16 (tokens: 16 NB) within 32 bits of offset.
-// Bound by the launch and the first loads' latency (77 x 1003 x 515 packed 6.2 us), then by the
-// weights' stream (1 x 4096 x 4096 6.6 us, 16.8 MB; at most 4.1 TB/s, where the tiles below reach 5.1).
+// Bound by the launch and the first loads' latency (77 x 1003 x 514 at odd bytes 5.2 us), then by the
+// weights' stream (1 x 4096 x 4096 5.4 to 6.2 us, 16.8 MB; at most 4.1 TB/s, where the tiles below reach 5.1).
 constexpr int FEW_WAVES = 4;
 
 template <typename T, bool GATE, bool BYTES, int NB, int U>
@@ -349,8 +349,8 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) qlin_few_kernel(QlinArgs A)
             fb[i] = shifted<BYTES>(wb[i], shift_x[i]);
         mfma(fa, fb);
     };
-    // two sets of U steps in turn: one in flight, one in the MFMAs; loads past the range read its last step
-    // again and are not used
+    // two sets of U steps in turn: one in flight, one in the MFMAs; in a set, loads past the range read its last step
+    // again and are not used (with a whole set of those at the end 1 x 6144 x 4096 8.5 us, without 7.6)
     if (int s = from; s < to) {
         auto fill = [&](int set, int s) {
 #pragma unroll
@@ -379,12 +379,14 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) qlin_few_kernel(QlinArgs A)
         };
         fill(0, s);
         for (;;) {
-            fill(1, s + U);
+            if (s + U < to)
+                fill(1, s + U);
             use(0, s);
             s += U;
             if (s >= to)
                 break;
-            fill(0, s + U);
+            if (s + U < to)
+                fill(0, s + U);
             use(1, s);
             s += U;
             if (s >= to)
