@@ -54,9 +54,12 @@ class GatedFfn:
         def codes(cols):
             return torch.empty(max_rows, -(-cols // 16) * 16, dtype=torch.int8, device=dev)
 
-        self.c1, self.q1 = codes(hidden), torch.empty(max_rows, device=dev)
+        def scales():   # fp32 whatever torch's default type
+            return torch.empty(max_rows, dtype=torch.float32, device=dev)
+
+        self.c1, self.q1 = codes(hidden), scales()
         self.h = torch.empty(max_rows, units, dtype=self.dtype, device=dev)
-        self.c2, self.q2 = codes(units), torch.empty(max_rows, device=dev)
+        self.c2, self.q2 = codes(units), scales()
         # the bound serves every call; the block's launches follow one another on one stream
         self.workspace = torch.empty(aqd.QLIN_WORKSPACE_BYTES, dtype=torch.uint8, device=dev)
         self._graph = None

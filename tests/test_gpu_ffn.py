@@ -83,3 +83,28 @@ def test_refusals():
     wider = randn(5, 64)
     with pytest.raises(aqd.AqdError):   # total is x, shifted by one element
         f.forward(wider[:4], x, x.clone(), wider.view(-1)[1:257].view(4, 64))
+
+
+def test_under_a_16_bit_default_type():
+    """torch's default type may be 16 bits wide, as in language-model programs: the block's scales stay fp32."""
+    import torch
+    rows, hidden, units = 40, 512, 1000
+    outs = []
+    for default in (torch.float32, torch.bfloat16):
+        torch.set_default_dtype(default)
+        try:
+            g = torch.Generator(device="cuda").manual_seed(1)
+            w = [torch.randn(*s, generator=g, device="cuda", dtype=torch.float32).bfloat16() / 16
+                 for s in ((hidden,), (units, hidden), (units, hidden), (hidden, units))]
+            x = torch.randn(2, rows, hidden, generator=g, device="cuda", dtype=torch.float32).bfloat16()
+            f = ffn.GatedFfn(*w, max_rows=rows)
+            assert f.q1.dtype == f.q2.dtype == torch.float32
+            y, total = torch.empty_like(x[0]), torch.empty_like(x[0])
+            f.forward(x[0], x[1], y, total)
+            torch.cuda.synchronize()
+        finally:
+            torch.set_default_dtype(torch.float32)
+        outs.append((y, total, f.q1.clone(), f.q2.clone()))
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+    assert outs[0][0].ne(0).any()
