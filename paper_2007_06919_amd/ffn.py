@@ -23,6 +23,11 @@ import sys
 from . import aqd
 
 
+def _ld(t):
+    """Row stride of a [rows][cols] tensor for the library, which takes 0 for packed rows; a single row has none."""
+    return t.stride(0) if t.shape[0] > 1 else 0
+
+
 def quantize_rows(w, stream=None):
     """(codes, scales) of a real matrix, one scale per row; rows of codes start at multiples of 16 bytes."""
     import torch
@@ -65,22 +70,24 @@ class GatedFfn:
         self._graph = None
 
     def forward(self, x, residual, y, total, stream=None):
-        """y = block(norm(x + residual)), total = x + residual; all [rows][hidden] with contiguous rows. total may be
-        residual. On one stream at a time."""
+        """y = block(norm(x + residual)), total = x + residual; all [rows][hidden] with contiguous rows that share no
+        element (no expanded tensors). total may be residual. On one stream at a time."""
         rows = x.shape[0]
         if rows > self.max_rows:
             raise ValueError(f"{rows} rows, and buffers for {self.max_rows}")
         for t in (x, residual, y, total):
             if t.shape != (rows, self.hidden) or t.dtype != self.dtype or t.stride(1) != 1:
                 raise ValueError(f"tensors must be [{rows}][{self.hidden}] {self.dtype} with contiguous rows")
+            if rows > 1 and t.stride(0) < self.hidden:
+                raise ValueError(f"rows of a tensor share memory: {self.hidden} columns, stride {t.stride(0)}")
         ws = self.workspace
-        aqd.qnorm_run(rows, self.hidden, self.type, self.eps, x, x.stride(0), residual, residual.stride(0), self.norm_weight,
-                      total, total.stride(0), self.c1, self.c1.stride(0), self.q1, stream)
+        aqd.qnorm_run(rows, self.hidden, self.type, self.eps, x, _ld(x), residual, _ld(residual), self.norm_weight,
+                      total, _ld(total), self.c1, self.c1.stride(0), self.q1, stream)
         aqd.qlin_run(rows, self.units, self.hidden, self.type, aqd.QLIN_SILU_GATE, self.c1, self.c1.stride(0), self.q1, self.w1,
                      self.w1.stride(0), self.s1, None, self.h, self.units, ws, ws.numel(), stream)
         aqd.qrows_run(rows, self.units, self.type, self.h, self.units, self.c2, self.c2.stride(0), self.q2, stream)
         aqd.qlin_run(rows, self.hidden, self.units, self.type, aqd.QLIN_PLAIN, self.c2, self.c2.stride(0), self.q2, self.w2,
-                     self.w2.stride(0), self.s2, None, y, y.stride(0), ws, ws.numel(), stream)
+                     self.w2.stride(0), self.s2, None, y, _ld(y), ws, ws.numel(), stream)
         return y
 
     def capture(self, x, residual, y, total, stream):

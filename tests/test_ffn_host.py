@@ -36,3 +36,33 @@ def test_scales_have_32_bits_whatever_the_default_type(calls, default):
     for q in (f.q1, f.q2, f.s1, f.s2):
         assert q.dtype == torch.float32
     assert f.q1.shape == f.q2.shape == (ROWS,)
+
+
+def test_rows_that_share_memory_are_refused(calls):
+    """A stride of 0 (an expanded row) means packed rows to the library, which would read past such a tensor, or write."""
+    f = ffn.GatedFfn(*weights(), max_rows=ROWS)
+    row = torch.zeros(1, HIDDEN, dtype=torch.bfloat16).expand(ROWS, HIDDEN)
+    sliding = torch.zeros(HIDDEN + ROWS, dtype=torch.bfloat16).as_strided((ROWS, HIDDEN), (1, 1))
+    del calls[:]
+    for bad in (row, sliding):
+        for at in range(4):
+            tensors = [rows_of() for _ in range(4)]
+            tensors[at] = bad
+            with pytest.raises(ValueError):
+                f.forward(*tensors)
+    assert not calls
+
+
+def test_row_strides_reach_the_library(calls):
+    f = ffn.GatedFfn(*weights(), max_rows=ROWS)
+    x, residual, y, total = (torch.zeros(ROWS, HIDDEN + 8 * i, dtype=torch.bfloat16)[:, :HIDDEN] for i in range(4))
+    del calls[:]
+    f.forward(x, residual, y, total)
+    norm, _, _, last = [a for _, a in calls]
+    assert (norm[5], norm[7], norm[10]) == (HIDDEN, HIDDEN + 8, HIDDEN + 24) and last[13] == HIDDEN + 16
+    # a single row has no stride: torch gives any, as here 1
+    del calls[:]
+    one = torch.zeros(HIDDEN, 1, dtype=torch.bfloat16).t()
+    assert one.stride(0) == 1
+    f.forward(one, one.clone(), rows_of(1), rows_of(1))
+    assert calls[0][1][5] in (0, HIDDEN)
