@@ -24,8 +24,8 @@ from . import aqd
 
 
 def _ld(t):
-    """Row stride of a [rows][cols] tensor for the library, which takes 0 for packed rows; a single row has none."""
-    return t.stride(0) if t.shape[0] > 1 else 0
+    """Row stride of a [rows][cols] tensor for the library, which takes 0 for packed rows; a single row has none, nor has None."""
+    return t.stride(0) if t is not None and t.shape[0] > 1 else 0
 
 
 def quantize_rows(w, stream=None):
@@ -71,11 +71,12 @@ class GatedFfn:
 
     def forward(self, x, residual, y, total, stream=None):
         """y = block(norm(x + residual)), total = x + residual; all [rows][hidden] with contiguous rows that share no
-        element (no expanded tensors). total may be residual. On one stream at a time."""
+        element (no expanded tensors). residual and total may be None (the first block of a network has no residual); total
+        may be residual. On one stream at a time."""
         rows = x.shape[0]
         if rows > self.max_rows:
             raise ValueError(f"{rows} rows, and buffers for {self.max_rows}")
-        for t in (x, residual, y, total):
+        for t in (x, y, *(t for t in (residual, total) if t is not None)):
             if t.shape != (rows, self.hidden) or t.dtype != self.dtype or t.stride(1) != 1:
                 raise ValueError(f"tensors must be [{rows}][{self.hidden}] {self.dtype} with contiguous rows")
             if rows > 1 and t.stride(0) < self.hidden:

@@ -66,3 +66,13 @@ def test_row_strides_reach_the_library(calls):
     assert one.stride(0) == 1
     f.forward(one, one.clone(), rows_of(1), rows_of(1))
     assert calls[0][1][5] in (0, HIDDEN)
+
+
+def test_the_first_block_has_no_residual(calls):
+    f = ffn.GatedFfn(*weights(), max_rows=ROWS)
+    del calls[:]
+    f.forward(rows_of(), None, rows_of(), rows_of())
+    assert calls[0][0] == "qnorm_run" and calls[0][1][6] is None and calls[0][1][9] is not None
+    del calls[:]
+    f.forward(rows_of(), None, rows_of(), None)
+    assert calls[0][1][6] is None and calls[0][1][9] is None

@@ -108,3 +108,18 @@ def test_under_a_16_bit_default_type():
     for a, b in zip(*outs):
         assert torch.equal(a, b)
     assert outs[0][0].ne(0).any()
+
+
+def test_without_a_residual():
+    """The first block of a network: the same as a residual of zeros, with the sum asked for and without."""
+    import torch
+    rows, hidden = 7, 256
+    f, _, randn = block(torch, hidden, 640, rows)
+    x = randn(rows, hidden)
+    y, total = [torch.empty_like(x) for _ in range(3)], [torch.empty_like(x) for _ in range(2)]
+    f.forward(x, torch.zeros_like(x), y[0], total[0])
+    f.forward(x, None, y[1], total[1])
+    f.forward(x, None, y[2], None)
+    torch.cuda.synchronize()
+    assert torch.equal(y[0], y[1]) and torch.equal(y[0], y[2]) and y[0].ne(0).any()
+    assert torch.equal(total[0], x) and torch.equal(total[1], x)
