@@ -28,6 +28,19 @@ def _ld(t):
     return t.stride(0) if t is not None and t.shape[0] > 1 else 0
 
 
+def _meet(a, b):
+    """Whether two [rows][cols] tensors of one type may share an element (column ranges of one buffer do not)."""
+    size, cols = a.element_size(), a.shape[1]
+    pa, pb = a.data_ptr(), b.data_ptr()
+    ea, eb = (p + size * ((t.shape[0] - 1) * _ld(t) + cols) for p, t in ((pa, a), (pb, b)))
+    if not a.shape[0] or pa >= eb or pb >= ea:
+        return False
+    if a.shape[0] == 1 or _ld(a) != _ld(b):
+        return True
+    d = (pb - pa) // size % _ld(a)
+    return d < cols or d + cols > _ld(a)
+
+
 def quantize_rows(w, stream=None):
     """(codes, scales) of a real matrix, one scale per row; rows of codes start at multiples of 16 bytes."""
     import torch
@@ -72,7 +85,7 @@ class GatedFfn:
     def forward(self, x, residual, y, total, stream=None):
         """y = block(norm(x + residual)), total = x + residual; all [rows][hidden] with contiguous rows that share no
         element (no expanded tensors). residual and total may be None (the first block of a network has no residual); total
-        may be residual. On one stream at a time."""
+        may be residual, and y may be x or residual, but not share an element with total. On one stream at a time."""
         rows = x.shape[0]
         if rows > self.max_rows:
             raise ValueError(f"{rows} rows, and buffers for {self.max_rows}")
@@ -81,6 +94,8 @@ class GatedFfn:
                 raise ValueError(f"tensors must be [{rows}][{self.hidden}] {self.dtype} with contiguous rows")
             if rows > 1 and t.stride(0) < self.hidden:
                 raise ValueError(f"rows of a tensor share memory: {self.hidden} columns, stride {t.stride(0)}")
+        if total is not None and _meet(y, total):
+            raise ValueError("y and total share memory")
         ws = self.workspace
         aqd.qnorm_run(rows, self.hidden, self.type, self.eps, x, _ld(x), residual, _ld(residual), self.norm_weight,
                       total, _ld(total), self.c1, self.c1.stride(0), self.q1, stream)

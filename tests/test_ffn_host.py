@@ -76,3 +76,21 @@ def test_the_first_block_has_no_residual(calls):
     del calls[:]
     f.forward(rows_of(), None, rows_of(), None)
     assert calls[0][1][6] is None and calls[0][1][9] is None
+
+
+def test_outputs_apart(calls):
+    """y is written last: over total it would leave no sum."""
+    f = ffn.GatedFfn(*weights(), max_rows=ROWS)
+    both = torch.zeros(ROWS, 2 * HIDDEN, dtype=torch.bfloat16)
+    buf = torch.zeros((ROWS + 1) * HIDDEN, dtype=torch.bfloat16)
+    del calls[:]
+    y = rows_of()
+    for y, total in ((y, y), (buf[:ROWS * HIDDEN].view(ROWS, HIDDEN), buf[HIDDEN:].view(ROWS, HIDDEN)),
+                     (both[:, :HIDDEN], both[:, 8:HIDDEN + 8])):
+        with pytest.raises(ValueError):
+            f.forward(rows_of(), rows_of(), y, total)
+    assert not calls
+    f.forward(rows_of(), rows_of(), both[:, :HIDDEN], both[:, HIDDEN:])   # two column ranges of one buffer
+    x = rows_of()
+    f.forward(x, rows_of(), x, rows_of())                                # y over x, which is read by then
+    assert len(calls) == 8
