@@ -52,7 +52,8 @@ def quantize_rows(w, stream=None):
 
 
 class GatedFfn:
-    """norm_weight [hidden], gate and up [units][hidden], down [hidden][units]: device tensors of one real type."""
+    """norm_weight [hidden], gate and up [units][hidden], down [hidden][units]: device tensors of one real type, that of
+    the block's inputs and outputs too."""
 
     def __init__(self, norm_weight, gate, up, down, eps=1e-5, max_rows=4096):
         import torch
@@ -60,6 +61,8 @@ class GatedFfn:
         if up.shape != gate.shape or down.shape != (hidden, units) or norm_weight.shape != (hidden,):
             raise ValueError(f"shapes do not make a block: norm {tuple(norm_weight.shape)}, gate {tuple(gate.shape)}, "
                              f"up {tuple(up.shape)}, down {tuple(down.shape)}")
+        if not norm_weight.dtype == gate.dtype == up.dtype == down.dtype:
+            raise ValueError(f"one type for all: norm {norm_weight.dtype}, gate {gate.dtype}, up {up.dtype}, down {down.dtype}")
         if max_rows < 1:
             raise ValueError("max_rows must be at least 1")
         self.hidden, self.units, self.eps, self.max_rows = hidden, units, float(eps), max_rows

@@ -10,7 +10,8 @@ HIDDEN, UNITS, ROWS = 64, 96, 4
 
 @pytest.fixture
 def calls(monkeypatch):
-    """The library's calls in order, as (name, arguments)."""
+    """The library's calls in order, as (name, arguments); tensors of the host pass for tensors of the GPU."""
+    monkeypatch.setattr(ffn, "DEVICE", "cpu", raising=False)
     made = []
     for name in ("qrows_run", "qnorm_run", "qlin_run"):
         monkeypatch.setattr(aqd, name, lambda *a, _name=name, **kw: made.append((_name, a)))
@@ -94,3 +95,17 @@ def test_outputs_apart(calls):
     x = rows_of()
     f.forward(x, rows_of(), x, rows_of())                                # y over x, which is read by then
     assert len(calls) == 8
+
+
+def test_one_type(calls):
+    """Every tensor is read as the type of the block: a norm weight in fp32 beside matrices in bf16 is refused, not misread."""
+    for at in range(4):
+        w = list(weights())
+        w[at] = w[at].float()
+        with pytest.raises(ValueError):
+            ffn.GatedFfn(*w)
+    with pytest.raises((ValueError, TypeError)):
+        ffn.GatedFfn(*weights(torch.float64))
+    assert not calls
+    for dtype in (torch.float32, torch.float16, torch.bfloat16):
+        ffn.GatedFfn(*weights(dtype), max_rows=1)
