@@ -22,6 +22,8 @@ import sys
 
 from . import aqd
 
+DEVICE = "cuda"   # where the library's kernels run: no other address may reach them
+
 
 def _ld(t):
     """Row stride of a [rows][cols] tensor for the library, which takes 0 for packed rows; a single row has none, nor has None."""
@@ -44,6 +46,11 @@ def _meet(a, b):
 def quantize_rows(w, stream=None):
     """(codes, scales) of a real matrix, one scale per row; rows of codes start at multiples of 16 bytes."""
     import torch
+    if w.device.type != DEVICE:
+        raise ValueError(f"the matrix is on {w.device}, not on the GPU")
+    if w.device.index is not None and w.device.index != torch.cuda.current_device():
+        with torch.cuda.device(w.device.index):
+            return quantize_rows(w, stream)
     rows, cols = w.shape
     codes = torch.zeros(rows, -(-cols // 16) * 16, dtype=torch.int8, device=w.device)[:, :cols]
     scales = torch.empty(rows, dtype=torch.float32, device=w.device)
@@ -63,6 +70,9 @@ class GatedFfn:
                              f"up {tuple(up.shape)}, down {tuple(down.shape)}")
         if not norm_weight.dtype == gate.dtype == up.dtype == down.dtype:
             raise ValueError(f"one type for all: norm {norm_weight.dtype}, gate {gate.dtype}, up {up.dtype}, down {down.dtype}")
+        if gate.device.type != DEVICE or not norm_weight.device == gate.device == up.device == down.device:
+            raise ValueError(f"one GPU for all: norm on {norm_weight.device}, gate on {gate.device}, up on {up.device}, "
+                             f"down on {down.device}")
         if max_rows < 1:
             raise ValueError("max_rows must be at least 1")
         self.hidden, self.units, self.eps, self.max_rows = hidden, units, float(eps), max_rows
@@ -70,7 +80,8 @@ class GatedFfn:
         self.norm_weight = norm_weight.contiguous()
         self.w1, self.s1 = quantize_rows(torch.cat([gate, up]))
         self.w2, self.s2 = quantize_rows(down)
-        dev = gate.device
+        dev = self.device = gate.device
+        self.index = dev.index
 
         def codes(cols):
             return torch.empty(max_rows, -(-cols // 16) * 16, dtype=torch.int8, device=dev)
@@ -89,12 +100,16 @@ class GatedFfn:
         """y = block(norm(x + residual)), total = x + residual; all [rows][hidden] with contiguous rows that share no
         element (no expanded tensors). residual and total may be None (the first block of a network has no residual); total
         may be residual, and y may be x or residual, but not share an element with total. On one stream at a time."""
+        import torch
+        if self.index is not None and self.index != torch.cuda.current_device():
+            with torch.cuda.device(self.index):
+                return self.forward(x, residual, y, total, stream)
         rows = x.shape[0]
         if rows > self.max_rows:
             raise ValueError(f"{rows} rows, and buffers for {self.max_rows}")
         for t in (x, y, *(t for t in (residual, total) if t is not None)):
-            if t.shape != (rows, self.hidden) or t.dtype != self.dtype or t.stride(1) != 1:
-                raise ValueError(f"tensors must be [{rows}][{self.hidden}] {self.dtype} with contiguous rows")
+            if t.shape != (rows, self.hidden) or t.dtype != self.dtype or t.stride(1) != 1 or t.device != self.device:
+                raise ValueError(f"tensors must be [{rows}][{self.hidden}] {self.dtype} with contiguous rows on {self.device}")
             if rows > 1 and t.stride(0) < self.hidden:
                 raise ValueError(f"rows of a tensor share memory: {self.hidden} columns, stride {t.stride(0)}")
         if total is not None and _meet(y, total):
@@ -119,6 +134,10 @@ class GatedFfn:
             self._graph = aqd.graph_end(stream)
 
     def replay(self, stream):
+        import torch
+        if self.index is not None and self.index != torch.cuda.current_device():
+            with torch.cuda.device(self.index):
+                return self.replay(stream)
         aqd.graph_launch(self._graph, stream)
 
     def close(self):

@@ -109,3 +109,53 @@ def test_one_type(calls):
     assert not calls
     for dtype in (torch.float32, torch.float16, torch.bfloat16):
         ffn.GatedFfn(*weights(dtype), max_rows=1)
+
+
+def test_one_device(calls, monkeypatch):
+    """A host address must not reach a kernel, nor one of another device. ("meta" stands for the other device.)"""
+    for at in range(4):
+        w = list(weights())
+        w[at] = w[at].to("meta")
+        with pytest.raises(ValueError):
+            ffn.GatedFfn(*w)
+    f = ffn.GatedFfn(*weights(), max_rows=ROWS)
+    del calls[:]
+    for at in range(4):
+        tensors = [rows_of() for _ in range(4)]
+        tensors[at] = tensors[at].to("meta")
+        with pytest.raises(ValueError):
+            f.forward(*tensors)
+    monkeypatch.setattr(ffn, "DEVICE", "cuda")
+    for make in (lambda: ffn.GatedFfn(*weights()), lambda: ffn.quantize_rows(weights()[1])):   # on the host
+        with pytest.raises(ValueError):
+            make()
+    assert not calls
+
+
+def test_work_goes_to_the_tensors_device(calls, monkeypatch):
+    """A launch without a stream goes to the current device, which has to be the tensors'."""
+    f = ffn.GatedFfn(*weights(), max_rows=ROWS)
+    now, seen = [0], []
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+
+    class On:
+        def __init__(self, device):
+            self.to = torch.device(device).index if not isinstance(device, int) else device
+
+        def __enter__(self):
+            self.was, now[0] = now[0], self.to
+
+        def __exit__(self, *_):
+            now[0] = self.was
+
+    monkeypatch.setattr(torch.cuda, "device", On)
+    monkeypatch.setattr(aqd, "qnorm_run", lambda *a: seen.append(now[0]))
+    monkeypatch.setattr(aqd, "graph_launch", lambda *a: seen.append(now[0]))
+    for index, want in ((0, 0), (1, 1)):
+        f.index = index
+        f.forward(*(rows_of() for _ in range(4)))
+        f._graph = 1
+        f.replay(5)
+        f._graph = None
+        assert seen == [want, want] and now[0] == 0
+        del seen[:]
