@@ -52,9 +52,11 @@ def quantize_rows(w, stream=None):
         with torch.cuda.device(w.device.index):
             return quantize_rows(w, stream)
     rows, cols = w.shape
+    if w.stride(1) != 1 or rows > 1 and w.stride(0) < cols:
+        w = w.contiguous()
     codes = torch.zeros(rows, -(-cols // 16) * 16, dtype=torch.int8, device=w.device)[:, :cols]
     scales = torch.empty(rows, dtype=torch.float32, device=w.device)
-    aqd.qrows_run(rows, cols, aqd.real_type(w), w, w.stride(0), codes, codes.stride(0), scales, stream)
+    aqd.qrows_run(rows, cols, aqd.real_type(w), w, _ld(w), codes, codes.stride(0), scales, stream)
     return codes, scales
 
 

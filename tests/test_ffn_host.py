@@ -159,3 +159,22 @@ def test_work_goes_to_the_tensors_device(calls, monkeypatch):
         f._graph = None
         assert seen == [want, want] and now[0] == 0
         del seen[:]
+
+
+def test_matrices_of_any_strides_are_quantised_as_they_are(calls, monkeypatch):
+    """What the library reads, at the stride it is given, is the matrix: columns apart, transposed, expanded, a single row."""
+    got = []
+
+    def read(rows, cols, kind, x, ld, codes, ld_codes, scales, stream=None):
+        got.append(torch.as_strided(x, (rows, cols), (ld or cols, 1), x.storage_offset()).clone())
+
+    monkeypatch.setattr(aqd, "qrows_run", read)
+    wide = torch.arange(12 * 40, dtype=torch.float32).view(12, 40)
+    for m in (wide, wide[:, ::2], wide.t(), wide[:, 3:30], wide[:1].expand(5, 40), wide[:1, ::3], wide[:, :1], wide[:, :1].t(),
+              wide[::2], wide[:0]):
+        codes, scales = ffn.quantize_rows(m)
+        assert torch.equal(got.pop(), m) and codes.shape == m.shape and scales.shape == m.shape[:1]
+        assert codes.stride(1) == 1 and codes.stride(0) % 16 == 0
+    for bad in (wide[0], wide.view(3, 4, 40)):
+        with pytest.raises(ValueError):
+            ffn.quantize_rows(bad)

@@ -123,3 +123,15 @@ def test_without_a_residual():
     torch.cuda.synchronize()
     assert torch.equal(y[0], y[1]) and torch.equal(y[0], y[2]) and y[0].ne(0).any()
     assert torch.equal(total[0], x) and torch.equal(total[1], x)
+
+
+def test_matrices_of_any_strides():
+    """Weights handed over as transposed, sliced or expanded views give the codes of their packed copies."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(3)
+    wide = torch.randn(48, 96, generator=g, device="cuda")
+    for m in (wide, wide[:, ::2], wide.t(), wide[:1].expand(5, 96), wide[:1, ::3], wide[:, 3:30]):
+        codes, scales = ffn.quantize_rows(m)
+        want, want_scales = ffn.quantize_rows(m.clone(memory_format=torch.contiguous_format))
+        assert torch.equal(codes, want) and torch.equal(scales, want_scales) and codes.shape == m.shape
+        assert bool(((codes * scales[:, None] - m).abs() <= 0.51 * scales[:, None]).all())
