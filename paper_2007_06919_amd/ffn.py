@@ -44,7 +44,8 @@ def _meet(a, b):
 
 
 def quantize_rows(w, stream=None):
-    """(codes, scales) of a real matrix, one scale per row; rows of codes start at multiples of 16 bytes."""
+    """(codes, scales) of a real matrix, one scale per row; rows of codes start at multiples of 16 bytes. On `stream`
+    (None: the current one) in order with the current stream: after the work that it has, before what it gets next."""
     import torch
     if w.device.type != DEVICE:
         raise ValueError(f"the matrix is on {w.device}, not on the GPU")
@@ -54,9 +55,15 @@ def quantize_rows(w, stream=None):
     rows, cols = w.shape
     if w.stride(1) != 1 or rows > 1 and w.stride(0) < cols:
         w = w.contiguous()
-    codes = torch.zeros(rows, -(-cols // 16) * 16, dtype=torch.int8, device=w.device)[:, :cols]
+    codes = torch.empty(rows, -(-cols // 16) * 16, dtype=torch.int8, device=w.device)[:, :cols]
     scales = torch.empty(rows, dtype=torch.float32, device=w.device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream)
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
     aqd.qrows_run(rows, cols, aqd.real_type(w), w, _ld(w), codes, codes.stride(0), scales, stream)
+    if stream is not None:
+        torch.cuda.current_stream().wait_stream(stream)
     return codes, scales
 
 

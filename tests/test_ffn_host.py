@@ -178,3 +178,27 @@ def test_matrices_of_any_strides_are_quantised_as_they_are(calls, monkeypatch):
     for bad in (wide[0], wide.view(3, 4, 40)):
         with pytest.raises(ValueError):
             ffn.quantize_rows(bad)
+
+
+def test_quantising_on_another_stream_is_in_order(calls, monkeypatch):
+    """torch's work on the current stream (the matrix, what the new tensors' memory held before) comes before the
+    kernel on `stream`, and the kernel before what follows on the current stream."""
+    class Stream:
+        cuda_stream = 77
+
+        def __init__(self, name):
+            self.name = name
+
+        def wait_stream(self, other):
+            calls.append(("wait", (self.name, other.name)))
+
+    here, other = Stream("here"), Stream("other")
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: here)
+    filled = []
+    monkeypatch.setattr(torch, "zeros", lambda *a, **kw: filled.append(a))   # a fill would be on the current stream
+    ffn.quantize_rows(weights()[1], other)
+    assert not filled and [c if c[0] == "wait" else c[0] for c in calls] == \
+        [("wait", ("other", "here")), "qrows_run", ("wait", ("here", "other"))]
+    del calls[:]
+    ffn.quantize_rows(weights()[1])
+    assert [c[0] for c in calls] == ["qrows_run"]

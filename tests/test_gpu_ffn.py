@@ -135,3 +135,18 @@ def test_matrices_of_any_strides():
         want, want_scales = ffn.quantize_rows(m.clone(memory_format=torch.contiguous_format))
         assert torch.equal(codes, want) and torch.equal(scales, want_scales) and codes.shape == m.shape
         assert bool(((codes * scales[:, None] - m).abs() <= 0.51 * scales[:, None]).all())
+
+
+def test_quantising_on_another_stream():
+    """In order with the current stream on both sides, for a stream object and for its handle."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(6)
+    w = torch.randn(2000, 1003, generator=g, device="cuda")
+    want = ffn.quantize_rows(w)
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        fresh = w * 2 / 2   # on the current stream, not waited for
+        codes, scales = ffn.quantize_rows(fresh, stream)
+        got = codes.clone(), scales.clone()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
