@@ -58,7 +58,7 @@ def quantize_rows(w, stream=None):
     codes = torch.empty(rows, -(-cols // 16) * 16, dtype=torch.int8, device=w.device)[:, :cols]
     scales = torch.empty(rows, dtype=torch.float32, device=w.device)
     if isinstance(stream, int):
-        stream = torch.cuda.ExternalStream(stream)
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
     if stream is not None:
         stream.wait_stream(torch.cuda.current_stream())
     aqd.qrows_run(rows, cols, aqd.real_type(w), w, _ld(w), codes, codes.stride(0), scales, stream)

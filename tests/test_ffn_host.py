@@ -202,3 +202,20 @@ def test_quantising_on_another_stream_is_in_order(calls, monkeypatch):
     del calls[:]
     ffn.quantize_rows(weights()[1])
     assert [c[0] for c in calls] == ["qrows_run"]
+
+
+def test_the_null_streams_handle(calls, monkeypatch):
+    """Handle 0 is the default stream; torch.cuda.ExternalStream(0) would be one of torch's own streams instead."""
+    waits = []
+
+    class Stream:
+        cuda_stream = 0
+
+        def wait_stream(self, other):
+            waits.append((self, other))
+
+    default, here = Stream(), Stream()
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda *a: default)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: here)
+    ffn.quantize_rows(weights()[1], 0)
+    assert waits == [(default, here), (here, default)] and calls[0][1][-1] is default
