@@ -67,9 +67,16 @@ def quantize_rows(w, stream=None):
     return codes, scales
 
 
+def _finish(device):
+    import torch
+    torch.cuda.current_stream(device).synchronize()
+
+
 class GatedFfn:
     """norm_weight [hidden], gate and up [units][hidden], down [hidden][units]: device tensors of one real type, that of
-    the block's inputs and outputs too."""
+    the block's inputs and outputs too. The set-up has ended on the GPU when the constructor returns, so passes may run on any
+    stream, one at a time. Before a block that ran on a stream given by its handle is dropped, that stream is waited for; those
+    given as torch's streams, or current, torch waits for itself before it gives the block's memory to others."""
 
     def __init__(self, norm_weight, gate, up, down, eps=1e-5, max_rows=4096):
         import torch
@@ -104,11 +111,29 @@ class GatedFfn:
         # the bound serves every call; the block's launches follow one another on one stream
         self.workspace = torch.empty(aqd.QLIN_WORKSPACE_BYTES, dtype=torch.uint8, device=dev)
         self._graph = None
+        self._buffers = (self.norm_weight, self.w1, self.s1, self.w2, self.s2, self.c1, self.q1, self.h, self.c2, self.q2,
+                         self.workspace)
+        self._streams = {aqd._stream(None)}   # handles of those that torch keeps the buffers for
+        _finish(dev)
+
+    def _use_on(self, stream):
+        """The handle of `stream` (None: the current one), for which torch keeps the buffers from now on."""
+        import torch
+        handle = aqd._stream(stream)
+        if handle not in self._streams:
+            if stream is None:
+                stream = torch.cuda.current_stream()
+            if isinstance(stream, torch.cuda.Stream) and not isinstance(stream, torch.cuda.ExternalStream):
+                for t in self._buffers:
+                    t.record_stream(stream)
+                self._streams.add(handle)
+        return handle
 
     def forward(self, x, residual, y, total, stream=None):
         """y = block(norm(x + residual)), total = x + residual; all [rows][hidden] with contiguous rows that share no
         element (no expanded tensors). residual and total may be None (the first block of a network has no residual); total
-        may be residual, and y may be x or residual, but not share an element with total. On one stream at a time."""
+        may be residual, and y may be x or residual, but not share an element with total. The tensors are ready on `stream` (None: the
+        current one) and outlive the pass. On one stream at a time."""
         import torch
         if self.index is not None and self.index != torch.cuda.current_device():
             with torch.cuda.device(self.index):
@@ -123,7 +148,7 @@ class GatedFfn:
                 raise ValueError(f"rows of a tensor share memory: {self.hidden} columns, stride {t.stride(0)}")
         if total is not None and _meet(y, total):
             raise ValueError("y and total share memory")
-        ws = self.workspace
+        stream, ws = self._use_on(stream), self.workspace
         aqd.qnorm_run(rows, self.hidden, self.type, self.eps, x, _ld(x), residual, _ld(residual), self.norm_weight,
                       total, _ld(total), self.c1, self.c1.stride(0), self.q1, stream)
         aqd.qlin_run(rows, self.units, self.hidden, self.type, aqd.QLIN_SILU_GATE, self.c1, self.c1.stride(0), self.q1, self.w1,
@@ -147,7 +172,7 @@ class GatedFfn:
         if self.index is not None and self.index != torch.cuda.current_device():
             with torch.cuda.device(self.index):
                 return self.replay(stream)
-        aqd.graph_launch(self._graph, stream)
+        aqd.graph_launch(self._graph, self._use_on(stream))
 
     def close(self):
         if self._graph is not None:

@@ -12,6 +12,8 @@ HIDDEN, UNITS, ROWS = 64, 96, 4
 def calls(monkeypatch):
     """The library's calls in order, as (name, arguments); tensors of the host pass for tensors of the GPU."""
     monkeypatch.setattr(ffn, "DEVICE", "cpu", raising=False)
+    monkeypatch.setattr(ffn, "_finish", lambda device: None, raising=False)
+    monkeypatch.setattr(aqd, "_stream", lambda s: 0 if s is None else s if isinstance(s, int) else s.cuda_stream)
     made = []
     for name in ("qrows_run", "qnorm_run", "qlin_run"):
         monkeypatch.setattr(aqd, name, lambda *a, _name=name, **kw: made.append((_name, a)))
@@ -219,3 +221,36 @@ def test_the_null_streams_handle(calls, monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: here)
     ffn.quantize_rows(weights()[1], 0)
     assert waits == [(default, here), (here, default)] and calls[0][1][-1] is default
+
+
+def test_set_up_is_done_when_the_block_is_there(monkeypatch, calls):
+    """The first pass may be on any stream: the weights' kernels have ended by then."""
+    monkeypatch.setattr(ffn, "_finish", lambda device: calls.append(("finish", (device,))), raising=False)
+    ffn.GatedFfn(*weights(), max_rows=ROWS)
+    assert [c[0] for c in calls] == ["qrows_run", "qrows_run", "finish"]
+
+
+def test_buffers_are_kept_for_the_streams_that_use_them(calls, monkeypatch):
+    """torch may give the memory of a dropped block to others at once, but for the streams that it knows of."""
+    f = ffn.GatedFfn(*weights(), max_rows=ROWS)
+    kept = []
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: kept.append((t.data_ptr(), s)))
+    monkeypatch.setattr(aqd, "graph_launch", lambda *a: None)
+
+    class Stream:
+        def __init__(self, handle):
+            self.cuda_stream = handle
+
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    here, side = Stream(0), Stream(77)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: here)
+    own = {t.data_ptr() for t in (f.norm_weight, f.w1, f.s1, f.w2, f.s2, f.c1, f.q1, f.h, f.c2, f.q2, f.workspace)}
+    f.forward(*(rows_of() for _ in range(4)))
+    assert not kept   # the stream of the set-up
+    for _ in range(2):
+        f.forward(*(rows_of() for _ in range(4)), side)
+    assert {p for p, _ in kept} == own and len(kept) == len(own) and {s for _, s in kept} == {side}
+    f._graph, third = 1, Stream(78)
+    f.replay(third)
+    f._graph = None
+    assert {p for p, s in kept if s is third} == own

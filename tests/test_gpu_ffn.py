@@ -150,3 +150,21 @@ def test_quantising_on_another_stream():
         got = codes.clone(), scales.clone()
         torch.cuda.synchronize()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_first_pass_on_another_stream():
+    """No wait between the set-up on the current stream and a pass on another one, nor before the block is dropped."""
+    import torch
+    rows, hidden = 16, 512
+    f, w, randn = block(torch, hidden, 1024, rows)
+    x, r = randn(rows, hidden), randn(rows, hidden)
+    want, total = torch.empty_like(x), torch.empty_like(x)
+    f.forward(x, r, want, total)
+    torch.cuda.synchronize()
+    side, y = torch.cuda.Stream(), torch.empty_like(x)
+    g = ffn.GatedFfn(*w, max_rows=rows)
+    g.forward(x, r, y, total, side)
+    del g
+    junk = [torch.full((1 << 20,), 77, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert torch.equal(y, want) and junk[0][0] == 77
