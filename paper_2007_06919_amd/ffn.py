@@ -67,9 +67,10 @@ def quantize_rows(w, stream=None):
     return codes, scales
 
 
-def _finish(device):
+def _finish(device, all=False):
+    """Wait for the current stream, or for all."""
     import torch
-    torch.cuda.current_stream(device).synchronize()
+    torch.cuda.synchronize(device) if all else torch.cuda.current_stream(device).synchronize()
 
 
 class GatedFfn:
@@ -110,7 +111,7 @@ class GatedFfn:
         self.c2, self.q2 = codes(units), scales()
         # the bound serves every call; the block's launches follow one another on one stream
         self.workspace = torch.empty(aqd.QLIN_WORKSPACE_BYTES, dtype=torch.uint8, device=dev)
-        self._graph = None
+        self._graph = self._recorded = None
         self._buffers = (self.norm_weight, self.w1, self.s1, self.w2, self.s2, self.c1, self.q1, self.h, self.c2, self.q2,
                          self.workspace)
         self._streams = {aqd._stream(None)}   # handles of those that torch keeps the buffers for
@@ -159,15 +160,24 @@ class GatedFfn:
         return y
 
     def capture(self, x, residual, y, total, stream):
-        """Record a pass on these tensors into a HIP graph (`stream`: not the null stream)."""
+        """Record a pass on these tensors into a HIP graph (`stream`: not the null stream), which holds them until `close` or
+        the next recording."""
         self.close()
         aqd.graph_begin(stream)
         try:
             self.forward(x, residual, y, total, stream)
-        finally:
-            self._graph = aqd.graph_end(stream)
+        except BaseException:
+            try:
+                aqd.graph_destroy(aqd.graph_end(stream))
+            except aqd.AqdError:
+                pass
+            raise
+        self._graph = aqd.graph_end(stream)
+        self._recorded = x, residual, y, total
 
     def replay(self, stream):
+        if self._graph is None:
+            raise RuntimeError("no pass is recorded: capture() first")
         import torch
         if self.index is not None and self.index != torch.cuda.current_device():
             with torch.cuda.device(self.index):
@@ -175,9 +185,17 @@ class GatedFfn:
         aqd.graph_launch(self._graph, self._use_on(stream))
 
     def close(self):
+        """Forget the recorded pass."""
         if self._graph is not None:
+            _finish(self.device, all=True)   # no replay may be pending
             aqd.graph_destroy(self._graph)
-            self._graph = None
+            self._graph = self._recorded = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 def reference(x, residual, norm_weight, gate, up, down, eps):

@@ -11,8 +11,8 @@ HIDDEN, UNITS, ROWS = 64, 96, 4
 @pytest.fixture
 def calls(monkeypatch):
     """The library's calls in order, as (name, arguments); tensors of the host pass for tensors of the GPU."""
-    monkeypatch.setattr(ffn, "DEVICE", "cpu", raising=False)
-    monkeypatch.setattr(ffn, "_finish", lambda device: None, raising=False)
+    monkeypatch.setattr(ffn, "DEVICE", "cpu")
+    monkeypatch.setattr(ffn, "_finish", lambda device, all=False: None)
     monkeypatch.setattr(aqd, "_stream", lambda s: 0 if s is None else s if isinstance(s, int) else s.cuda_stream)
     made = []
     for name in ("qrows_run", "qnorm_run", "qlin_run"):
@@ -225,7 +225,7 @@ def test_the_null_streams_handle(calls, monkeypatch):
 
 def test_set_up_is_done_when_the_block_is_there(monkeypatch, calls):
     """The first pass may be on any stream: the weights' kernels have ended by then."""
-    monkeypatch.setattr(ffn, "_finish", lambda device: calls.append(("finish", (device,))), raising=False)
+    monkeypatch.setattr(ffn, "_finish", lambda device: calls.append(("finish", (device,))))
     ffn.GatedFfn(*weights(), max_rows=ROWS)
     assert [c[0] for c in calls] == ["qrows_run", "qrows_run", "finish"]
 
@@ -254,3 +254,73 @@ def test_buffers_are_kept_for_the_streams_that_use_them(calls, monkeypatch):
     f.replay(third)
     f._graph = None
     assert {p for p, s in kept if s is third} == own
+
+
+class Graphs:
+    """The recording calls, with what they did."""
+
+    def __init__(self, monkeypatch):
+        self.live, self.began, self.launched = set(), 0, []
+        monkeypatch.setattr(aqd, "graph_begin", self.begin)
+        monkeypatch.setattr(aqd, "graph_end", self.end)
+        monkeypatch.setattr(aqd, "graph_destroy", self.live.remove)
+        monkeypatch.setattr(aqd, "graph_launch", lambda g, s: self.launched.append(g))
+
+    def begin(self, stream):
+        self.began += 1
+
+    def end(self, stream):
+        self.live.add(self.began)
+        return self.began
+
+
+def test_a_pass_that_cannot_be_recorded_leaves_no_graph(calls, monkeypatch):
+    f, graphs = ffn.GatedFfn(*weights(), max_rows=ROWS), Graphs(monkeypatch)
+    monkeypatch.setattr(ffn, "_finish", lambda device, all=False: None)
+
+    def fail(*a):
+        raise aqd.AqdError(aqd.AQD_ERR_DEVICE, "launch failed")
+
+    tensors = [rows_of() for _ in range(4)]
+    with monkeypatch.context() as m:
+        m.setattr(aqd, "qrows_run", fail)   # the third of the four launches
+        with pytest.raises(aqd.AqdError):
+            f.capture(*tensors, 5)
+    with pytest.raises(ValueError):
+        f.capture(rows_of(ROWS + 1), *tensors[1:], 5)
+    assert not graphs.live
+    with pytest.raises(RuntimeError):
+        f.replay(5)
+    assert not graphs.launched
+    f.capture(*tensors, 5)
+    f.replay(5)
+    assert len(graphs.live) == 1 and graphs.launched == list(graphs.live)
+    f.close()
+    with pytest.raises(RuntimeError):
+        f.replay(5)
+    assert not graphs.live
+
+
+def test_recorded_tensors_stay(calls, monkeypatch):
+    """A graph holds addresses: the block holds the tensors until the graph goes, and both go with the block."""
+    import gc
+    import weakref
+    f, graphs = ffn.GatedFfn(*weights(), max_rows=ROWS), Graphs(monkeypatch)
+    ended = []
+    monkeypatch.setattr(ffn, "_finish", lambda device, all=False: ended.append(all))
+    tensors = [rows_of() for _ in range(4)]
+    there = [weakref.ref(t) for t in tensors]
+    f.capture(*tensors, 5)
+    del tensors
+    del calls[:]   # (the recorded calls hold them too)
+    gc.collect()
+    assert all(t() is not None for t in there)
+    f.close()
+    assert ended == [True] and not graphs.live   # replays may be pending
+    gc.collect()
+    assert all(t() is None for t in there)
+    f.capture(*(rows_of() for _ in range(4)), 5)
+    del f
+    del calls[:]
+    gc.collect()
+    assert not graphs.live
