@@ -335,7 +335,7 @@ enum { AQD_F32 = 0, AQD_F16 = 1, AQD_BF16 = 2 };   /* types of real-valued tenso
  * zeros has codes 0. A row that holds an infinity or a NaN has codes 0 and the
  * scale NaN. Quantises activations, and offline the weights [n][k] of qlin. */
 typedef struct {
-    int rows, cols; /* cols >= 1 */
+    int rows, cols; /* 1 <= cols <= INT32_MAX - 16384 */
     int type;       /* AQD_F32, AQD_F16 or AQD_BF16 */
     int64_t ld_x, ld_codes;
 } qrows_desc_t;
@@ -353,7 +353,7 @@ aqd_status_t qrows_run(const qrows_desc_t *desc, const void *x, int8_t *codes, f
  * finite has codes 0 and the scale NaN. All tensors are of `type`; weight has
  * cols elements. sum may be residual or x (with its stride): in place. */
 typedef struct {
-    int rows, cols; /* cols >= 1 */
+    int rows, cols; /* 1 <= cols <= INT32_MAX - 16384 */
     int type;
     float eps;      /* finite, >= 0 */
     int64_t ld_x, ld_residual, ld_sum, ld_codes;

@@ -1804,6 +1804,8 @@ aqd_status_t rows_call(RowsArgs &a, int rows, hipStream_t stream)
 {
     const int size = real_size(a.type);
     REQUIRE(rows >= 0 && a.cols >= 1, "rows must be at least 0 and cols at least 1");
+    // the kernels' column indices have 32 bits and run past a row's end by up to 8192 and a vector
+    REQUIRE(a.cols <= INT32_MAX - 16384, "too many cols");
     REQUIRE(size, "type must be AQD_F32, AQD_F16 or AQD_BF16");
     a.rows = rows;
     for (long long *ld : {&a.ld_x, &a.ld_residual, &a.ld_sum, &a.ld_codes}) {

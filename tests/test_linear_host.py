@@ -120,3 +120,20 @@ def test_real_types():
 def test_a_single_row_has_a_bounded_stride_too(call, bad):
     """2^62 elements of 4 bytes are 0 bytes in 64 bits, which no overlap check may divide by."""
     refused(call, rows=1, **bad)
+
+
+MOST_COLS = 2 ** 31 - 1 - 16384   # column indices are 32 bits wide, and run past the row's end by what a workgroup takes at once
+
+
+@pytest.mark.parametrize("cols", [MOST_COLS + 1, 2 ** 31 - 8193, 2 ** 31 - 1])
+@pytest.mark.parametrize("rows", [0, 1])
+def test_rows_too_long_for_their_indices_are_refused(cols, rows):
+    far = {name: (i + 1) << 40 for i, name in enumerate(ADDR)}
+    for call in (rows_call, norm_call):
+        refused(call, rows=rows, cols=cols, **far)
+        assert "cols" in aqd.last_error()
+
+
+def test_the_longest_rows_are_taken():
+    rows_call(rows=0, cols=MOST_COLS)
+    norm_call(rows=0, cols=MOST_COLS)
