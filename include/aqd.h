@@ -367,7 +367,8 @@ aqd_status_t qnorm_run(const qnorm_desc_t *desc, const void *x, const void *resi
  *   AQD_QLIN_PLAIN:     y[t][j] = z[t][j], j < n; w has n rows
  *   AQD_QLIN_SILU_GATE: y[t][j] = z[t][j] / (1 + exp(-z[t][j])) * z[t][n + j]; w has 2n
  *                       rows, the gate's n first (a gated feed-forward unit)
- * rounded once to `type`. x: [rows][k] int8, w: [n or 2n][k] int8, all 256 code
+ * rounded once to `type`. The gate's factor z / (1 + exp(-z)) is within (|z| + 4) 2^-23 of itself, and may be -0
+ * where z < -87.3 (below 9e-37). x: [rows][k] int8, w: [n or 2n][k] int8, all 256 code
  * values; x_scales [rows], w_scales and bias (NULL: none) one per row of w. NaN and
  * infinite scales act as in fp32: a row whose scale is NaN gives a row of NaN.
  * UNSUPPORTED for k > 131071, from where on a sum could leave int32.

@@ -448,3 +448,25 @@ def test_rows_that_end_inside_a_stage(rows, n, k):
         z, v = sums[:, :n] / 4096, sums[:, n:] / 4096
         want = z / (1 + torch.exp(-z)) * v
         assert bool(((y.double() - want).abs() <= want.abs() * ((z.abs() + 4) * 2.0 ** -22 + 2.0 ** -23) + 2.0 ** -149).all())
+
+
+@pytest.mark.parametrize("rows, n, k", [(1, 70, 64), (40, 130, 64), (300, 520, 256), (5, 70, 7), (300, 520, 255)])
+def test_gates_of_known_values(rows, n, k):
+    """The gate's factor against 64 bits, where its bias alone makes z (the scales are 0). The hardware's exponential and
+    reciprocal are off by 2^-23 each, the sum and the last product by 2^-24, the exponential's argument by
+    (2^-24 log2(e) + 1.93e-8) |z|, of which the exponential makes ln(2) times as much: below (0.62 |z| + 3) 2^-23 of the
+    factor. Under -87.3 the reciprocal is below the normal numbers, for which the hardware may give 0."""
+    import torch
+    gates = np.array([-1e30, -200, -104, -89, -88, -87.2, -80, -60, -40, -20, -8, -1, -1e-3, -1e-30, 0, 1e-30, 0.5, 1, 8, 20, 80, 200,
+                      1e30], np.float32)
+    z = np.resize(gates, n)
+    x, w = (torch.ones(r, k, dtype=torch.int8, device="cuda:0") for r in (rows, 2 * n))
+    bias = torch.from_numpy(np.concatenate([z, np.ones(n, np.float32)])).cuda()
+    y = torch.full((rows, n), 5.0, device="cuda:0")
+    aqd.qlin_run(rows, n, k, aqd.F32, aqd.QLIN_SILU_GATE, x, 0, torch.zeros(rows, device="cuda:0"), w, 0,
+                 torch.zeros(2 * n, device="cuda:0"), bias, y, 0)
+    got, ze = y.double().cpu().numpy(), z.astype(np.float64)
+    e = np.exp(-np.abs(ze))
+    want = np.where(ze < 0, ze * e / (1 + e), ze / (1 + e))
+    tol = np.where(ze < -87.3, np.abs(want), np.abs(want) * (np.abs(ze) + 4) * 2.0 ** -23)
+    assert (np.abs(got - want) <= tol).all() and (got[:, z < 0] <= 0).all()
