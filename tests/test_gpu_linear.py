@@ -468,5 +468,6 @@ def test_gates_of_known_values(rows, n, k):
     got, ze = y.double().cpu().numpy(), z.astype(np.float64)
     e = np.exp(-np.abs(ze))
     want = np.where(ze < 0, ze * e / (1 + e), ze / (1 + e))
-    tol = np.where(ze < -87.3, np.abs(want), np.abs(want) * (np.abs(ze) + 4) * 2.0 ** -23)
+    part = np.where(ze < 0, 1, e) / (1 + e)   # of the exponential's error, what the sum with 1 leaves
+    tol = np.where(ze < -87.3, np.abs(want), np.abs(want) * (np.abs(ze) * part + 4) * 2.0 ** -23)
     assert (np.abs(got - want) <= tol).all() and (got[:, z < 0] <= 0).all()
