@@ -121,11 +121,8 @@ namespace {
 
 hipError_t launch_part(const QlinArgs &a, int shape, hipStream_t stream)
 {
-    if (a.gate)
-        launch_shape<float, true, true>(a, shape, stream);
-    else
-        launch_shape<float, false, true>(a, shape, stream);
-    return hipGetLastError();
+    const bool known = a.gate ? launch_shape<float, true, true>(a, shape, stream) : launch_shape<float, false, true>(a, shape, stream);
+    return known ? hipGetLastError() : hipErrorInvalidValue;
 }
 
 template <typename T>

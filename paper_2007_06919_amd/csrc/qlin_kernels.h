@@ -896,40 +896,41 @@ void launch_tile(const QlinArgs &a, hipStream_t stream)
     }
 }
 
-// rows of w (with the gate: of both halves) x tokens; a gated tile's waves hold pairs of row tiles
+// rows of w (with the gate: of both halves) x tokens; a gated tile's waves hold pairs of row tiles. False for a shape that
+// is not there in this form, for which nothing is launched.
 template <typename T, bool GATE, bool PART>
-void launch_shape(const QlinArgs &a, int shape, hipStream_t stream)
+bool launch_shape(const QlinArgs &a, int shape, hipStream_t stream)
 {
     switch (shape) {
-    case QLIN_ANY: return launch_any<T, GATE, PART>(a, stream);
+    case QLIN_ANY: return launch_any<T, GATE, PART>(a, stream), true;
     case QLIN_64x32:
         if constexpr (GATE)
-            return launch_tile<T, GATE, PART, true, 128, 32, 2, 1, 4>(a, stream);
+            return launch_tile<T, GATE, PART, true, 128, 32, 2, 1, 4>(a, stream), true;
         else
-            return launch_tile<T, GATE, PART, true, 64, 32, 2, 1, 4>(a, stream);
+            return launch_tile<T, GATE, PART, true, 64, 32, 2, 1, 4>(a, stream), true;
     case QLIN_64x64:   // plain only: the gated 128x64 has the same tile
         if constexpr (!GATE)
-            return launch_tile<T, GATE, PART, true, 64, 64, 2, 2, 4>(a, stream);
+            return launch_tile<T, GATE, PART, true, 64, 64, 2, 2, 4>(a, stream), true;
         break;
     case QLIN_128x64:
         if constexpr (GATE)
-            return launch_tile<T, GATE, PART, true, 128, 64, 2, 2, 3>(a, stream);
+            return launch_tile<T, GATE, PART, true, 128, 64, 2, 2, 3>(a, stream), true;
         else
-            return launch_tile<T, GATE, PART, true, 128, 64, 4, 2, 3>(a, stream);
+            return launch_tile<T, GATE, PART, true, 128, 64, 4, 2, 3>(a, stream), true;
     case QLIN_128x128:
         if constexpr (GATE)
-            return launch_tile<T, GATE, PART, true, 128, 128, 2, 4, 3>(a, stream);
+            return launch_tile<T, GATE, PART, true, 128, 128, 2, 4, 3>(a, stream), true;
         else
-            return launch_tile<T, GATE, PART, true, 128, 128, 4, 2, 3>(a, stream);
+            return launch_tile<T, GATE, PART, true, 128, 128, 4, 2, 3>(a, stream), true;
     case QLIN_128x128_TWO:   // two stages of LDS: two workgroups to a CU
         if constexpr (GATE)
-            return launch_tile<T, GATE, PART, true, 128, 128, 2, 4, 2>(a, stream);
+            return launch_tile<T, GATE, PART, true, 128, 128, 2, 4, 2>(a, stream), true;
         else
-            return launch_tile<T, GATE, PART, true, 128, 128, 4, 2, 2>(a, stream);
-    case QLIN_256x128: return launch_tile<T, GATE, PART, true, 256, 128, 4, 2, 3>(a, stream);
-    case QLIN_256x256: return launch_tile<T, GATE, PART, true, 256, 256, 2, 4, 2>(a, stream);
-    case QLIN_128x128_ANY: return launch_tile<T, GATE, PART, false, 128, 128, 2, 2, 2>(a, stream);
-    case QLIN_256x256_ANY: return launch_tile<T, GATE, PART, false, 256, 256, 2, 4, 2>(a, stream);
+            return launch_tile<T, GATE, PART, true, 128, 128, 4, 2, 2>(a, stream), true;
+    case QLIN_256x128: return launch_tile<T, GATE, PART, true, 256, 128, 4, 2, 3>(a, stream), true;
+    case QLIN_256x256: return launch_tile<T, GATE, PART, true, 256, 256, 2, 4, 2>(a, stream), true;
+    case QLIN_128x128_ANY: return launch_tile<T, GATE, PART, false, 128, 128, 2, 2, 2>(a, stream), true;
+    case QLIN_256x256_ANY: return launch_tile<T, GATE, PART, false, 256, 256, 2, 4, 2>(a, stream), true;
     default: break;
     }
     if constexpr (!PART) {
@@ -937,18 +938,16 @@ void launch_shape(const QlinArgs &a, int shape, hipStream_t stream)
         if (shape == QLIN_FEW16)
             return bytes ? launch_few<T, GATE, true, 1, 4>(a, stream) : launch_few<T, GATE, false, 1, 4>(a, stream);
         if (shape == QLIN_FEW64)
-            return launch_few<T, GATE, true, 4, 2>(a, stream);   // (aligned rows have faster tiles)
+            return launch_few<T, GATE, true, 4, 2>(a, stream), true;   // (aligned rows have faster tiles)
     }
+    return false;
 }
 
 template <typename T>
 hipError_t launch_typed(const QlinArgs &a, int shape, hipStream_t stream)
 {
-    if (a.gate)
-        launch_shape<T, true, false>(a, shape, stream);
-    else
-        launch_shape<T, false, false>(a, shape, stream);
-    return hipGetLastError();
+    const bool known = a.gate ? launch_shape<T, true, false>(a, shape, stream) : launch_shape<T, false, false>(a, shape, stream);
+    return known ? hipGetLastError() : hipErrorInvalidValue;
 }
 
 }  // namespace

@@ -4,6 +4,7 @@ import ctypes
 
 import pytest
 
+import linear_plan
 from paper_2007_06919_amd import aqd
 
 A = 1 << 20   # an address for each tensor, far from the others
@@ -137,3 +138,14 @@ def test_rows_too_long_for_their_indices_are_refused(cols, rows):
 def test_the_longest_rows_are_taken():
     rows_call(rows=0, cols=MOST_COLS)
     norm_call(rows=0, cols=MOST_COLS)
+
+
+@pytest.mark.parametrize("shape, parts, act", [
+    (linear_plan.T64x64, 1, aqd.QLIN_SILU_GATE), (linear_plan.T64x64, 2, aqd.QLIN_SILU_GATE),   # plain only
+    (linear_plan.FEW16, 2, aqd.QLIN_PLAIN), (linear_plan.FEW64, 2, aqd.QLIN_SILU_GATE),         # never split
+    (len(linear_plan.NAMES), 1, aqd.QLIN_PLAIN), (-1, 1, aqd.QLIN_PLAIN),
+])
+def test_a_kernel_that_is_not_there_is_an_error(shape, parts, act):
+    """A plan may name a kernel that has no such form: an error, where a launch of nothing would be a success."""
+    for kind in (aqd.F32, aqd.F16, aqd.BF16):
+        assert linear_plan.launch(linear_plan.args(64, 256, 4096, kind, act), (shape, parts, 0)) == 1   # hipErrorInvalidValue
