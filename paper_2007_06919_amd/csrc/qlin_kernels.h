@@ -936,7 +936,7 @@ bool launch_shape(const QlinArgs &a, int shape, hipStream_t stream)
     if constexpr (!PART) {
         const bool bytes = (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.ld_x | (uintptr_t)a.ld_w) & 3) != 0;
         if (shape == QLIN_FEW16)
-            return bytes ? launch_few<T, GATE, true, 1, 4>(a, stream) : launch_few<T, GATE, false, 1, 4>(a, stream);
+            return bytes ? launch_few<T, GATE, true, 1, 4>(a, stream) : launch_few<T, GATE, false, 1, 4>(a, stream), true;
         if (shape == QLIN_FEW64)
             return launch_few<T, GATE, true, 4, 2>(a, stream), true;   // (aligned rows have faster tiles)
     }
