@@ -502,6 +502,15 @@ __device__ __forceinline__ Place place(unsigned id, unsigned total, int tiles_n,
     return p;
 }
 
+// What a wave's lanes wrote to LDS is there for its other lanes, which the LDS's order within a wave makes so by itself: this
+// keeps the compiler to it (no instruction).
+__device__ __forceinline__ void lanes_meet()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // The sums of a wave to y (or the partial sums): 32 tokens at a time through the wave's own
 // 32 x (32 NA) int32 of LDS, so that stores are whole lines of consecutive outputs, and a
 // lane keeps the scales of its channels. A lane holds token lane % 32, rows 8 g + 4 (lane / 32)
@@ -546,6 +555,7 @@ __device__ __forceinline__ void store_tile(const QlinArgs &A, const v16i (&acc)[
                 const int slot = (row / 4 + 2 * g + (lane >> 5)) ^ (tw & (SLOTS - 1));
                 *(v4i *)(stage + (tw * SLOTS + slot) * 16) = v4i{acc[i][b][4 * g], acc[i][b][4 * g + 1], acc[i][b][4 * g + 2], acc[i][b][4 * g + 3]};
             }
+        lanes_meet();
         // (past: past the L2, in tiles of large outputs; a choice within a round would be lost where the compiler joins
         // the stores again)
         auto rounds = [&](auto past) {
@@ -596,13 +606,11 @@ __device__ __forceinline__ void store_tile(const QlinArgs &A, const v16i (&acc)[
                 }
             }
         };
-        if constexpr (PAST && !PART) {
-            if (A.whole_lines) {
-                rounds(std::true_type{});
-                continue;
-            }
-        }
-        rounds(std::false_type{});
+        if (PAST && !PART && A.whole_lines)
+            rounds(std::true_type{});
+        else
+            rounds(std::false_type{});
+        lanes_meet();   // the next tokens take their place
     }
 }
 
