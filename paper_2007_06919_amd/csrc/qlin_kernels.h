@@ -38,6 +38,16 @@ __device__ __forceinline__ void scaled4(const QlinArgs &A, const v4i acc, int j,
 // numbers, and -0
 __device__ __forceinline__ float silu(float z) { return z * __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
 
+// z as the fp32 number that it is. Without this, a gated product and its conversion to fp16 become one instruction in some
+// kernels, which rounds once where the others round twice: outputs of a split sum were not those of the whole one.
+template <typename T>
+__device__ __forceinline__ float in_fp32(float z)
+{
+    if constexpr (std::is_same<T, _Float16>::value)
+        asm("" : "+v"(z));
+    return z;
+}
+
 // four consecutive outputs of a token from column j on; value: the gated unit's second half
 template <typename T, bool GATE>
 __device__ __forceinline__ void emit4(const QlinArgs &A, long long t, int j, const v4i acc, const v4i value, float sx)
@@ -52,7 +62,7 @@ __device__ __forceinline__ void emit4(const QlinArgs &A, long long t, int j, con
         scaled4(A, value, A.n + j, left, sx, v);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            z[e] = silu(z[e]) * v[e];
+            z[e] = in_fp32<T>(silu(z[e]) * v[e]);
     }
     T *y = (T *)A.y + t * A.ld_y + j;
     typename Four<T>::type o;
@@ -586,7 +596,7 @@ __device__ __forceinline__ void store_tile(const QlinArgs &A, const v16i (&acc)[
                         for (int f = 0; f < 4; ++f) {
                             float z = __builtin_fmaf((float)c[f] * sx, ws[e + f], wb[e + f]);
                             if constexpr (GATE)
-                                z = silu(z) * __builtin_fmaf((float)d[f] * sx, vs[e + f], vb[e + f]);
+                                z = in_fp32<T>(silu(z) * __builtin_fmaf((float)d[f] * sx, vs[e + f], vb[e + f]));
                             zs[e + f] = z;
                         }
                     }

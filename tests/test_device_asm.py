@@ -115,3 +115,12 @@ def test_matrix_kernels_have_no_mfma_hazards(device_asm, src, least):
     found, n = mfma_hazards.scan(device_asm[src][1])
     assert n >= least, n
     assert found == [], "\n".join(found[:10])
+
+
+def test_products_round_to_fp32_before_fp16(device_asm):
+    """No multiplication is joined with its conversion to fp16 (one rounding instead of two) in the 8-bit product, whose kernels
+    all give the same bits."""
+    for src in ("qlin.hip", "qlin_f16.hip"):
+        dis = device_asm[src][1]
+        assert "v_cvt_pk_f16_f32" in dis or "v_cvt_f16_f32" in dis
+        assert not re.findall(r"v_(?:fma|mad)_mix\w*", dis), src

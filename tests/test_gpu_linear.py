@@ -471,3 +471,38 @@ def test_gates_of_known_values(rows, n, k):
     part = np.where(ze < 0, 1, e) / (1 + e)   # of the exponential's error, what the sum with 1 leaves
     tol = np.where(ze < -87.3, np.abs(want), np.abs(want) * (np.abs(ze) * part + 4) * 2.0 ** -23)
     assert (np.abs(got - want) <= tol).all() and (got[:, z < 0] <= 0).all()
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("act", [aqd.QLIN_PLAIN, aqd.QLIN_SILU_GATE])
+def test_every_kernel_gives_the_same_bits(act, t):
+    """A row's outputs do not depend on the rows beside it, nor on where rows start: tiles, the small launches' kernels, the
+    one for any stride and a split sum. 400 thousand outputs: a rounding to fp32 left out before one to fp16 shows in some."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(9)
+    rows, n, k = 200, 2000, 4096
+    wide = 2 * n if act else n
+    x, w = (torch.randint(-128, 128, (r, k), generator=g, device="cuda", dtype=torch.int8) for r in (rows, wide))
+    sx = (torch.rand(rows, generator=g, device="cuda") + 0.5) / 74
+    sw = (torch.rand(wide, generator=g, device="cuda") + 0.5) / (74 * math.sqrt(k))
+    work = torch.empty(aqd.QLIN_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+
+    def product(x, sx, w, ws=None):
+        y = torch.zeros(x.shape[0], n, dtype=dtype(torch, t), device="cuda")
+        aqd.qlin_run(x.shape[0], n, k, TYPES[t], act, x, x.stride(0), sx, w, w.stride(0), sw, None, y, 0, ws,
+                     work.numel() if ws is not None else 0)
+        return y
+
+    def moved(m, ld, shift):
+        return matrix(torch, m, ld, shift)[1]
+
+    whole = product(x, sx, w)
+    assert whole.ne(0).any()
+    for rows_at in (slice(0, 1), slice(3, 15), slice(20, 60), slice(0, 130)):
+        part = x[rows_at].contiguous()
+        assert torch.equal(product(part, sx[rows_at].contiguous(), w), whole[rows_at])
+        assert torch.equal(product(moved(part, k + 1, 1), sx[rows_at].contiguous(), moved(w, k + 3, 2)), whole[rows_at])
+        assert torch.equal(product(part, sx[rows_at].contiguous(), w, work), whole[rows_at])
+    far = torch.empty(2 * (1 << 23) + k, dtype=torch.int8, device="cuda").as_strided((3, k), (1 << 23, 1))
+    far.copy_(x[:3])
+    assert torch.equal(product(far, sx[:3].contiguous(), w), whole[:3])
