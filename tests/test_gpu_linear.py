@@ -391,7 +391,7 @@ def test_on_another_stream_and_in_a_graph():
         aqd.graph_destroy(graph)
 
 
-# sizes at which each of the kernels is the fastest, or nearly (rows at any address: k odd)
+# large sizes, for several of the kernels (sizes for each of them: linear_plan.COVER; rows at any address: k odd)
 LARGE = [(2100, 2200, 640), (4000, 1300, 1100), (2500, 4100, 2048), (1300, 1500, 1000), (520, 2100, 512), (9000, 330, 200),
          (300, 1000, 6000), (140, 520, 16000), (1700, 900, 333), (2300, 2100, 1001), (90, 4000, 2001), (700, 300, 7777)]
 
