@@ -376,8 +376,9 @@ aqd_status_t qnorm_run(const qnorm_desc_t *desc, const void *x, const void *resi
  * workspace (device, 16-byte aligned, ws_bytes): with it, launches of few output tiles split
  * the sum over k between workgroups, partial sums (int32, exact) in the workspace.
  * qlin_workspace gives the size for a call (0: it does not split; never more than
- * AQD_QLIN_WORKSPACE_BYTES, which therefore serves every call); less than that, or NULL, runs
- * unsplit with the same result, bit for bit. Calls that share a workspace must not overlap in time.
+ * AQD_QLIN_WORKSPACE_BYTES, which therefore serves every call); with less, the sum is split into
+ * fewer parts that fit, or not at all, as it is with NULL: the same result, bit for bit, and no byte past
+ * ws_bytes is written. Calls that share a workspace must not overlap in time.
  * Its size depends on the description alone. */
 #define AQD_QLIN_WORKSPACE_BYTES (64u << 20)
 enum { AQD_QLIN_PLAIN = 0, AQD_QLIN_SILU_GATE = 1 };
