@@ -25,22 +25,14 @@ from . import aqd
 DEVICE = "cuda"   # where the library's kernels run: no other address may reach them
 
 
-def _ld(t):
-    """Row stride of a [rows][cols] tensor for the library, which takes 0 for packed rows; a single row has none, nor has None."""
-    return t.stride(0) if t is not None and t.shape[0] > 1 else 0
-
-
-def _meet(a, b):
+def _meet(a, ld_a, b, ld_b, rows, cols):
     """Whether two [rows][cols] tensors of one type may share an element (column ranges of one buffer do not)."""
-    size, cols = a.element_size(), a.shape[1]
-    pa, pb = a.data_ptr(), b.data_ptr()
-    ea, eb = (p + size * ((t.shape[0] - 1) * _ld(t) + cols) for p, t in ((pa, a), (pb, b)))
-    if not a.shape[0] or pa >= eb or pb >= ea:
+    if not rows:
         return False
-    if a.shape[0] == 1 or _ld(a) != _ld(b):
-        return True
-    d = (pb - pa) // size % _ld(a)
-    return d < cols or d + cols > _ld(a)
+    gap = (b.data_ptr() - a.data_ptr()) // a.element_size()
+    if gap >= (rows - 1) * ld_a + cols or -gap >= (rows - 1) * ld_b + cols:
+        return False
+    return rows == 1 or ld_a != ld_b or gap % ld_a < cols or gap % ld_a + cols > ld_a
 
 
 def quantize_rows(w, stream=None):
@@ -61,7 +53,7 @@ def quantize_rows(w, stream=None):
         stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
     if stream is not None:
         stream.wait_stream(torch.cuda.current_stream())
-    aqd.qrows_run(rows, cols, aqd.real_type(w), w, _ld(w), codes, codes.stride(0), scales, stream)
+    aqd.qrows_run(rows, cols, aqd.real_type(w), w, w.stride(0) if rows > 1 else 0, codes, codes.stride(0), scales, stream)
     if stream is not None:
         torch.cuda.current_stream().wait_stream(stream)
     return codes, scales
@@ -110,7 +102,9 @@ class GatedFfn:
         self.h = torch.empty(max_rows, units, dtype=self.dtype, device=dev)
         self.c2, self.q2 = codes(units), scales()
         # the bound serves every call; the block's launches follow one another on one stream
-        self.workspace = torch.empty(aqd.QLIN_WORKSPACE_BYTES, dtype=torch.uint8, device=dev)
+        self.ws_bytes = aqd.QLIN_WORKSPACE_BYTES
+        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
+        self.ld_c1, self.ld_w1, self.ld_c2, self.ld_w2 = (t.stride(0) for t in (self.c1, self.w1, self.c2, self.w2))
         self._graph = self._recorded = None
         self._buffers = (self.norm_weight, self.w1, self.s1, self.w2, self.s2, self.c1, self.q1, self.h, self.c2, self.q2,
                          self.workspace)
@@ -119,9 +113,9 @@ class GatedFfn:
 
     def _use_on(self, stream):
         """The handle of `stream` (None: the current one), for which torch keeps the buffers from now on."""
-        import torch
         handle = aqd._stream(stream)
         if handle not in self._streams:
+            import torch
             if stream is None:
                 stream = torch.cuda.current_stream()
             if isinstance(stream, torch.cuda.Stream) and not isinstance(stream, torch.cuda.ExternalStream):
@@ -139,25 +133,36 @@ class GatedFfn:
         if self.index is not None and self.index != torch.cuda.current_device():
             with torch.cuda.device(self.index):
                 return self.forward(x, residual, y, total, stream)
-        rows = x.shape[0]
+        rows, hidden, units, ws = x.shape[0], self.hidden, self.units, self.workspace
         if rows > self.max_rows:
             raise ValueError(f"{rows} rows, and buffers for {self.max_rows}")
-        for t in (x, y, *(t for t in (residual, total) if t is not None)):
-            if t.shape != (rows, self.hidden) or t.dtype != self.dtype or t.stride(1) != 1 or t.device != self.device:
-                raise ValueError(f"tensors must be [{rows}][{self.hidden}] {self.dtype} with contiguous rows on {self.device}")
-            if rows > 1 and t.stride(0) < self.hidden:
-                raise ValueError(f"rows of a tensor share memory: {self.hidden} columns, stride {t.stride(0)}")
-        if total is not None and _meet(y, total):
+        ld_x, ld_y = self._row_stride(x, rows), self._row_stride(y, rows)
+        ld_residual = 0 if residual is None else self._row_stride(residual, rows)
+        ld_total = 0 if total is None else self._row_stride(total, rows)
+        if total is not None and _meet(y, ld_y, total, ld_total, rows, hidden):
             raise ValueError("y and total share memory")
-        stream, ws = self._use_on(stream), self.workspace
-        aqd.qnorm_run(rows, self.hidden, self.type, self.eps, x, _ld(x), residual, _ld(residual), self.norm_weight,
-                      total, _ld(total), self.c1, self.c1.stride(0), self.q1, stream)
-        aqd.qlin_run(rows, self.units, self.hidden, self.type, aqd.QLIN_SILU_GATE, self.c1, self.c1.stride(0), self.q1, self.w1,
-                     self.w1.stride(0), self.s1, None, self.h, self.units, ws, ws.numel(), stream)
-        aqd.qrows_run(rows, self.units, self.type, self.h, self.units, self.c2, self.c2.stride(0), self.q2, stream)
-        aqd.qlin_run(rows, self.hidden, self.units, self.type, aqd.QLIN_PLAIN, self.c2, self.c2.stride(0), self.q2, self.w2,
-                     self.w2.stride(0), self.s2, None, y, _ld(y), ws, ws.numel(), stream)
+        stream = self._use_on(stream)
+        aqd.qnorm_run(rows, hidden, self.type, self.eps, x, ld_x, residual, ld_residual, self.norm_weight, total, ld_total,
+                      self.c1, self.ld_c1, self.q1, stream)
+        aqd.qlin_run(rows, units, hidden, self.type, aqd.QLIN_SILU_GATE, self.c1, self.ld_c1, self.q1, self.w1, self.ld_w1, self.s1, None,
+                     self.h, units, ws, self.ws_bytes, stream)
+        aqd.qrows_run(rows, units, self.type, self.h, units, self.c2, self.ld_c2, self.q2, stream)
+        aqd.qlin_run(rows, hidden, units, self.type, aqd.QLIN_PLAIN, self.c2, self.ld_c2, self.q2, self.w2, self.ld_w2, self.s2, None,
+                     y, ld_y, ws, self.ws_bytes, stream)
         return y
+
+    def _row_stride(self, t, rows):
+        """A caller's tensor, checked; its row stride as the library takes it, which reads 0 as packed rows. A single row has none."""
+        if t.shape != (rows, self.hidden) or t.dtype != self.dtype or t.device != self.device:
+            raise ValueError(f"tensors must be [{rows}][{self.hidden}] {self.dtype} on {self.device}")
+        ld, step = t.stride()
+        if step != 1:
+            raise ValueError("the rows of a tensor are not contiguous")
+        if rows < 2:
+            return 0
+        if ld < self.hidden:
+            raise ValueError(f"rows of a tensor share memory: {self.hidden} columns, stride {ld}")
+        return ld
 
     def capture(self, x, residual, y, total, stream):
         """Record a pass on these tensors into a HIP graph (`stream`: not the null stream), which holds them until `close` or
