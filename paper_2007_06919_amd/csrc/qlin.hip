@@ -12,8 +12,11 @@ namespace {
 // fit a CU, and its time in us per stage of 128 k while few CUs run and while all do, and per round
 // of workgroups apart from the stages (first loads, stores), with the gate that many times as much.
 // Fitted to launches of 1140 random sizes (1 to 11000 tokens, 128 to 16384 outputs and k, plain and
-// gated, every shape with 1 to 8 parts): the plan's launch is 2% (aligned rows) and 1.2% slower than
-// the fastest of them on average, 7% and 4% at the ninetieth percentile. Without one of the shapes the
+// gated, every shape with 1 to 8 parts, by least squares of the times' logarithms, each weighted by the
+// square of the fastest's share of it, without those over twice the fastest). On 400 other sizes of that range, bf16, the
+// plan's launch is 4.3% (rows at multiples of 4) and 3.2% (at any byte) slower than the fastest on average, 14% and 9% at the
+// ninetieth percentile, 1.53 and 1.66 times at worst (gated 408 x 1034 x 14543 48.7 us, 31.9 with 256x128 in 6 parts;
+// 1 x 11360 x 767 8.4, FEW16 5.1). On the sizes of the fit, without one of the shapes the
 // fastest is 0.3% (128x128_TWO; 32% at worst, many tiles and a short k) to 1.8% slower on average; one shape
 // for all, 2 to 10 times at the other end of the sizes.
 struct Shape {

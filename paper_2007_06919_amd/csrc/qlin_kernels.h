@@ -455,9 +455,10 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) qlin_few_kernel(QlinArgs A)
 // The 16-byte columns of LDS row r (128 bytes) sit XORed with swz(r), which is done by permuting the
 // lanes' source columns; fragment reads hit every bank once (no conflict in the counters).
 //
-// Large products are bound by power: 8192 x 8192 x 8192 takes 450 to 466 us (2360 to 2440 TOPS), its matrix cores busy
-// for 63% of the cycles of a clock that falls to 1.7 GHz (on codes of zero 404 us). Small tiles are bound by their
-// copies (about 47 bytes a clock and CU) and their first and last microseconds.
+// Large products are bound by power: 8192 x 8192 x 8192 takes 449 to 474 us (2320 to 2450 TOPS), its matrix cores busy
+// for 63% of the cycles of a clock that falls to 1.7 GHz (on codes of zero 404 us). Small tiles (up to 128 x 64)
+// are bound by their copies (24 KiB a stage in 0.25 us: 47 bytes a clock and CU) and their first and last microseconds. The
+// 128 x 128 tiles of a sum split in 4 over rows of 16384 bytes (192 x 4096 x 16384) are bound by neither: 20 bytes a clock.
 typedef int v16i __attribute__((ext_vector_type(16)));
 typedef uint32_t v4u32 __attribute__((ext_vector_type(4)));
 
