@@ -393,6 +393,126 @@ aqd_status_t qlin_run(const qlin_desc_t *desc, const int8_t *x, const float *x_s
                       const float *w_scales, const float *bias, void *y, void *workspace, size_t ws_bytes,
                       aqd_stream_t stream);
 
+/* ---- attention: norms and rotation of heads, a 4-bit cache, attention over it and over prompts -------
+ * The attention half of a transformer's block, next to the linear layers above. Queries, keys
+ * and values are tensors [tokens][heads][dim] of a real type whose channels are contiguous; each has a
+ * token stride and a head stride in elements, so they may be slices of one joint projection's rows, or
+ * [heads][tokens][dim]. Of the two strides the smaller is at least dim, and the larger at least what
+ * the other dimension spans (a stride is ignored where its dimension has one entry): no element twice.
+ * Pointers need the alignment of their elements only. What lies between rows is never written. An output must share no
+ * element with an input or another output, but for aqd_heads_run's. A count of 0 (tokens, queries,
+ * batch) is a no-op. The calls allocate nothing and may be recorded into a graph; device
+ * arrays of indices are read when the launch runs, and an index out of range is never followed (what
+ * happens instead stands at each call).
+ *
+ * Norm of each query and key head, and its rotation by the token's position, in one pass (fp32, rounded once):
+ *   n[c] = x[c] / sqrt(mean(x^2) + eps) * weight[c]                 (weight NULL: n = x, for q and k each)
+ *   y[a] = n[a] cos - n[b] sin,  y[b] = n[b] cos + n[a] sin         for the pairs (a, b) of the first rot channels
+ *   y[c] = n[c]                                                     for the others
+ * AQD_PAIRS_HALVES: a = i, b = i + rot / 2; AQD_PAIRS_NEIGHBOURS: a = 2 i, b = 2 i + 1; 0 <= i < rot / 2.
+ * table: fp32 [positions][rot], of each position the cosines of its rot / 2 angles, then their sines;
+ * position: the tokens' rows of it, int32 [tokens]. Where a position is outside of 0 .. positions - 1, the rotated
+ * channels are NaN. rot may be 0 (position and table NULL), k_heads may be 0 (k, yk NULL). weights have dim elements of
+ * `type`. yq may be q, and yk k, with its strides: in place. */
+enum { AQD_PAIRS_HALVES = 0, AQD_PAIRS_NEIGHBOURS = 1 };
+typedef struct {
+    int tokens, q_heads, k_heads;   /* q_heads >= 1; tokens * (q_heads + k_heads) <= INT32_MAX */
+    int dim, rot;                   /* even, 2 <= dim <= 1024, 0 <= rot <= dim */
+    int pairs, type, positions;
+    float eps;                      /* finite, >= 0 */
+    int64_t q_token, q_head, k_token, k_head, yq_token, yq_head, yk_token, yk_head;
+} aqd_heads_desc_t;
+aqd_status_t aqd_heads_run(const aqd_heads_desc_t *desc, const void *q, const void *k, const void *q_weight, const void *k_weight,
+                           const int32_t *position, const float *table, void *yq, void *yk, aqd_stream_t stream);
+
+/* A cache of keys and values in 4 bits. Channels are quantised in groups of one token and head:
+ *   a = the element of largest magnitude (the positive one where both signs have it)
+ *   s = -a / 8 rounded to bf16, 0 where that is below 2^-119
+ *   code[c] = min(max(rint(x[c] * (1 / s)), -8), 7) + 8, 8 where s is 0     (fp32 operations)
+ * and a code stands for s * (code - 8): the largest element exactly but for the rounding of s, the others within |s| / 2
+ * of themselves, or |s| (1 + 2^-5) where one of the other sign is nearly as large. A group that holds an infinity or a NaN has codes 8
+ * and the scale NaN (0x7FC0).
+ *
+ * The cache is one buffer of qcache_bytes, 16-byte aligned, of `pages` pages of `page` tokens; a token's slot
+ * is its page's number * page + its place in the page. A page has one block per head: of its tokens
+ * the keys' codes (page * dim / 2 bytes), the values' codes, then the keys' scales [page][dim / group] and the
+ * values'. Of a token's key channels 8 w .. 8 w + 7 make the 32-bit word w, channels 2 j and 2 j + 1 in the nibbles (4 bits from the
+ * lowest on) j and j + 4; word w stands at place (w % 4) * dim / 32 + w / 4 of the token's dim / 8. Values: 16-bit
+ * units [page / 4][16][dim / 64][4], unit (t / 4, m, h, t % 4) has in its nibble n channel
+ * 64 h + 16 n + m of token t. That is the order the attention's operands have, so that it loads 16 bytes at a time and no
+ * code has to change lanes; programs that fill pages otherwise than by qcache_write keep to it. */
+typedef struct {
+    int heads;        /* >= 1 */
+    int dim, group;   /* 64, 128 or 256; 32, 64 or 128, at most dim */
+    int page, pages;  /* 16, 32, 64, 128 or 256 tokens; >= 0, pages * page <= INT32_MAX */
+} qcache_desc_t;
+aqd_status_t qcache_bytes(const qcache_desc_t *desc, size_t *bytes);
+
+/* Quantises the tokens of k and v into the cache, token t into slot slots[t] (int32 [tokens]); a token whose slot
+ * is outside of the cache (-1, say) is left out. Slots of one call must differ: one that is named twice holds a mixture of its
+ * tokens. Other slots are not changed. */
+typedef struct {
+    qcache_desc_t cache;
+    int tokens, type;
+    int64_t k_token, k_head, v_token, v_head;
+} qcache_rows_desc_t;
+aqd_status_t qcache_write(const qcache_rows_desc_t *desc, const void *k, const void *v, const int32_t *slots, void *cache,
+                          aqd_stream_t stream);
+/* The reverse: what the slots' codes stand for, rounded to `type`, into k and v. Rows of tokens whose slot is outside of the
+ * cache are left as they were; slots may repeat. */
+aqd_status_t qcache_read(const qcache_rows_desc_t *desc, const void *cache, const int32_t *slots, void *k, void *v, aqd_stream_t stream);
+
+/* Attention over the cache, causal: sequence b has lengths[b] tokens in the cache, in the pages that
+ * tables[b * ld_table + i] names (int32), and its queries are rows q_start[b] .. q_start[b + 1] - 1 of q (int32 [batch + 1];
+ * NULL: one query a sequence, queries == batch). With n queries, the i-th sees the first
+ * lengths[b] - n + 1 + i tokens, and
+ *   y = sum over those of softmax(scale * q . k) v
+ * for query head h with key head h / (q_heads / heads). A query that sees no token (an empty sequence) has zeros. Rows of
+ * q outside of every sequence are left as they were. fp32 scores and sums; the weights times the values' scales are rounded to
+ * `type` for the matrix product: each term within half a unit of its last place.
+ * max_queries and max_keys bound the sequences' queries and lengths, which sizes the launch; of a longer sequence
+ * the first max_queries queries and max_keys tokens count (and no more than ld_table pages). Queries that see a token whose page
+ * number is outside of 0 .. pages - 1 are NaN. What lies in a page past a sequence's end does not matter.
+ * q, y: AQD_F16 or AQD_BF16 (UNSUPPORTED: AQD_F32), [queries][q_heads][dim].
+ *
+ * workspace (device, 16-byte aligned, ws_bytes): with it, the tokens of long sequences are split between workgroups, which
+ * is what makes few sequences fast. qattn_workspace gives the size for a call (never more than AQD_ATTN_WORKSPACE_BYTES); with
+ * less, or NULL, the launch splits less or not at all. Calls that share a workspace must not overlap in time. */
+#define AQD_ATTN_WORKSPACE_BYTES (64u << 20)
+typedef struct {
+    qcache_desc_t cache;
+    int batch, q_heads;               /* q_heads a multiple of cache.heads */
+    int queries, max_queries, max_keys;
+    int type;
+    float scale;                      /* finite */
+    int64_t ld_table;                 /* >= 1 where batch > 1 */
+    int64_t q_token, q_head, y_token, y_head;
+} qattn_desc_t;
+aqd_status_t qattn_workspace(const qattn_desc_t *desc, size_t *bytes);
+aqd_status_t qattn_run(const qattn_desc_t *desc, const void *q, const int32_t *q_start, const void *cache, const int32_t *tables,
+                       const int32_t *lengths, void *y, void *workspace, size_t ws_bytes, aqd_stream_t stream);
+
+/* Attention over keys and values in memory, for whole prompts of packed sequences: sequence b's queries are rows
+ * q_start[b] .. q_start[b + 1] - 1 of q, its keys and values rows k_start[b] .. k_start[b + 1] - 1 (int32 [batch + 1] each);
+ * with n queries and m keys the i-th query sees all m keys, or with causal set the first m - n + 1 + i (prompts that continue
+ * what was read before have more keys than queries). Scores, heads, zeros, rows outside and rounding as qattn_run's; the weights are
+ * rounded to `type` for the product with v. What a query does not see has no part in its result,
+ * infinities and NaN included. max_queries and max_keys bound the sequences' rows, which sizes the launch; of a longer
+ * sequence the first max_queries queries and all keys count. Starts are taken as if within 0 .. queries and 0 .. keys,
+ * and a sequence whose start lies behind its end as empty; no row of q may be two sequences'.
+ * dim: a multiple of 8 up to 256 (UNSUPPORTED above); AQD_F16 or AQD_BF16 (UNSUPPORTED: AQD_F32).
+ * workspace as qattn_run's (aqd_attn_workspace): few queries over many keys are split. */
+typedef struct {
+    int batch, q_heads, heads, dim;   /* q_heads a multiple of heads */
+    int queries, keys, max_queries, max_keys;
+    int causal, type;
+    float scale;                      /* finite */
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head, y_token, y_head;
+} aqd_attn_desc_t;
+aqd_status_t aqd_attn_workspace(const aqd_attn_desc_t *desc, size_t *bytes);
+aqd_status_t aqd_attn_run(const aqd_attn_desc_t *desc, const void *q, const void *k, const void *v, const int32_t *q_start,
+                          const int32_t *k_start, void *y, void *workspace, size_t ws_bytes, aqd_stream_t stream);
+
 /* Diagnostic for measurements (the benchmark's measured ceiling next to the
  * dense int8 peak figure): launches `workgroups` workgroups of 4 waves,
  * each wave issuing iters x 16 independent 16x16x64 int8 MFMAs on register

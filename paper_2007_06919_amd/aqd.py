@@ -24,6 +24,8 @@ MAX_SEGS = 16
 F32, F16, BF16 = 0, 1, 2
 QLIN_PLAIN, QLIN_SILU_GATE = 0, 1
 QLIN_WORKSPACE_BYTES = 64 << 20
+PAIRS_HALVES, PAIRS_NEIGHBOURS = 0, 1
+ATTN_WORKSPACE_BYTES = 64 << 20
 
 STATUS_NAMES = {0: "AQD_OK", 1: "AQD_ERR_INVALID", 2: "AQD_ERR_UNSUPPORTED",
                 3: "AQD_ERR_NOMEM", 4: "AQD_ERR_DEVICE"}
@@ -76,6 +78,33 @@ class QlinDesc(ctypes.Structure):
                [(n, c_int64) for n in ("ld_x", "ld_w", "ld_y")]
 
 
+class HeadsDesc(ctypes.Structure):
+    _fields_ = [(n, c_int) for n in ("tokens", "q_heads", "k_heads", "dim", "rot", "pairs", "type", "positions")] + \
+               [("eps", c_float)] + \
+               [(n, c_int64) for n in ("q_token", "q_head", "k_token", "k_head", "yq_token", "yq_head", "yk_token", "yk_head")]
+
+
+class QcacheDesc(ctypes.Structure):
+    _fields_ = [(n, c_int) for n in ("heads", "dim", "group", "page", "pages")]
+
+
+class QcacheRowsDesc(ctypes.Structure):
+    _fields_ = [("cache", QcacheDesc)] + [(n, c_int) for n in ("tokens", "type")] + \
+               [(n, c_int64) for n in ("k_token", "k_head", "v_token", "v_head")]
+
+
+class QattnDesc(ctypes.Structure):
+    _fields_ = [("cache", QcacheDesc)] + \
+               [(n, c_int) for n in ("batch", "q_heads", "queries", "max_queries", "max_keys", "type")] + [("scale", c_float)] + \
+               [(n, c_int64) for n in ("ld_table", "q_token", "q_head", "y_token", "y_head")]
+
+
+class AttnDesc(ctypes.Structure):
+    _fields_ = [(n, c_int) for n in ("batch", "q_heads", "heads", "dim", "queries", "keys", "max_queries", "max_keys", "causal", "type")] + \
+               [("scale", c_float)] + \
+               [(n, c_int64) for n in ("q_token", "q_head", "k_token", "k_head", "v_token", "v_head", "y_token", "y_head")]
+
+
 class QaddParams(ctypes.Structure):
     _fields_ = [(n, c_void_p) for n in ("skip_c", "skip_d", "skip_side", "mult", "shift")]
 
@@ -109,6 +138,14 @@ def lib():
             "qnorm_run": ([POINTER(QnormDesc), vp, vp, vp, vp, vp, vp, vp], st),
             "qlin_workspace": ([POINTER(QlinDesc), POINTER(ctypes.c_size_t)], st),
             "qlin_run": ([POINTER(QlinDesc), vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp], st),
+            "aqd_heads_run": ([POINTER(HeadsDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp], st),
+            "qcache_bytes": ([POINTER(QcacheDesc), POINTER(ctypes.c_size_t)], st),
+            "qcache_write": ([POINTER(QcacheRowsDesc), vp, vp, vp, vp, vp], st),
+            "qcache_read": ([POINTER(QcacheRowsDesc), vp, vp, vp, vp, vp], st),
+            "qattn_workspace": ([POINTER(QattnDesc), POINTER(ctypes.c_size_t)], st),
+            "qattn_run": ([POINTER(QattnDesc), vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp], st),
+            "aqd_attn_workspace": ([POINTER(AttnDesc), POINTER(ctypes.c_size_t)], st),
+            "aqd_attn_run": ([POINTER(AttnDesc), vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp], st),
             "aqd_mfma_probe": ([i, i, vp, vp], st),
             "aqd_graph_begin": ([vp], st),
             "aqd_graph_end": ([vp, POINTER(c_void_p)], st),
@@ -137,6 +174,8 @@ def exported_symbols():
             "qconv_group_workspace", "qconv_run_group_ws", "qconv_run_group_static",
             "qconv_run_proj", "qconv_destroy", "qconv_path",
             "qadd_run", "aqd_maxpool_run", "qrows_run", "qnorm_run", "qlin_workspace", "qlin_run",
+            "aqd_heads_run", "qcache_bytes", "qcache_write", "qcache_read", "qattn_workspace", "qattn_run",
+            "aqd_attn_workspace", "aqd_attn_run",
             "aqd_mfma_probe", "aqd_channel_sums", "aqd_graph_begin", "aqd_graph_end",
             "aqd_graph_launch", "aqd_graph_destroy", "aqd_last_error", "aqd_pack_codes",
             "aqd_unpack_codes", "aqd_approx_ratio", "aqd_normalize_multiplier",
@@ -331,6 +370,71 @@ def qlin_run(rows, n, k, type, act, x, ld_x, x_scales, w, ld_w, w_scales, bias, 
     d = QlinDesc(rows, n, k, type, act, ld_x, ld_w, ld_y)
     _check(lib().qlin_run(ctypes.byref(d), _addr(x), _addr(x_scales), _addr(w), _addr(w_scales), _addr(bias), _addr(y),
                           _addr(workspace), ws_bytes, _stream(stream)))
+
+
+# --------------------------------------------------------------- attention
+def heads_run(tokens, q_heads, k_heads, dim, rot, pairs, type, positions, eps, q, q_token, q_head, k, k_token, k_head,
+              q_weight, k_weight, position, table, yq, yq_token, yq_head, yk, yk_token, yk_head, stream=None):
+    """Norm of each query and key head and its rotation by position (see aqd.h). A weight may be None (no norm); yq may be
+    q and yk k; k may be None with k_heads 0, position and table with rot 0."""
+    d = HeadsDesc(tokens, q_heads, k_heads, dim, rot, pairs, type, positions, eps, q_token, q_head, k_token, k_head, yq_token,
+                  yq_head, yk_token, yk_head)
+    _check(lib().aqd_heads_run(ctypes.byref(d), _addr(q), _addr(k), _addr(q_weight), _addr(k_weight), _addr(position),
+                               _addr(table), _addr(yq), _addr(yk), _stream(stream)))
+
+
+def qcache_bytes(cache: QcacheDesc) -> int:
+    """Bytes of a 4-bit cache of keys and values: QcacheDesc(heads, dim, group, page, pages)."""
+    b = ctypes.c_size_t(0)
+    _check(lib().qcache_bytes(ctypes.byref(cache), ctypes.byref(b)))
+    return b.value
+
+
+def qcache_write(cache, tokens, type, k, k_token, k_head, v, v_token, v_head, slots, data, stream=None):
+    """Keys and values into the slots of a 4-bit cache (see aqd.h)."""
+    d = QcacheRowsDesc(cache, tokens, type, k_token, k_head, v_token, v_head)
+    _check(lib().qcache_write(ctypes.byref(d), _addr(k), _addr(v), _addr(slots), _addr(data), _stream(stream)))
+
+
+def qcache_read(cache, tokens, type, data, slots, k, k_token, k_head, v, v_token, v_head, stream=None):
+    """Keys and values out of the slots of a 4-bit cache (see aqd.h)."""
+    d = QcacheRowsDesc(cache, tokens, type, k_token, k_head, v_token, v_head)
+    _check(lib().qcache_read(ctypes.byref(d), _addr(data), _addr(slots), _addr(k), _addr(v), _stream(stream)))
+
+
+def qattn_workspace(cache, batch, q_heads, queries, max_queries, max_keys, type) -> int:
+    """Workspace bytes with which qattn_run splits long sequences (0: it does not; at most ATTN_WORKSPACE_BYTES)."""
+    row = q_heads * cache.dim
+    d = QattnDesc(cache, batch, q_heads, queries, max_queries, max_keys, type, 1.0, 1, row, cache.dim, row, cache.dim)
+    b = ctypes.c_size_t(0)
+    _check(lib().qattn_workspace(ctypes.byref(d), ctypes.byref(b)))
+    return b.value
+
+
+def qattn_run(cache, batch, q_heads, queries, max_queries, max_keys, type, scale, q, q_token, q_head, q_start, data, tables,
+              ld_table, lengths, y, y_token, y_head, workspace=None, ws_bytes=0, stream=None):
+    """Attention over a 4-bit cache (see aqd.h; q_start None: one query a sequence)."""
+    d = QattnDesc(cache, batch, q_heads, queries, max_queries, max_keys, type, scale, ld_table, q_token, q_head, y_token, y_head)
+    _check(lib().qattn_run(ctypes.byref(d), _addr(q), _addr(q_start), _addr(data), _addr(tables), _addr(lengths), _addr(y),
+                           _addr(workspace), ws_bytes, _stream(stream)))
+
+
+def attn_workspace(batch, q_heads, heads, dim, queries, keys, max_queries, max_keys, causal, type) -> int:
+    """Workspace bytes with which attn_run splits the keys (0: it does not; at most ATTN_WORKSPACE_BYTES)."""
+    d = AttnDesc(batch, q_heads, heads, dim, queries, keys, max_queries, max_keys, int(causal), type, 1.0,
+                 q_heads * dim, dim, heads * dim, dim, heads * dim, dim, q_heads * dim, dim)
+    b = ctypes.c_size_t(0)
+    _check(lib().aqd_attn_workspace(ctypes.byref(d), ctypes.byref(b)))
+    return b.value
+
+
+def attn_run(batch, q_heads, heads, dim, queries, keys, max_queries, max_keys, causal, type, scale, q, q_token, q_head,
+             k, k_token, k_head, v, v_token, v_head, q_start, k_start, y, y_token, y_head, workspace=None, ws_bytes=0, stream=None):
+    """Attention over the keys and values of packed sequences (see aqd.h)."""
+    d = AttnDesc(batch, q_heads, heads, dim, queries, keys, max_queries, max_keys, int(causal), type, scale, q_token, q_head,
+                 k_token, k_head, v_token, v_head, y_token, y_head)
+    _check(lib().aqd_attn_run(ctypes.byref(d), _addr(q), _addr(k), _addr(v), _addr(q_start), _addr(k_start), _addr(y),
+                              _addr(workspace), ws_bytes, _stream(stream)))
 
 
 def mfma_probe(workgroups, iters, out, stream=None):

@@ -1950,6 +1950,356 @@ aqd_status_t qlin_run(const qlin_desc_t *d, const int8_t *x, const float *x_scal
     return AQD_OK;
 }
 
+}  // extern "C"
+
+// ------------------------------------------------------------------ attention
+namespace {
+
+// a tensor [tokens][heads][dim] as rows of its larger stride
+struct Rows3 {
+    Span outer;
+    long long step, width;   // of the smaller stride, and of dim elements, bytes
+};
+
+// Strides of a dimension with one entry are ignored (and set to what a packed tensor has); false for strides by which two
+// elements could be one, or the tensor leave the address space.
+bool strides_ok(long long &token, long long &head, long long tokens, long long heads, long long dim)
+{
+    const auto fits = [](long long stride, long long count) { return stride <= (INT64_C(1) << 56) / std::max(count, 1LL); };
+    if (heads <= 1)
+        head = dim;
+    if (!fits(head, heads))
+        return false;
+    if (tokens <= 1)
+        token = std::max((heads - 1) * head + dim, head);
+    if (!fits(token, tokens))
+        return false;
+    const bool by_token = token >= head;
+    const long long inner = by_token ? head : token, outer = by_token ? token : head, n = by_token ? heads : tokens;
+    return inner >= dim && (outer >= (n - 1) * inner + dim || (by_token ? tokens : heads) <= 1);
+}
+
+Rows3 rows3(const void *p, long long token, long long head, long long tokens, long long heads, long long dim, int size)
+{
+    const bool by_token = token >= head;
+    const long long inner = by_token ? head : token, outer = by_token ? token : head, n = by_token ? heads : tokens;
+    return {{(uintptr_t)p, outer * size, ((n - 1) * inner + dim) * size, by_token ? tokens : heads}, inner * size, dim * size};
+}
+
+bool share(const Rows3 &a, const Rows3 &b)
+{
+    if (!share(a.outer, b.outer))
+        return false;
+    // rows of one make whose heads (or tokens) lie between one another
+    if (a.step != b.step || a.outer.ld != b.outer.ld || a.outer.ld % a.step)
+        return true;
+    const uintptr_t step = (uintptr_t)a.step, x = a.outer.at, y = b.outer.at;
+    const long long gap = (long long)(y >= x ? (y - x) % step : (step - (x - y) % step) % step);   // b's first element, within a step of a
+    return gap < a.width || gap + b.width > a.step;
+}
+
+bool share(const Rows3 &a, const Span &b) { return share(a.outer, b); }
+
+Span bytes_of(const void *p, long long n) { return {(uintptr_t)p, n, n, n > 0}; }
+
+aqd_status_t cache_shape(const qcache_desc_t &d, QcacheShape &c)
+{
+    REQUIRE(d.heads >= 1 && d.heads <= 65535, "heads must be 1 to 65535");
+    REQUIRE(d.dim == 64 || d.dim == 128 || d.dim == 256, "dim must be 64, 128 or 256");
+    REQUIRE((d.group == 32 || d.group == 64 || d.group == 128) && d.group <= d.dim, "group must be 32, 64 or 128, and at most dim");
+    REQUIRE(d.page >= 16 && d.page <= 256 && !(d.page & (d.page - 1)), "page must be 16, 32, 64, 128 or 256");
+    REQUIRE(d.pages >= 0 && d.pages <= INT32_MAX / d.page, "pages must be at least 0, and slots fit an int32");
+    c = {d.heads, d.dim, d.group, d.page, d.pages, (long long)d.page * (d.dim + 4 * (d.dim / d.group))};
+    return AQD_OK;
+}
+
+long long cache_bytes(const QcacheShape &c) { return c.block_bytes * c.heads * c.pages; }
+
+aqd_status_t cache_rows(const qcache_rows_desc_t *d, const void *k, const void *v, const int32_t *slots, const void *cache, bool write,
+                        QcacheArgs &a)
+{
+    REQUIRE(d, "null description");
+    const aqd_status_t st = cache_shape(d->cache, a.c);
+    if (st != AQD_OK)
+        return st;
+    const int size = real_size(d->type);
+    REQUIRE(size, "type must be AQD_F32, AQD_F16 or AQD_BF16");
+    REQUIRE(d->tokens >= 0 && (long long)d->tokens * d->cache.heads <= INT32_MAX, "tokens must be at least 0, and not too many");
+    a.tokens = d->tokens;
+    a.type = d->type;
+    a.k_token = d->k_token, a.k_head = d->k_head, a.v_token = d->v_token, a.v_head = d->v_head;
+    if (!a.tokens)
+        return AQD_OK;
+    REQUIRE(strides_ok(a.k_token, a.k_head, a.tokens, a.c.heads, a.c.dim) && strides_ok(a.v_token, a.v_head, a.tokens, a.c.heads, a.c.dim),
+            "strides of k or v by which elements could share memory, or too large");
+    if (!a.c.pages)
+        return AQD_OK;   // no slot is inside the cache
+    REQUIRE(k && v && slots && cache, "null pointer");
+    REQUIRE(aligned_to(k, size) && aligned_to(v, size) && aligned_to(slots, 4), "a pointer is not aligned to its elements");
+    REQUIRE(aligned16(cache), "the cache must be 16-byte aligned");
+    const Rows3 rk = rows3(k, a.k_token, a.k_head, a.tokens, a.c.heads, a.c.dim, size);
+    const Rows3 rv = rows3(v, a.v_token, a.v_head, a.tokens, a.c.heads, a.c.dim, size);
+    const Span s = bytes_of(slots, 4LL * a.tokens), c = bytes_of(cache, cache_bytes(a.c));
+    REQUIRE(!share(rk, c) && !share(rv, c), "the cache overlaps k or v");
+    REQUIRE(write ? !share(c, s) : !share(rk, s) && !share(rv, s) && !share(rk, rv), "an output overlaps another tensor");
+    a.k = const_cast<void *>(k);
+    a.v = const_cast<void *>(v);
+    a.slots = slots;
+    a.cache = (uint8_t *)const_cast<void *>(cache);
+    return AQD_OK;
+}
+
+aqd_status_t attn_type(int type)
+{
+    REQUIRE(real_size(type), "type must be AQD_F32, AQD_F16 or AQD_BF16");
+    if (type == AQD_F32)
+        return fail(AQD_ERR_UNSUPPORTED, "attention takes 16-bit types");
+    return AQD_OK;
+}
+
+aqd_status_t qattn_args(const qattn_desc_t *d, QattnArgs &a)
+{
+    REQUIRE(d, "null description");
+    aqd_status_t st = cache_shape(d->cache, a.c);
+    if (st == AQD_OK)
+        st = attn_type(d->type);
+    if (st != AQD_OK)
+        return st;
+    REQUIRE(d->batch >= 0 && d->queries >= 0 && d->max_queries >= 0 && d->max_keys >= 0, "a negative count");
+    REQUIRE(d->q_heads >= 1 && d->q_heads <= 65535 && d->q_heads % d->cache.heads == 0, "q_heads must be a multiple of the cache's heads, up to 65535");
+    REQUIRE(std::isfinite(d->scale), "scale must be finite");
+    a.batch = d->batch, a.q_heads = d->q_heads, a.queries = d->queries, a.type = d->type, a.scale = d->scale;
+    a.max_queries = std::min(d->max_queries, d->queries);
+    a.max_keys = d->max_keys;
+    REQUIRE(a.max_keys <= INT32_MAX - 65536, "too many keys");
+    REQUIRE((long long)a.queries * a.q_heads <= INT32_MAX - 65536 && (double)a.batch * a.q_heads * (a.max_queries + 16.0) <= INT32_MAX - 65536,
+            "too many queries");
+    a.q_token = d->q_token, a.q_head = d->q_head, a.y_token = d->y_token, a.y_head = d->y_head, a.ld_table = d->ld_table;
+    REQUIRE(strides_ok(a.q_token, a.q_head, a.queries, a.q_heads, a.c.dim) && strides_ok(a.y_token, a.y_head, a.queries, a.q_heads, a.c.dim),
+            "strides of q or y by which elements could share memory, or too large");
+    REQUIRE(a.ld_table >= (a.batch > 1) && a.ld_table <= INT32_MAX, "ld_table must be at least 1, and fit an int32");
+    if (a.batch <= 1 && a.ld_table < 1)
+        a.ld_table = (a.max_keys + a.c.page - 1) / a.c.page;
+    return AQD_OK;
+}
+
+aqd_status_t attn_args(const aqd_attn_desc_t *d, AttnArgs &a)
+{
+    REQUIRE(d, "null description");
+    const aqd_status_t st = attn_type(d->type);
+    if (st != AQD_OK)
+        return st;
+    REQUIRE(d->batch >= 0 && d->queries >= 0 && d->keys >= 0 && d->max_queries >= 0 && d->max_keys >= 0, "a negative count");
+    REQUIRE(d->heads >= 1 && d->q_heads >= 1 && d->q_heads <= 65535 && d->q_heads % d->heads == 0, "q_heads must be a multiple of heads, up to 65535");
+    REQUIRE(d->dim >= 1, "dim must be at least 1");
+    REQUIRE(d->causal == 0 || d->causal == 1, "causal must be 0 or 1");
+    REQUIRE(std::isfinite(d->scale), "scale must be finite");
+    if (d->dim % 8 || d->dim > 256)
+        return fail(AQD_ERR_UNSUPPORTED, "dim must be a multiple of 8 up to 256");
+    a.batch = d->batch, a.q_heads = d->q_heads, a.heads = d->heads, a.dim = d->dim, a.queries = d->queries, a.keys = d->keys;
+    a.max_queries = std::min(d->max_queries, d->queries);
+    a.max_keys = std::min(d->max_keys, d->keys);
+    a.causal = d->causal, a.type = d->type, a.scale = d->scale;
+    REQUIRE(a.keys <= INT32_MAX - 65536 && (long long)a.queries * a.q_heads <= INT32_MAX - 65536 &&
+                (double)a.batch * a.q_heads * (a.max_queries + 16.0) <= INT32_MAX - 65536, "too many queries or keys");
+    a.q_token = d->q_token, a.q_head = d->q_head, a.k_token = d->k_token, a.k_head = d->k_head;
+    a.v_token = d->v_token, a.v_head = d->v_head, a.y_token = d->y_token, a.y_head = d->y_head;
+    REQUIRE(strides_ok(a.q_token, a.q_head, a.queries, a.q_heads, a.dim) && strides_ok(a.k_token, a.k_head, a.keys, a.heads, a.dim) &&
+                strides_ok(a.v_token, a.v_head, a.keys, a.heads, a.dim) && strides_ok(a.y_token, a.y_head, a.queries, a.q_heads, a.dim),
+            "strides by which elements could share memory, or too large");
+    return AQD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+aqd_status_t aqd_heads_run(const aqd_heads_desc_t *d, const void *q, const void *k, const void *q_weight, const void *k_weight,
+                           const int32_t *position, const float *table, void *yq, void *yk, aqd_stream_t stream)
+{
+    REQUIRE(d, "null description");
+    const int size = real_size(d->type);
+    REQUIRE(size, "type must be AQD_F32, AQD_F16 or AQD_BF16");
+    REQUIRE(d->tokens >= 0 && d->q_heads >= 1 && d->k_heads >= 0, "tokens and k_heads must be at least 0, q_heads at least 1");
+    REQUIRE((double)d->tokens * ((double)d->q_heads + d->k_heads) <= INT32_MAX, "too many heads");
+    REQUIRE(d->dim >= 2 && d->dim <= 1024 && d->dim % 2 == 0, "dim must be even, 2 to 1024");
+    REQUIRE(d->rot >= 0 && d->rot <= d->dim && d->rot % 2 == 0, "rot must be even, 0 to dim");
+    REQUIRE(d->pairs == AQD_PAIRS_HALVES || d->pairs == AQD_PAIRS_NEIGHBOURS, "unknown pairs");
+    REQUIRE(std::isfinite(d->eps) && d->eps >= 0.f, "eps must be finite and not negative");
+    REQUIRE(d->positions >= 0, "positions must be at least 0");
+    HeadsArgs a = {};
+    a.q = {q, q_weight, yq, d->q_token, d->q_head, d->yq_token, d->yq_head};
+    a.k = {k, k_weight, yk, d->k_token, d->k_head, d->yk_token, d->yk_head};
+    a.position = position;
+    a.table = table;
+    a.tokens = d->tokens, a.q_heads = d->q_heads, a.heads = d->q_heads + d->k_heads;
+    a.dim = d->dim, a.rot = d->rot, a.pairs = d->pairs, a.type = d->type, a.positions = d->positions, a.eps = d->eps;
+    if (!a.tokens)
+        return AQD_OK;
+    REQUIRE(strides_ok(a.q.token, a.q.head, a.tokens, d->q_heads, a.dim) && strides_ok(a.q.y_token, a.q.y_head, a.tokens, d->q_heads, a.dim),
+            "strides of q or yq by which elements could share memory, or too large");
+    REQUIRE(q && yq && (!a.rot || (position && (table || !a.positions))), "null pointer");
+    REQUIRE(aligned_to(q, size) && aligned_to(yq, size) && aligned_to(q_weight, size) && aligned_to(k_weight, size) &&
+                aligned_to(position, 4) && aligned_to(table, 4), "a pointer is not aligned to its elements");
+    const Rows3 x = rows3(q, a.q.token, a.q.head, a.tokens, d->q_heads, a.dim, size);
+    const Rows3 y = rows3(yq, a.q.y_token, a.q.y_head, a.tokens, d->q_heads, a.dim, size);
+    const Span rest[] = {bytes_of(q_weight, a.dim * size), bytes_of(k_weight, d->k_heads ? a.dim * size : 0),
+                         bytes_of(position, a.rot ? 4LL * a.tokens : 0), bytes_of(table, 4LL * a.positions * a.rot)};
+    REQUIRE((yq == q && a.q.token == a.q.y_token && a.q.head == a.q.y_head) || !share(y, x), "yq overlaps q, and is not in its place");
+    for (const Span &s : rest)
+        REQUIRE(!share(y, s), "yq overlaps an input");
+    if (d->k_heads) {
+        REQUIRE(strides_ok(a.k.token, a.k.head, a.tokens, d->k_heads, a.dim) && strides_ok(a.k.y_token, a.k.y_head, a.tokens, d->k_heads, a.dim),
+                "strides of k or yk by which elements could share memory, or too large");
+        REQUIRE(k && yk, "null pointer");
+        REQUIRE(aligned_to(k, size) && aligned_to(yk, size), "a pointer is not aligned to its elements");
+        const Rows3 xk = rows3(k, a.k.token, a.k.head, a.tokens, d->k_heads, a.dim, size);
+        const Rows3 z = rows3(yk, a.k.y_token, a.k.y_head, a.tokens, d->k_heads, a.dim, size);
+        REQUIRE((yk == k && a.k.token == a.k.y_token && a.k.head == a.k.y_head) || !share(z, xk), "yk overlaps k, and is not in its place");
+        REQUIRE(!share(y, xk) && !share(z, x) && !share(y, z), "yq and yk overlap one another, or each other's inputs");
+        for (const Span &s : rest)
+            REQUIRE(!share(z, s), "yk overlaps an input");
+    }
+    if (launch_heads(a, (hipStream_t)stream) != hipSuccess)
+        return fail(AQD_ERR_DEVICE, "head norm launch failed");
+    return AQD_OK;
+}
+
+aqd_status_t qcache_bytes(const qcache_desc_t *d, size_t *bytes)
+{
+    REQUIRE(d && bytes, "null description or output pointer");
+    QcacheShape c;
+    const aqd_status_t st = cache_shape(*d, c);
+    if (st != AQD_OK)
+        return st;
+    *bytes = (size_t)cache_bytes(c);
+    return AQD_OK;
+}
+
+aqd_status_t qcache_write(const qcache_rows_desc_t *d, const void *k, const void *v, const int32_t *slots, void *cache, aqd_stream_t stream)
+{
+    QcacheArgs a = {};
+    const aqd_status_t st = cache_rows(d, k, v, slots, cache, true, a);
+    if (st != AQD_OK || !a.tokens || !a.c.pages)
+        return st;
+    if (launch_qcache_write(a, (hipStream_t)stream) != hipSuccess)
+        return fail(AQD_ERR_DEVICE, "cache write launch failed");
+    return AQD_OK;
+}
+
+aqd_status_t qcache_read(const qcache_rows_desc_t *d, const void *cache, const int32_t *slots, void *k, void *v, aqd_stream_t stream)
+{
+    QcacheArgs a = {};
+    const aqd_status_t st = cache_rows(d, k, v, slots, cache, false, a);
+    if (st != AQD_OK || !a.tokens || !a.c.pages)
+        return st;
+    if (launch_qcache_read(a, (hipStream_t)stream) != hipSuccess)
+        return fail(AQD_ERR_DEVICE, "cache read launch failed");
+    return AQD_OK;
+}
+
+aqd_status_t qattn_workspace(const qattn_desc_t *d, size_t *bytes)
+{
+    REQUIRE(bytes, "null output pointer");
+    QattnArgs a = {};
+    const aqd_status_t st = qattn_args(d, a);
+    if (st != AQD_OK)
+        return st;
+    *bytes = a.batch && a.max_queries ? qattn_plan(a, AQD_ATTN_WORKSPACE_BYTES).bytes : 0;
+    return AQD_OK;
+}
+
+aqd_status_t qattn_run(const qattn_desc_t *d, const void *q, const int32_t *q_start, const void *cache, const int32_t *tables,
+                       const int32_t *lengths, void *y, void *workspace, size_t ws_bytes, aqd_stream_t stream)
+{
+    QattnArgs a = {};
+    const aqd_status_t st = qattn_args(d, a);
+    if (st != AQD_OK || !a.batch || !a.max_queries)
+        return st;
+    REQUIRE(q && y && lengths, "null pointer");
+    REQUIRE(q_start || a.queries == a.batch, "without q_start there is one query a sequence");
+    REQUIRE((cache && tables) || !a.max_keys || !a.c.pages, "null pointer");
+    REQUIRE(tables || !a.max_keys, "null pointer");
+    REQUIRE(aligned_to(q, 2) && aligned_to(y, 2) && aligned_to(q_start, 4) && aligned_to(tables, 4) && aligned_to(lengths, 4),
+            "a pointer is not aligned to its elements");
+    REQUIRE(aligned16(cache) && aligned16(workspace), "the cache and the workspace must be 16-byte aligned");
+    const Rows3 out = rows3(y, a.y_token, a.y_head, a.queries, a.q_heads, a.c.dim, 2);
+    const Rows3 in = rows3(q, a.q_token, a.q_head, a.queries, a.q_heads, a.c.dim, 2);
+    const Span rest[] = {bytes_of(q_start, 4LL * (a.batch + 1)), bytes_of(lengths, 4LL * a.batch),
+                         bytes_of(cache, cache_bytes(a.c)), bytes_of(tables, 4LL * a.batch * a.ld_table)};
+    REQUIRE(!share(out, in), "y overlaps q");
+    for (const Span &s : rest)
+        REQUIRE(!share(out, s), "y overlaps an input");
+    a.q = q;
+    a.y = y;
+    a.q_start = q_start;
+    a.cache = (const uint8_t *)cache;
+    a.tables = tables;
+    a.lengths = lengths;
+    a.part = (float *)workspace;
+    const AttnPlan plan = qattn_plan(a, workspace ? std::min<size_t>(ws_bytes, AQD_ATTN_WORKSPACE_BYTES) : 0);
+    if (plan.bytes) {
+        const Span ws = bytes_of(workspace, (long long)plan.bytes);
+        REQUIRE(!share(out, ws) && !share(in, ws), "the workspace overlaps q or y");
+        for (const Span &s : rest)
+            REQUIRE(!share(ws, s), "the workspace overlaps an input");
+    }
+    if (launch_qattn(a, plan, (hipStream_t)stream) != hipSuccess)
+        return fail(AQD_ERR_DEVICE, "attention launch failed");
+    return AQD_OK;
+}
+
+aqd_status_t aqd_attn_workspace(const aqd_attn_desc_t *d, size_t *bytes)
+{
+    REQUIRE(bytes, "null output pointer");
+    AttnArgs a = {};
+    const aqd_status_t st = attn_args(d, a);
+    if (st != AQD_OK)
+        return st;
+    *bytes = a.batch && a.max_queries ? attn_plan(a, AQD_ATTN_WORKSPACE_BYTES).bytes : 0;
+    return AQD_OK;
+}
+
+aqd_status_t aqd_attn_run(const aqd_attn_desc_t *d, const void *q, const void *k, const void *v, const int32_t *q_start,
+                          const int32_t *k_start, void *y, void *workspace, size_t ws_bytes, aqd_stream_t stream)
+{
+    AttnArgs a = {};
+    const aqd_status_t st = attn_args(d, a);
+    if (st != AQD_OK || !a.batch || !a.max_queries)
+        return st;
+    REQUIRE(q && y && q_start && k_start && ((k && v) || !a.keys), "null pointer");
+    REQUIRE(aligned_to(q, 2) && aligned_to(k, 2) && aligned_to(v, 2) && aligned_to(y, 2) && aligned_to(q_start, 4) && aligned_to(k_start, 4),
+            "a pointer is not aligned to its elements");
+    REQUIRE(aligned16(workspace), "the workspace must be 16-byte aligned");
+    const Rows3 out = rows3(y, a.y_token, a.y_head, a.queries, a.q_heads, a.dim, 2);
+    const Rows3 in[] = {rows3(q, a.q_token, a.q_head, a.queries, a.q_heads, a.dim, 2), rows3(k, a.k_token, a.k_head, a.keys, a.heads, a.dim, 2),
+                        rows3(v, a.v_token, a.v_head, a.keys, a.heads, a.dim, 2)};
+    const Span rest[] = {bytes_of(q_start, 4LL * (a.batch + 1)), bytes_of(k_start, 4LL * (a.batch + 1))};
+    for (const Rows3 &r : in)
+        REQUIRE(!share(out, r), "y overlaps an input");
+    for (const Span &s : rest)
+        REQUIRE(!share(out, s), "y overlaps an input");
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.y = y;
+    a.q_start = q_start;
+    a.k_start = k_start;
+    a.part = (float *)workspace;
+    const AttnPlan plan = attn_plan(a, workspace ? std::min<size_t>(ws_bytes, AQD_ATTN_WORKSPACE_BYTES) : 0);
+    if (plan.bytes) {
+        const Span ws = bytes_of(workspace, (long long)plan.bytes);
+        REQUIRE(!share(out, ws), "the workspace overlaps y");
+        for (const Rows3 &r : in)
+            REQUIRE(!share(r, ws), "the workspace overlaps an input");
+        for (const Span &s : rest)
+            REQUIRE(!share(ws, s), "the workspace overlaps an input");
+    }
+    if (launch_attn(a, plan, (hipStream_t)stream) != hipSuccess)
+        return fail(AQD_ERR_DEVICE, "attention launch failed");
+    return AQD_OK;
+}
+
 // ------------------------------------------------------------------ host helpers
 aqd_status_t aqd_pack_codes(const uint8_t *codes, int64_t rows, int c, int bits, uint8_t *out)
 {

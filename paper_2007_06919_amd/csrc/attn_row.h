@@ -1,0 +1,67 @@
+// Attention of one query by one wave, key by key, on the vector units: only what the
+// query sees is ever multiplied. Serves any rows; slow.
+#pragma once
+
+#include "internal.h"
+
+namespace aqd {
+namespace {
+
+// scratch of a wave in LDS: the query, and the weights of 64 keys
+struct RowScratch {
+    float q[256], p[64];
+};
+
+// query(c), key(j, c), value(j, c): element c of the query, and of key and value j; keys: what the query sees;
+// out(c, y) takes the results. Lanes of a wave in step; the scratch is the wave's own.
+template <int DIM, typename Query, typename Key, typename Value, typename Out>
+__device__ void row_attention(RowScratch &lds, int dim, int keys, float scale, Query query, Key key, Value value, Out out)
+{
+    const int lane = threadIdx.x & 63;
+    constexpr int V = (DIM + 63) / 64;
+    for (int c = lane; c < dim; c += 64)
+        lds.q[c] = query(c) * scale;
+    __builtin_amdgcn_wave_barrier();
+    float y[V] = {}, most = -INFINITY, total = 0.f;
+    for (int first = 0; first < keys; first += 64) {
+        const int j = first + lane;
+        float s = -INFINITY;
+        if (j < keys) {
+            s = 0.f;
+            for (int c = 0; c < dim; ++c)
+                s = __builtin_fmaf(lds.q[c], key(j, c), s);
+        }
+        float top = s;
+        for (int d = 32; d; d >>= 1)
+            top = fmaxf(top, __shfl_xor(top, d));
+        // -infinity while no score is above it: weights 0 until then (an infinite or NaN score gives NaN below)
+        const float next = fmaxf(most, top), base = next == -INFINITY ? 0.f : next;
+        const float fade = expf(most - base), p = j < keys ? expf(s - base) : 0.f;
+        float sum = p;
+        for (int d = 32; d; d >>= 1)
+            sum += __shfl_xor(sum, d);
+        total = total * fade + sum;
+        most = next;
+        lds.p[lane] = p;
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            y[v] *= fade;
+        const int end = keys - first < 64 ? keys - first : 64;
+        for (int i = 0; i < end; ++i) {
+            const float w = lds.p[i];
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (lane + 64 * v < dim)
+                    y[v] = __builtin_fmaf(w, value(first + i, lane + 64 * v), y[v]);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (lane + 64 * v < dim)
+            out(lane + 64 * v, total != 0.f ? y[v] / total : 0.f);
+}
+
+}  // namespace
+}  // namespace aqd

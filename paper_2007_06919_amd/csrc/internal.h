@@ -240,4 +240,68 @@ hipError_t launch_qlin_f32(const QlinArgs &a, int shape, hipStream_t stream);
 hipError_t launch_qlin_f16(const QlinArgs &a, int shape, hipStream_t stream);
 hipError_t launch_qlin_bf16(const QlinArgs &a, int shape, hipStream_t stream);
 
+// ---- norms and rotation of heads (heads.hip) ---------------------------------------
+struct HeadsSide {
+    const void *x, *weight;
+    void *y;
+    long long token, head, y_token, y_head;   // strides, elements
+};
+struct HeadsArgs {
+    HeadsSide q, k;
+    const int32_t *position;
+    const float *table;
+    int tokens, q_heads, heads;               // heads: q's and k's
+    int dim, rot, pairs, type, positions;
+    float eps;
+};
+hipError_t launch_heads(const HeadsArgs &a, hipStream_t stream);
+
+// ---- the 4-bit cache (qcache.hip) ---------------------------------------------------
+struct QcacheShape {
+    int heads, dim, group, page, pages;
+    long long block_bytes;   // of one head in a page
+};
+struct QcacheArgs {
+    QcacheShape c;
+    uint8_t *cache;
+    const int32_t *slots;
+    void *k, *v;             // read by a write, written by a read
+    long long k_token, k_head, v_token, v_head;
+    int tokens, type;
+};
+hipError_t launch_qcache_write(const QcacheArgs &a, hipStream_t stream);
+hipError_t launch_qcache_read(const QcacheArgs &a, hipStream_t stream);
+
+// ---- attention over the cache (qattn.hip) and over rows in memory (attn.hip) ---------
+struct AttnPlan {
+    int parts;      // workgroups that share a sequence's keys
+    int chunk;      // keys of each
+    size_t bytes;   // their results in the workspace
+};
+struct QattnArgs {
+    QcacheShape c;
+    const uint8_t *cache;
+    const void *q;
+    void *y;
+    const int32_t *q_start, *tables, *lengths;
+    long long ld_table, q_token, q_head, y_token, y_head;
+    int batch, q_heads, queries, max_queries, max_keys, type;
+    float scale;
+    float *part;
+};
+AttnPlan qattn_plan(const QattnArgs &a, size_t room);
+hipError_t launch_qattn(const QattnArgs &a, const AttnPlan &plan, hipStream_t stream);
+
+struct AttnArgs {
+    const void *q, *k, *v;
+    void *y;
+    const int32_t *q_start, *k_start;
+    long long q_token, q_head, k_token, k_head, v_token, v_head, y_token, y_head;
+    int batch, q_heads, heads, dim, queries, keys, max_queries, max_keys, causal, type;
+    float scale;
+    float *part;
+};
+AttnPlan attn_plan(const AttnArgs &a, size_t room);
+hipError_t launch_attn(const AttnArgs &a, const AttnPlan &plan, hipStream_t stream);
+
 }  // namespace aqd
