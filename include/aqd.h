@@ -444,7 +444,7 @@ aqd_status_t aqd_heads_run(const aqd_heads_desc_t *desc, const void *q, const vo
 typedef struct {
     int heads;        /* >= 1 */
     int dim, group;   /* 64, 128 or 256; 32, 64 or 128, at most dim */
-    int page, pages;  /* 16, 32, 64, 128 or 256 tokens; >= 0, pages * page <= INT32_MAX */
+    int page, pages;  /* 16, 32, 64, 128 or 256 tokens; >= 0 (qattn: >= 1, or max_keys 0), pages * page <= INT32_MAX */
 } qcache_desc_t;
 aqd_status_t qcache_bytes(const qcache_desc_t *desc, size_t *bytes);
 

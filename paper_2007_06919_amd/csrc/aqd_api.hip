@@ -2072,8 +2072,10 @@ aqd_status_t qattn_args(const qattn_desc_t *d, QattnArgs &a)
     a.max_queries = std::min(d->max_queries, d->queries);
     a.max_keys = d->max_keys;
     REQUIRE(a.max_keys <= INT32_MAX - 65536, "too many keys");
-    REQUIRE((long long)a.queries * a.q_heads <= INT32_MAX - 65536 && (double)a.batch * a.q_heads * (a.max_queries + 16.0) <= INT32_MAX - 65536,
-            "too many queries");
+    REQUIRE(a.c.pages || !a.max_keys, "keys, and no pages");
+    // a workgroup has 16 rows, and a launch less than 2^32 threads
+    REQUIRE((long long)a.queries * a.q_heads <= INT32_MAX - 65536 &&
+                (double)a.batch * a.c.heads * ((double)a.max_queries * (a.q_heads / a.c.heads) / 16 + 1) <= 1 << 23, "too many queries");
     a.q_token = d->q_token, a.q_head = d->q_head, a.y_token = d->y_token, a.y_head = d->y_head, a.ld_table = d->ld_table;
     REQUIRE(strides_ok(a.q_token, a.q_head, a.queries, a.q_heads, a.c.dim) && strides_ok(a.y_token, a.y_head, a.queries, a.q_heads, a.c.dim),
             "strides of q or y by which elements could share memory, or too large");
@@ -2218,8 +2220,7 @@ aqd_status_t qattn_run(const qattn_desc_t *d, const void *q, const int32_t *q_st
         return st;
     REQUIRE(q && y && lengths, "null pointer");
     REQUIRE(q_start || a.queries == a.batch, "without q_start there is one query a sequence");
-    REQUIRE((cache && tables) || !a.max_keys || !a.c.pages, "null pointer");
-    REQUIRE(tables || !a.max_keys, "null pointer");
+    REQUIRE((cache && tables) || !a.max_keys, "null pointer");
     REQUIRE(aligned_to(q, 2) && aligned_to(y, 2) && aligned_to(q_start, 4) && aligned_to(tables, 4) && aligned_to(lengths, 4),
             "a pointer is not aligned to its elements");
     REQUIRE(aligned16(cache) && aligned16(workspace), "the cache and the workspace must be 16-byte aligned");

@@ -1,69 +1,499 @@
 // Attention over the 4-bit cache. Definition and layout: include/aqd.h.
+//
+// A workgroup has one sequence, one key head, 16 or 32 rows (the query heads of the key head, times
+// the sequence's queries) and a range of tokens; its four waves take 32 tokens in turn, each with a
+// softmax of its own, joined at the end. With S^T = K Q^T and O^T = V^T P^T (16 x 16 x 32 products) the
+// scores' lanes are the weights' lanes: lane (r, g) has the scores of tokens 4 g .. 4 g + 3 of a tile of 16 for row r,
+// which is what the second product takes for k = 8 g .. from two tiles, so no weight changes lanes.
+//
+// A code becomes an operand by one shift and one and-or for two: c is put below the leading bit of 128 (bf16) or 64
+// (fp16), which makes 128 + c or 64 + c. Products with a constant -136 or -72 take the offset, 8 included, out again
+// before it is scaled, so that the sums are those of c - 8, exactly. A key's scale multiplies its
+// scores of the group in fp32, a value's scale its weights before they are rounded to T.
+//
+// fp16 weights have few exponents: there the softmax's reference is the largest score plus the exponent of the values'
+// scales, so that the product of weight and scale is near 1 whatever the values' size.
 
-#include "attn_row.h"
+#include <algorithm>
+
+#include "attn_common.h"
 
 namespace aqd {
 namespace {
 
 template <typename T>
-__global__ void __launch_bounds__(64) qattn_row_kernel(QattnArgs A)
+struct Code;
+template <>
+struct Code<__bf16> {
+    static constexpr uint32_t MASK = 0x000F000Fu, BASE = 0x43004300u, OFF = 0xC308C308u;   // 128 + c; -136
+    static constexpr int AT = 0;
+    static constexpr bool NARROW = false;
+};
+template <>
+struct Code<_Float16> {
+    static constexpr uint32_t MASK = 0x00F000F0u, BASE = 0x54005400u, OFF = 0xD480D480u;   // 64 + c; -72
+    static constexpr int AT = 4;
+    static constexpr bool NARROW = true;
+};
+
+// nibbles J and J + 4 of a word as two operands
+template <typename T, int J>
+__device__ __forceinline__ uint32_t widen(uint32_t w)
 {
-    __shared__ RowScratch lds;
-    const int i = blockIdx.x % A.max_queries, rest = blockIdx.x / A.max_queries, head = rest % A.q_heads, b = rest / A.q_heads;
-    const int begin = A.q_start ? min(max(A.q_start[b], 0), A.queries) : b;
+    constexpr int shift = 4 * J - Code<T>::AT;
+    if constexpr (shift > 0)
+        w >>= shift;
+    else if constexpr (shift < 0)
+        w <<= -shift;
+    return (w & Code<T>::MASK) | Code<T>::BASE;
+}
+
+// 4 bytes per lane from global memory straight into LDS at la + 4 * lane
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void dma4(const void *g, uint32_t la)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+                 ::"s"(__builtin_amdgcn_readfirstlane(la)), "v"(g) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// two words at byte offsets of a wave-uniform address, through the scalar cache (a vector load would wait for the copies)
+__device__ __forceinline__ void scalar_loads(const int32_t *p, int a, int b, int &x, int &y)
+{
+    asm volatile("s_load_dword %0, %2, %3\n\ts_load_dword %1, %2, %4\n\ts_waitcnt lgkmcnt(0)" : "=&s"(x), "=&s"(y) : "s"(p), "s"(a), "s"(b));
+}
+
+// one sequence as the kernels see it
+struct Sequence {
+    int begin, n, length;
+};
+__device__ __forceinline__ Sequence sequence(const QattnArgs &A, int b)
+{
+    Sequence s;
+    s.begin = A.q_start ? min(max(A.q_start[b], 0), A.queries) : b;
     const int end = A.q_start ? min(max(A.q_start[b + 1], 0), A.queries) : b + 1;
-    const int n = min(end - begin, A.max_queries);
-    if (i >= n)
+    s.n = min(end - s.begin, A.max_queries);
+    s.length = (int)max(min((long long)min(A.lengths[b], A.max_keys), A.ld_table * A.c.page), 0LL);
+    return s;
+}
+// how many tokens a workgroup's rows see at most
+__device__ __forceinline__ int seen_by(const Sequence &s, int rows, int first_row, int per)
+{
+    const int last = min((first_row + rows - 1) / per, s.n - 1);
+    return max(s.length - s.n + 1 + last, 0);
+}
+
+template <int DIM, int GROUP, int R>
+struct Shape {
+    static constexpr int GROUPS = DIM / GROUP;
+    static constexpr int CODES = 16 * DIM;                                     // a tile's codes, keys and values, bytes
+    static constexpr int SCALES = 64 * GROUPS, SCALE_ROOM = SCALES < 256 ? 256 : SCALES;
+    static constexpr int TILE = CODES + SCALE_ROOM, STEP = 2 * TILE;           // a step: two tiles
+    static constexpr int COPIES = 2 * (CODES / 1024 + SCALE_ROOM / 256);       // of a step
+    static constexpr int RING = 18432 / STEP < 2 ? 2 : 18432 / STEP > 4 ? 4 : 18432 / STEP;
+    static constexpr int RESULT = 16 * (DIM + 4);                              // a wave's sums of 16 rows, fp32
+    static constexpr int WAVE = RING * STEP > 4 * RESULT ? RING * STEP : 4 * RESULT;
+};
+
+template <typename T, int DIM, int GROUP, int R>
+__global__ void __launch_bounds__(256, DIM == 256 && (R == 2 || GROUP == 32) ? 1 : 2) qattn_kernel(QattnArgs A, int tiles, int parts, int chunk)
+{
+    typedef Shape<DIM, GROUP, R> S;
+    constexpr int G = S::GROUPS, U = DIM / 32, TILES = DIM / 16;
+    __shared__ __align__(16) uint8_t lds[4 * S::WAVE];
+    static_assert(sizeof(lds) <= 81920, "two workgroups to a CU");
+    const int per = A.q_heads / A.c.heads;
+    const int kv = blockIdx.x % A.c.heads;
+    int rest = blockIdx.x / A.c.heads;
+    const int row_tile = rest % tiles;
+    rest /= tiles;
+    const int part = rest % parts, b = rest / parts;
+    const Sequence seq = sequence(A, b);
+    const int first_row = row_tile * 16 * R, rows = seq.n * per;
+    if (first_row >= rows)
         return;
-    const QcacheShape &c = A.c;
-    const int length = max((int)min((long long)min(A.lengths[b], A.max_keys), A.ld_table * c.page), 0);
-    const int keys = max(length - n + 1 + i, 0), kv = head / (A.q_heads / c.heads), groups = c.dim / c.group;
+    const int limit = seen_by(seq, 16 * R, first_row, per), start = part * chunk, end = min(start + chunk, limit);
+    if (part && start >= limit)
+        return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    uint8_t *ring = lds + wave * S::WAVE;
+    const uint32_t ring_at = lds_addr(ring);
     const int32_t *table = A.tables + b * A.ld_table;
-    const T *q = (const T *)A.q + (begin + i) * A.q_token + head * A.q_head;
-    T *y = (T *)A.y + (begin + i) * A.y_token + head * A.y_head;
-    const auto block = [&](int j) -> const uint8_t * {
-        const int page = table[j / c.page];
-        return page >= 0 && page < c.pages ? A.cache + ((long long)page * c.heads + kv) * c.block_bytes : nullptr;
+
+    // copies of the step at token t into the ring's place `at`; bits 0 and 1: the tiles' pages are none of the cache's
+    const int last_tile = (limit - 1) >> 4;
+    auto copy = [&](int t, int at) -> uint32_t {
+        uint32_t bad = 0;
+        const int firsts[2] = {min(t >> 4, last_tile) * 16, min((t >> 4) + 1, last_tile) * 16};
+        int pages[2];
+        scalar_loads(table, 4 * (firsts[0] / A.c.page), 4 * (firsts[1] / A.c.page), pages[0], pages[1]);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int first = firsts[half];
+            int page = pages[half];
+            if ((unsigned)page >= (unsigned)A.c.pages) {
+                bad |= 1u << half;
+                page = 0;
+            }
+            const int in = first % A.c.page;
+            const uint8_t *block = A.cache + ((long long)page * A.c.heads + kv) * A.c.block_bytes;
+            const uint32_t to = ring_at + at * S::STEP + half * S::TILE;
+            const uint8_t *codes = block + in * (DIM / 2), *scales = block + A.c.page * DIM + in * (2 * G);
+#pragma unroll
+            for (int i = 0; i < S::CODES / 1024; ++i) {
+                const int o = i * 1024 + lane * 16;
+                dma16(codes + (o < 8 * DIM ? o : o - 8 * DIM + A.c.page * (DIM / 2)), to + i * 1024);
+            }
+#pragma unroll
+            for (int i = 0; i < S::SCALE_ROOM / 256; ++i) {
+                const int o = i * 256 + lane * 4 < S::SCALES ? i * 256 + lane * 4 : 0;
+                dma4(scales + (o < 32 * G ? o : o - 32 * G + A.c.page * (2 * G)), to + S::CODES + i * 256);
+            }
+        }
+        return bad;
     };
-    const int scales = c.page * c.dim;
-    row_attention<256>(
-        lds, c.dim, keys, A.scale, [&](int e) { return (float)q[e]; },
-        [&](int j, int e) {
-            const uint8_t *p = block(j);
-            if (!p)
-                return (float)NAN;
-            const int t = j % c.page, w = e / 8, nibble = e % 8 / 2 + e % 2 * 4;
-            const uint32_t word = *(const uint32_t *)(p + t * (c.dim / 2) + 4 * (w % 4 * (c.dim / 32) + w / 4));
-            return (float)((int)(word >> (4 * nibble) & 15) - 8) * (float)*(const __bf16 *)(p + scales + 2 * (t * groups + e / c.group));
-        },
-        [&](int j, int e) {
-            const uint8_t *p = block(j);
-            if (!p)
-                return (float)NAN;
-            const int t = j % c.page;
-            const uint16_t unit = *(const uint16_t *)(p + c.page * c.dim / 2 + 2 * (((t / 4 * 16 + e % 16) * (c.dim / 64) + e / 64) * 4 + t % 4));
-            return (float)((unit >> (4 * (e / 16 % 4)) & 15) - 8) * (float)*(const __bf16 *)(p + scales + 2 * ((c.page + t) * groups + e / c.group));
-        },
-        [&](int e, float f) { y[e] = (T)f; });
+
+    // queries as operands, the sign of the scale with them; rows past the last are zeros
+    u32x4 q[R][U];
+    int seen[R];
+    const uint32_t flip = A.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        const int row = first_row + 16 * k + r, i = row / per;
+        seen[k] = row < rows ? seq.length - seq.n + 1 + i : 0;
+        const T *p = (const T *)A.q + (seq.begin + i) * A.q_token + (kv * per + row % per) * A.q_head + 8 * g;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            typedef T V __attribute__((ext_vector_type(8), aligned(2)));
+            u32x4 w = {0, 0, 0, 0};
+            if (row < rows)
+                w = __builtin_bit_cast(u32x4, *(const V *)(p + 32 * u));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                q[k][u][e] = w[e] ^ flip;
+        }
+    }
+    uint32_t bads = 0;   // two bits per step in flight, the next one lowest
+    const int t_first = start + 32 * wave;
+#pragma unroll
+    for (int i = 0; i < S::RING; ++i)
+        if (t_first + 128 * i < end)
+            bads |= copy(t_first + 128 * i, i) << (2 * i);
+
+    const int seen_least = seq.length - seq.n + 1 + first_row / per;
+    // (a scale of 0 would make -infinity * 0 of hidden scores)
+    const float scale = fmaxf(fabsf(A.scale) * LOG2E, 0x1p-100f);
+    const u32x4 off = {Code<T>::OFF, Code<T>::OFF, Code<T>::OFF, Code<T>::OFF};
+
+    f32x4 o[R][TILES];
+    float ref[R], total[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        ref[k] = -INFINITY;
+        total[k] = 0.f;
+#pragma unroll
+        for (int i = 0; i < TILES; ++i)
+            o[k][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    int at = 0;
+    for (int t = t_first; t < end; t += 128) {
+        // the steps behind this one may be under way
+        const int behind = (end - 1 - t) / 128;
+        if (behind >= S::RING - 1)
+            wait_vmcnt<(S::RING - 1) * S::COPIES>();
+        else if (S::RING > 2 && behind == 2)
+            wait_vmcnt<2 * S::COPIES>();
+        else if (behind == 1)
+            wait_vmcnt<S::COPIES>();
+        else
+            wait_vmcnt<0>();
+        const uint8_t *step = ring + at * S::STEP;
+        uint32_t kc[2][U], vc[2][U], ks[2][2 * G], vs[2][2 * G];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const uint8_t *tile = step + half * S::TILE;
+            load_words<U>(tile + r * (DIM / 2) + g * (DIM / 8), kc[half]);
+            load_words<U>(tile + 8 * DIM + g * (2 * DIM) + r * (DIM / 8), vc[half]);
+            load_words<2 * G>(tile + S::CODES + g * (8 * G), ks[half]);
+            load_words<2 * G>(tile + S::CODES + 32 * G + g * (8 * G), vs[half]);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        const uint32_t bad = bads & 3;
+        bads >>= 2;
+        if (t + 128 * S::RING < end)
+            bads |= copy(t + 128 * S::RING, at) << (2 * (S::RING - 1));
+        at = at + 1 == S::RING ? 0 : at + 1;
+
+        // scale i of group j in words of two
+        const auto number = [](const uint32_t *w, int token, int group) {
+            const int i = token * G + group;
+            return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+        };
+        const bool masked = t + 32 > seen_least || bad;
+        float s[R][8];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            u32x4 key[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t w = kc[half][u];
+                key[u] = u32x4{widen<T, 0>(w), widen<T, 1>(w), widen<T, 2>(w), widen<T, 3>(w)};
+            }
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+#pragma unroll
+                for (int j = 0; j < G; ++j) {
+                    f32x4 d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int u = j * (GROUP / 32); u < (j + 1) * (GROUP / 32); ++u)
+                        d = mfma16(off, q[k][u], d, T());
+#pragma unroll
+                    for (int u = j * (GROUP / 32); u < (j + 1) * (GROUP / 32); ++u)
+                        d = mfma16(key[u], q[k][u], d, T());
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float f = number(ks[half], i, j);
+                        s[k][4 * half + i] = j ? __builtin_fmaf(d[i], f, s[k][4 * half + i]) : d[i] * f;
+                    }
+                }
+        }
+        if (masked) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int token = t + 16 * half + 4 * g + i;
+#pragma unroll
+                    for (int k = 0; k < R; ++k)
+                        s[k][4 * half + i] = token < seen[k] ? (bad >> half & 1 ? NAN : s[k][4 * half + i]) : -INFINITY;
+                    // what lies behind the sequence's end may be any scale
+                    if (Code<T>::NARROW && token >= limit) {
+                        if constexpr (G > 1) {
+#pragma unroll
+                            for (int j = 0; j < G / 2; ++j)
+                                vs[half][i * (G / 2) + j] = 0;
+                        } else {
+                            vs[half][i / 2] &= i & 1 ? 0xFFFFu : 0xFFFF0000u;
+                        }
+                    }
+                }
+        }
+        // exponent of the largest value scale of the lane's tokens that is a number
+        float size = 0.f;
+        if constexpr (Code<T>::NARROW) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int i = 0; i < 2 * G; ++i) {
+                    // without its sign, and with a carry that takes infinity and NaN below all numbers
+                    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+                    const u16x2 x = __builtin_bit_cast(u16x2, vs[half][i]) * (unsigned short)2 + (unsigned short)0x100;
+                    top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, __builtin_bit_cast(u16x2, top)));
+                }
+            const int e = (int)max(top >> 24, (top & 0xFFFFu) >> 8) - 1 - 127;
+            // (weights of values that T rounds to 0 need not be near 1, and their sum has to stay a number)
+            size = (float)min(max(e, -40), 100);
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            float top = s[k][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i)
+                top = fmaxf(top, s[k][i]);
+            top = __builtin_fmaf(top, scale, size);
+            // weights up to 2^8 are as good as up to 1: the reference moves seldom
+            if (__builtin_amdgcn_ballot_w64(top > ref[k] + 8.f)) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float next = fmaxf(ref[k], top), fade = next == -INFINITY ? 1.f : exp2_fast(ref[k] - next);
+                ref[k] = next;
+                total[k] *= fade;
+#pragma unroll
+                for (int i = 0; i < TILES; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        o[k][i][e] *= fade;
+            }
+            const float base = ref[k] == -INFINITY ? 0.f : -ref[k];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s[k][i] = exp2_fast(__builtin_fmaf(s[k][i], scale, base));
+                total[k] += s[k][i];
+            }
+        }
+        static_for<G>([&](auto group) {
+            constexpr int J = decltype(group)::value;
+            u32x4 p[R];
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                float w[8];
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        w[4 * half + i] = s[k][4 * half + i] * number(vs[half], i, J);
+                        // (a scale that one row sees and another does not may be no number)
+                        if (masked && t + 16 * half + 4 * g + i >= seen[k])
+                            w[4 * half + i] = 0.f;
+                    }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    p[k][i] = pack2<T>(w[2 * i], w[2 * i + 1]);
+            }
+            static_for<GROUP / 16>([&](auto i) {
+                constexpr int tile = J * (GROUP / 16) + decltype(i)::value, h = tile / 4, n = tile % 4;
+                const u32x4 value = {widen<T, n>(vc[0][2 * h]), widen<T, n>(vc[0][2 * h + 1]), widen<T, n>(vc[1][2 * h]),
+                                     widen<T, n>(vc[1][2 * h + 1])};
+#pragma unroll
+                for (int k = 0; k < R; ++k) {
+                    o[k][tile] = mfma16(off, p[k], o[k][tile], T());
+                    o[k][tile] = mfma16(value, p[k], o[k][tile], T());
+                }
+            });
+        });
+    }
+
+    // join the waves, 16 rows at a time: [row][DIM] sums, then references and totals
+    float *sums = (float *)ring;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        __syncthreads();
+        total[k] += __shfl_xor(total[k], 16);
+        total[k] += __shfl_xor(total[k], 32);
+#pragma unroll
+        for (int i = 0; i < TILES; ++i)
+            *(f32x4 *)(sums + r * (DIM + 4) + 16 * i + 4 * g) = o[k][i];
+        if (g == 0) {
+            sums[r * (DIM + 4) + DIM] = ref[k];
+            sums[r * (DIM + 4) + DIM + 1] = total[k];
+        }
+        __syncthreads();
+        constexpr int LANES = DIM / 4;   // of a row
+        for (int i = threadIdx.x; i < 16 * LANES; i += 256) {
+            const int row = first_row + 16 * k + i / LANES, c = i % LANES * 4, from = i / LANES * (DIM + 4);
+            if (row >= rows)
+                break;
+            float most = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+                most = fmaxf(most, ((const float *)(lds + w * S::WAVE))[from + DIM]);
+            const float base = most == -INFINITY ? 0.f : most;
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float *p = (const float *)(lds + w * S::WAVE) + from;
+                const float f = exp2_fast(p[DIM] - base);
+                const f32x4 v = *(const f32x4 *)(p + c);
+                l += f * p[DIM + 1];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    sum[e] += f * v[e];
+            }
+            const int query = seq.begin + row / per, head = kv * per + row % per;
+            if (parts == 1) {
+                const float inverse = l != 0.f ? 1.f / l : 0.f;
+                typedef T V __attribute__((ext_vector_type(4), aligned(2)));
+                V v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[e] = (T)(sum[e] * inverse);
+                *(V *)((T *)A.y + query * A.y_token + head * A.y_head + c) = v;
+            } else {
+                const long long all = (long long)A.queries * A.q_heads, id = ((long long)query * A.q_heads + head) * parts + part;
+                *(f32x4 *)(A.part + id * DIM + c) = sum;
+                if (c == 0) {
+                    float *stat = A.part + all * parts * DIM + 2 * id;
+                    stat[0] = most;
+                    stat[1] = l;
+                }
+            }
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) qattn_join_kernel(QattnArgs A, int rows, int parts, int chunk)
+{
+    const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), all = (long long)A.batch * A.max_queries * A.q_heads;
+    if (at >= all)
+        return;
+    const int head = (int)(at % A.q_heads), i = (int)(at / A.q_heads % A.max_queries), b = (int)(at / A.q_heads / A.max_queries);
+    const Sequence seq = sequence(A, b);
+    if (i >= seq.n)
+        return;
+    // the parts that its workgroups' rows have
+    const int per = A.q_heads / A.c.heads, first_row = (i * per + head % per) / rows * rows;
+    const int limit = seen_by(seq, rows, first_row, per), used = max((limit + chunk - 1) / chunk, 1);
+    const long long query = seq.begin + i;
+    join_parts<T>(A.part, (long long)A.queries * A.q_heads, query * A.q_heads + head, parts, used, A.c.dim,
+                  (T *)A.y + query * A.y_token + head * A.y_head);
+}
+
+int row_tiles(const QattnArgs &a, int rows) { return (a.max_queries * (a.q_heads / a.c.heads) + rows - 1) / rows; }
+int rows_of(const QattnArgs &a) { return a.max_queries * (a.q_heads / a.c.heads) <= 16 ? 16 : 32; }
+
+template <typename T, int DIM, int GROUP, int R>
+hipError_t launch_rows(const QattnArgs &a, const AttnPlan &p, hipStream_t stream)
+{
+    const int tiles = row_tiles(a, 16 * R);
+    const dim3 grid((unsigned)(a.c.heads * tiles * p.parts * a.batch));
+    hipLaunchKernelGGL((qattn_kernel<T, DIM, GROUP, R>), grid, dim3(256), 0, stream, a, tiles, p.parts, p.chunk);
+    return hipGetLastError();
+}
+
+template <typename T, int DIM, int GROUP>
+hipError_t launch_group(const QattnArgs &a, const AttnPlan &p, hipStream_t stream)
+{
+    return rows_of(a) == 16 ? launch_rows<T, DIM, GROUP, 1>(a, p, stream) : launch_rows<T, DIM, GROUP, 2>(a, p, stream);
+}
+
+template <typename T, int DIM>
+hipError_t launch_dim(const QattnArgs &a, const AttnPlan &p, hipStream_t stream)
+{
+    if constexpr (DIM >= 128)
+        if (a.c.group == 128)
+            return launch_group<T, DIM, 128>(a, p, stream);
+    return a.c.group == 32 ? launch_group<T, DIM, 32>(a, p, stream) : launch_group<T, DIM, 64>(a, p, stream);
+}
+
+template <typename T>
+hipError_t launch_type(const QattnArgs &a, const AttnPlan &p, hipStream_t stream)
+{
+    const hipError_t e = a.c.dim == 64    ? launch_dim<T, 64>(a, p, stream)
+                         : a.c.dim == 128 ? launch_dim<T, 128>(a, p, stream)
+                                          : launch_dim<T, 256>(a, p, stream);
+    if (e != hipSuccess || p.parts == 1)
+        return e;
+    const long long all = (long long)a.batch * a.max_queries * a.q_heads;
+    hipLaunchKernelGGL(qattn_join_kernel<T>, dim3((unsigned)((all + 3) / 4)), dim3(256), 0, stream, a, rows_of(a), p.parts, p.chunk);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 AttnPlan qattn_plan(const QattnArgs &a, size_t room)
 {
-    (void)room;
-    return {1, a.max_keys, 0};
+    const int keys = (int)std::min<long long>(a.max_keys, a.ld_table * a.c.page);
+    const long long groups = (long long)a.batch * a.c.heads * row_tiles(a, rows_of(a));
+    // enough workgroups to fill the GPU several times over, as the sequences may be of any length, each of whole rounds of its waves
+    long long parts = std::max(1LL, std::min<long long>(4096 / std::max(groups, 1LL), (keys + 255) / 256));
+    const long long one = (long long)a.queries * a.q_heads * (a.c.dim + 2) * 4;
+    parts = std::min(parts, (long long)room / std::max(one, 1LL));
+    if (parts <= 1)
+        return {1, (keys + 127) / 128 * 128, 0};
+    const long long chunk = ((keys + parts - 1) / parts + 127) / 128 * 128;
+    parts = (keys + chunk - 1) / chunk;
+    if (parts <= 1)
+        return {1, (keys + 127) / 128 * 128, 0};
+    return {(int)parts, (int)chunk, (size_t)(one * parts)};
 }
 
 hipError_t launch_qattn(const QattnArgs &a, const AttnPlan &plan, hipStream_t stream)
 {
-    (void)plan;
-    const dim3 grid((unsigned)(a.batch * a.q_heads * a.max_queries));
-    if (a.type == AQD_F16)
-        hipLaunchKernelGGL(qattn_row_kernel<_Float16>, grid, dim3(64), 0, stream, a);
-    else
-        hipLaunchKernelGGL(qattn_row_kernel<__bf16>, grid, dim3(64), 0, stream, a);
-    return hipGetLastError();
+    return a.type == AQD_F16 ? launch_type<_Float16>(a, plan, stream) : launch_type<__bf16>(a, plan, stream);
 }
 
 }  // namespace aqd
