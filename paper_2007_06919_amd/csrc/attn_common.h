@@ -40,33 +40,83 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 
 constexpr float LOG2E = 1.44269504088896340736f;
 
-// The parts of one row: [parts][dim] sums and, behind all rows' sums, [parts][2] references and totals,
-// with which row `row` of `rows` is sum_p o_p 2^(ref_p - ref) / sum_p l_p 2^(ref_p - ref). One wave; no weight at all: zeros.
+// The parts of one row, sums [parts][dim] and, behind all rows' sums, [parts][2] references and totals: the row is
+// sum_p o_p 2^(ref_p - ref) / sum_p l_p 2^(ref_p - ref), zeros where there is no weight at all. One workgroup of four waves: 64 lanes
+// have four channels each, or for shorter rows several parts at a time.
+struct JoinScratch {
+    float sum[256][4], most[4], total[4];
+};
 template <typename T>
-__device__ __forceinline__ void join_parts(const float *part, long long rows, long long row, int all, int parts, int dim, T *y)
+__device__ __forceinline__ void join_parts(JoinScratch &lds, const float *part, long long rows, long long row, int all, int parts, int dim, T *y)
 {
-    const int lane = threadIdx.x & 63;
     const float *o = part + row * all * dim, *stat = part + rows * all * dim + row * all * 2;
+    const int lanes = (dim + 3) / 4, each = 256 / lanes, c = threadIdx.x % lanes * 4;
+    const int first = (int)threadIdx.x < each * lanes ? threadIdx.x / lanes : parts;
+    // the first loads of the sums are under way with those of the references
+    constexpr int EARLY = 4;
+    f32x4 early[EARLY];
+    float early_ref[EARLY], early_total[EARLY];
+#pragma unroll
+    for (int u = 0; u < EARLY; ++u) {
+        const int p = first + u * each;
+        early[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        early_ref[u] = -INFINITY;
+        early_total[u] = 0.f;
+        if (p < parts) {
+            early[u] = *(const f32x4 *)(o + (long long)p * dim + c);
+            early_ref[u] = stat[2 * p];
+            early_total[u] = stat[2 * p + 1];
+        }
+    }
     float ref = -INFINITY;
-    for (int p = lane; p < parts; p += 64)
+    for (int p = threadIdx.x; p < parts; p += 256)
         ref = fmaxf(ref, stat[2 * p]);
     for (int d = 32; d; d >>= 1)
         ref = fmaxf(ref, __shfl_xor(ref, d));
+    if ((threadIdx.x & 63) == 0)
+        lds.most[threadIdx.x >> 6] = ref;
+    __syncthreads();
+    ref = fmaxf(fmaxf(lds.most[0], lds.most[1]), fmaxf(lds.most[2], lds.most[3]));
     const float base = ref == -INFINITY ? 0.f : ref;
-    float sum[4] = {}, total = 0.f;
-    for (int p = 0; p < parts; ++p) {
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    float total = 0.f;
+#pragma unroll
+    for (int u = 0; u < EARLY; ++u) {
+        const float f = exp2_fast(early_ref[u] - base);
+        total += f * early_total[u];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            sum[e] += f * early[u][e];
+    }
+#pragma unroll 4
+    for (int p = first + EARLY * each; p < parts; p += each) {
         const float f = exp2_fast(stat[2 * p] - base);
+        const f32x4 v = *(const f32x4 *)(o + (long long)p * dim + c);
         total += f * stat[2 * p + 1];
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-            if (lane + 64 * v < dim)
-                sum[v] += f * o[(long long)p * dim + lane + 64 * v];
+        for (int e = 0; e < 4; ++e)
+            sum[e] += f * v[e];
     }
+    *(f32x4 *)lds.sum[threadIdx.x] = sum;
+    // every lane of a part has its total; those of the first channels are added
+    float mine = c == 0 ? total : 0.f;
+    for (int d = 32; d; d >>= 1)
+        mine += __shfl_xor(mine, d);
+    if ((threadIdx.x & 63) == 0)
+        lds.total[threadIdx.x >> 6] = mine;
+    __syncthreads();
+    if ((int)threadIdx.x >= lanes)
+        return;
+    for (int i = 1; i < each; ++i)
+        sum += *(const f32x4 *)lds.sum[threadIdx.x + i * lanes];
+    total = lds.total[0] + lds.total[1] + lds.total[2] + lds.total[3];
     const float inverse = total != 0.f ? 1.f / total : 0.f;
+    typedef T V __attribute__((ext_vector_type(4), aligned(2)));
+    V v;
 #pragma unroll
-    for (int v = 0; v < 4; ++v)
-        if (lane + 64 * v < dim)
-            y[lane + 64 * v] = (T)(sum[v] * inverse);
+    for (int e = 0; e < 4; ++e)
+        v[e] = (T)(sum[e] * inverse);
+    *(V *)(y + c) = v;
 }
 
 }  // namespace

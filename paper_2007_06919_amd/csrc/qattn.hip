@@ -36,25 +36,30 @@ struct Code<_Float16> {
     static constexpr bool NARROW = true;
 };
 
-// nibbles J and J + 4 of a word as two operands
+// nibbles J and J + 4 of a word as two operands. mask and base: MASK and BASE in registers, of which the compiler must not
+// know the value: with constants it takes two instructions for the and and the or.
 template <typename T, int J>
-__device__ __forceinline__ uint32_t widen(uint32_t w)
+__device__ __forceinline__ uint32_t widen(uint32_t w, uint32_t mask, uint32_t base)
 {
     constexpr int shift = 4 * J - Code<T>::AT;
     if constexpr (shift > 0)
         w >>= shift;
     else if constexpr (shift < 0)
         w <<= -shift;
-    return (w & Code<T>::MASK) | Code<T>::BASE;
+    return (w & mask) | base;
 }
 
-// 4 bytes per lane from global memory straight into LDS at la + 4 * lane
+// 16 or 4 bytes per lane from `offset` bytes past a wave-uniform address straight into LDS at la + 16 * lane
+// or 4 * lane (see dma16)
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void dma4(const void *g, uint32_t la)
+__device__ __forceinline__ void copy16(const uint8_t *base, uint32_t offset, uint32_t la)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
-                 ::"s"(__builtin_amdgcn_readfirstlane(la)), "v"(g) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(la), "v"(offset), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void copy4(const uint8_t *base, uint32_t offset, uint32_t la)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(la), "v"(offset), "s"(base) : "memory", "m0");
 }
 #pragma clang diagnostic pop
 
@@ -91,13 +96,13 @@ struct Shape {
     static constexpr int SCALES = 64 * GROUPS, SCALE_ROOM = SCALES < 256 ? 256 : SCALES;
     static constexpr int TILE = CODES + SCALE_ROOM, STEP = 2 * TILE;           // a step: two tiles
     static constexpr int COPIES = 2 * (CODES / 1024 + SCALE_ROOM / 256);       // of a step
-    static constexpr int RING = 18432 / STEP < 2 ? 2 : 18432 / STEP > 4 ? 4 : 18432 / STEP;
+    static constexpr int RING = DIM == 64 ? 4 : 2;                             // steps under way
     static constexpr int RESULT = 16 * (DIM + 4);                              // a wave's sums of 16 rows, fp32
     static constexpr int WAVE = RING * STEP > 4 * RESULT ? RING * STEP : 4 * RESULT;
 };
 
 template <typename T, int DIM, int GROUP, int R>
-__global__ void __launch_bounds__(256, DIM == 256 && (R == 2 || GROUP == 32) ? 1 : 2) qattn_kernel(QattnArgs A, int tiles, int parts, int chunk)
+__global__ void __launch_bounds__(256, DIM == 256 ? (R == 2 || GROUP == 32 ? 1 : 2) : DIM == 128 && R == 2 ? 2 : 3) qattn_kernel(QattnArgs A, int tiles, int parts, int chunk)
 {
     typedef Shape<DIM, GROUP, R> S;
     constexpr int G = S::GROUPS, U = DIM / 32, TILES = DIM / 16;
@@ -118,38 +123,42 @@ __global__ void __launch_bounds__(256, DIM == 256 && (R == 2 || GROUP == 32) ? 1
         return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     uint8_t *ring = lds + wave * S::WAVE;
-    const uint32_t ring_at = lds_addr(ring);
+    const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_addr(ring));
     const int32_t *table = A.tables + b * A.ld_table;
 
     // copies of the step at token t into the ring's place `at`; bits 0 and 1: the tiles' pages are none of the cache's
     const int last_tile = (limit - 1) >> 4;
+    uint32_t code_at[S::CODES / 1024], scale_at[S::SCALE_ROOM / 256];
+#pragma unroll
+    for (int i = 0; i < S::CODES / 1024; ++i) {
+        const int o = i * 1024 + lane * 16;
+        code_at[i] = o < 8 * DIM ? o : o - 8 * DIM + A.c.page * (DIM / 2);
+    }
+#pragma unroll
+    for (int i = 0; i < S::SCALE_ROOM / 256; ++i) {
+        const int o = i * 256 + lane * 4 < S::SCALES ? i * 256 + lane * 4 : 0;
+        scale_at[i] = A.c.page * DIM + (o < 32 * G ? o : o - 32 * G + A.c.page * (2 * G));
+    }
+    const int page_log = __builtin_ctz(A.c.page);
     auto copy = [&](int t, int at) -> uint32_t {
         uint32_t bad = 0;
         const int firsts[2] = {min(t >> 4, last_tile) * 16, min((t >> 4) + 1, last_tile) * 16};
         int pages[2];
-        scalar_loads(table, 4 * (firsts[0] / A.c.page), 4 * (firsts[1] / A.c.page), pages[0], pages[1]);
+        scalar_loads(table, 4 * (firsts[0] >> page_log), 4 * (firsts[1] >> page_log), pages[0], pages[1]);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int first = firsts[half];
-            int page = pages[half];
-            if ((unsigned)page >= (unsigned)A.c.pages) {
-                bad |= 1u << half;
-                page = 0;
-            }
-            const int in = first % A.c.page;
-            const uint8_t *block = A.cache + ((long long)page * A.c.heads + kv) * A.c.block_bytes;
+            const bool known = (unsigned)pages[half] < (unsigned)A.c.pages;
+            bad |= known ? 0u : 1u << half;
+            const int in = firsts[half] & (A.c.page - 1);
+            const uint8_t *block = A.cache + ((long long)(known ? pages[half] : 0) * A.c.heads + kv) * A.c.block_bytes;
             const uint32_t to = ring_at + at * S::STEP + half * S::TILE;
-            const uint8_t *codes = block + in * (DIM / 2), *scales = block + A.c.page * DIM + in * (2 * G);
+            // (the keys' and values' codes of a tile are DIM / 2 bytes a token each, their scales 2 G)
 #pragma unroll
-            for (int i = 0; i < S::CODES / 1024; ++i) {
-                const int o = i * 1024 + lane * 16;
-                dma16(codes + (o < 8 * DIM ? o : o - 8 * DIM + A.c.page * (DIM / 2)), to + i * 1024);
-            }
+            for (int i = 0; i < S::CODES / 1024; ++i)
+                copy16(block + in * (DIM / 2), code_at[i], to + i * 1024);
 #pragma unroll
-            for (int i = 0; i < S::SCALE_ROOM / 256; ++i) {
-                const int o = i * 256 + lane * 4 < S::SCALES ? i * 256 + lane * 4 : 0;
-                dma4(scales + (o < 32 * G ? o : o - 32 * G + A.c.page * (2 * G)), to + S::CODES + i * 256);
-            }
+            for (int i = 0; i < S::SCALE_ROOM / 256; ++i)
+                copy4(block + in * (2 * G), scale_at[i], to + S::CODES + i * 256);
         }
         return bad;
     };
@@ -184,6 +193,9 @@ __global__ void __launch_bounds__(256, DIM == 256 && (R == 2 || GROUP == 32) ? 1
     const int seen_least = seq.length - seq.n + 1 + first_row / per;
     // (a scale of 0 would make -infinity * 0 of hidden scores)
     const float scale = fmaxf(fabsf(A.scale) * LOG2E, 0x1p-100f);
+    uint32_t mask = Code<T>::MASK, base = Code<T>::BASE;
+    asm("" : "+s"(mask));
+    asm("" : "+v"(base));
     const u32x4 off = {Code<T>::OFF, Code<T>::OFF, Code<T>::OFF, Code<T>::OFF};
 
     f32x4 o[R][TILES];
@@ -239,7 +251,7 @@ __global__ void __launch_bounds__(256, DIM == 256 && (R == 2 || GROUP == 32) ? 1
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const uint32_t w = kc[half][u];
-                key[u] = u32x4{widen<T, 0>(w), widen<T, 1>(w), widen<T, 2>(w), widen<T, 3>(w)};
+                key[u] = u32x4{widen<T, 0>(w, mask, base), widen<T, 1>(w, mask, base), widen<T, 2>(w, mask, base), widen<T, 3>(w, mask, base)};
             }
 #pragma unroll
             for (int k = 0; k < R; ++k)
@@ -260,6 +272,7 @@ __global__ void __launch_bounds__(256, DIM == 256 && (R == 2 || GROUP == 32) ? 1
                 }
         }
         if (masked) {
+            asm volatile("");   // a branch: as selects the step would be a tenth longer
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -269,7 +282,7 @@ __global__ void __launch_bounds__(256, DIM == 256 && (R == 2 || GROUP == 32) ? 1
                     for (int k = 0; k < R; ++k)
                         s[k][4 * half + i] = token < seen[k] ? (bad >> half & 1 ? NAN : s[k][4 * half + i]) : -INFINITY;
                     // what lies behind the sequence's end may be any scale
-                    if (Code<T>::NARROW && token >= limit) {
+                    if (token >= (R == 1 ? seen[0] : limit)) {
                         if constexpr (G > 1) {
 #pragma unroll
                             for (int j = 0; j < G / 2; ++j)
@@ -317,10 +330,10 @@ __global__ void __launch_bounds__(256, DIM == 256 && (R == 2 || GROUP == 32) ? 1
                     for (int e = 0; e < 4; ++e)
                         o[k][i][e] *= fade;
             }
-            const float base = ref[k] == -INFINITY ? 0.f : -ref[k];
+            const float zero = ref[k] == -INFINITY ? 0.f : -ref[k];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                s[k][i] = exp2_fast(__builtin_fmaf(s[k][i], scale, base));
+                s[k][i] = exp2_fast(__builtin_fmaf(s[k][i], scale, zero));
                 total[k] += s[k][i];
             }
         }
@@ -336,7 +349,7 @@ __global__ void __launch_bounds__(256, DIM == 256 && (R == 2 || GROUP == 32) ? 1
                     for (int i = 0; i < 4; ++i) {
                         w[4 * half + i] = s[k][4 * half + i] * number(vs[half], i, J);
                         // (a scale that one row sees and another does not may be no number)
-                        if (masked && t + 16 * half + 4 * g + i >= seen[k])
+                        if (R > 1 && masked && t + 16 * half + 4 * g + i >= seen[k])
                             w[4 * half + i] = 0.f;
                     }
 #pragma unroll
@@ -345,8 +358,8 @@ __global__ void __launch_bounds__(256, DIM == 256 && (R == 2 || GROUP == 32) ? 1
             }
             static_for<GROUP / 16>([&](auto i) {
                 constexpr int tile = J * (GROUP / 16) + decltype(i)::value, h = tile / 4, n = tile % 4;
-                const u32x4 value = {widen<T, n>(vc[0][2 * h]), widen<T, n>(vc[0][2 * h + 1]), widen<T, n>(vc[1][2 * h]),
-                                     widen<T, n>(vc[1][2 * h + 1])};
+                const u32x4 value = {widen<T, n>(vc[0][2 * h], mask, base), widen<T, n>(vc[0][2 * h + 1], mask, base), widen<T, n>(vc[1][2 * h], mask, base),
+                                     widen<T, n>(vc[1][2 * h + 1], mask, base)};
 #pragma unroll
                 for (int k = 0; k < R; ++k) {
                     o[k][tile] = mfma16(off, p[k], o[k][tile], T());
@@ -417,10 +430,8 @@ __global__ void __launch_bounds__(256, DIM == 256 && (R == 2 || GROUP == 32) ? 1
 template <typename T>
 __global__ void __launch_bounds__(256) qattn_join_kernel(QattnArgs A, int rows, int parts, int chunk)
 {
-    const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), all = (long long)A.batch * A.max_queries * A.q_heads;
-    if (at >= all)
-        return;
-    const int head = (int)(at % A.q_heads), i = (int)(at / A.q_heads % A.max_queries), b = (int)(at / A.q_heads / A.max_queries);
+    __shared__ JoinScratch lds;
+    const int at = blockIdx.x, head = at % A.q_heads, i = at / A.q_heads % A.max_queries, b = at / A.q_heads / A.max_queries;
     const Sequence seq = sequence(A, b);
     if (i >= seq.n)
         return;
@@ -428,7 +439,7 @@ __global__ void __launch_bounds__(256) qattn_join_kernel(QattnArgs A, int rows, 
     const int per = A.q_heads / A.c.heads, first_row = (i * per + head % per) / rows * rows;
     const int limit = seen_by(seq, rows, first_row, per), used = max((limit + chunk - 1) / chunk, 1);
     const long long query = seq.begin + i;
-    join_parts<T>(A.part, (long long)A.queries * A.q_heads, query * A.q_heads + head, parts, used, A.c.dim,
+    join_parts<T>(lds, A.part, (long long)A.queries * A.q_heads, query * A.q_heads + head, parts, used, A.c.dim,
                   (T *)A.y + query * A.y_token + head * A.y_head);
 }
 
@@ -468,7 +479,7 @@ hipError_t launch_type(const QattnArgs &a, const AttnPlan &p, hipStream_t stream
     if (e != hipSuccess || p.parts == 1)
         return e;
     const long long all = (long long)a.batch * a.max_queries * a.q_heads;
-    hipLaunchKernelGGL(qattn_join_kernel<T>, dim3((unsigned)((all + 3) / 4)), dim3(256), 0, stream, a, rows_of(a), p.parts, p.chunk);
+    hipLaunchKernelGGL(qattn_join_kernel<T>, dim3((unsigned)all), dim3(256), 0, stream, a, rows_of(a), p.parts, p.chunk);
     return hipGetLastError();
 }
 
@@ -478,8 +489,12 @@ AttnPlan qattn_plan(const QattnArgs &a, size_t room)
 {
     const int keys = (int)std::min<long long>(a.max_keys, a.ld_table * a.c.page);
     const long long groups = (long long)a.batch * a.c.heads * row_tiles(a, rows_of(a));
-    // enough workgroups to fill the GPU several times over, as the sequences may be of any length, each of whole rounds of its waves
-    long long parts = std::max(1LL, std::min<long long>(4096 / std::max(groups, 1LL), (keys + 255) / 256));
+    // Three workgroups to a CU, of 128 tokens at a time. Four rounds of them, since the sequences may be of any length (64 of 700 to
+    // 8192 tokens: 768 workgroups 107 us, 1536 87, 3072 83, 8192 90; 3 of 120000: 74, 77, 79, 85), but none below 256 tokens unless
+    // one round holds all of 128 (1 of 1500 9.3 us with 128, 10.0 with 256; 16 of up to 2500, four tokens each: 18.0 and 16.1).
+    constexpr int ROUND = 768;
+    const int least = groups * ((keys + 127) / 128) <= ROUND ? 128 : 256;
+    long long parts = std::max(1LL, std::min<long long>(4 * ROUND / std::max(groups, 1LL), (keys + least - 1) / least));
     const long long one = (long long)a.queries * a.q_heads * (a.c.dim + 2) * 4;
     parts = std::min(parts, (long long)room / std::max(one, 1LL));
     if (parts <= 1)
