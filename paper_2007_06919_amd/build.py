@@ -29,11 +29,13 @@ FLAGS = [
     "-Wall", "-Wno-unused-function", "-Wno-unused-command-line-argument",
     "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,
 ]
+# the attention's vector units read and write what its matrix cores do: accumulators stay in vector registers as long as they fit
+FILE_FLAGS = {"attn.hip": ("-mllvm", "-amdgpu-mfma-vgpr-form=1")}
 
 
 def _compile(src: str, verbose: bool, extra) -> str:
     obj = os.path.join(BUILD, os.path.splitext(src)[0] + ".o")
-    cmd = [HIPCC, *FLAGS, *extra, "-c", os.path.join(CSRC, src), "-o", obj]
+    cmd = [HIPCC, *FLAGS, *FILE_FLAGS.get(src, ()), *extra, "-c", os.path.join(CSRC, src), "-o", obj]
     if verbose:
         print(" ".join(cmd), flush=True)
     r = subprocess.run(cmd, capture_output=True, text=True)

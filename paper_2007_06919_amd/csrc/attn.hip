@@ -1,45 +1,412 @@
 // Attention over keys and values of packed sequences. Definition: include/aqd.h.
+//
+// A workgroup has one sequence, one key head, 128 rows (queries times the query heads of the key head, a query's heads next to
+// one another) and a range of keys. Each of its four waves has 32 R rows. S^T = K Q^T and O^T = V^T P^T in 32 x 32 x 16 products: the
+// lane that has the scores of row r and tokens 4 h .. 4 h + 3 and so on is the lane that gives those weights to the
+// second product, so weights stay where they are. Q is in registers, tiles of K and V are copied straight into
+// a ring in LDS, in an order of their 16-byte pieces that leaves the reads without bank conflicts; V's columns come out of LDS
+// by the transposing read.
+//
+// A step of 32 keys has three parts that do not wait for one another: the scores of the next step and the sums of the
+// last one on the matrix cores, the weights of this one on the vector units (a running softmax whose reference moves
+// only when a score is above it by 2^8).
+//
+// The weights of hidden keys are 0, but 0 times an infinity or a NaN is not: rows whose result is no number are done
+// again one by one with nothing hidden in their sums.
+
+#include <algorithm>
 
 #include "attn_row.h"
 
 namespace aqd {
 namespace {
 
-template <typename T>
-__global__ void __launch_bounds__(64) attn_row_kernel(AttnArgs A)
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c, __bf16)
 {
-    __shared__ RowScratch lds;
-    const int i = blockIdx.x % A.max_queries, rest = blockIdx.x / A.max_queries, head = rest % A.q_heads, b = rest / A.q_heads;
-    const int begin = min(max(A.q_start[b], 0), A.queries), n = min(min(max(A.q_start[b + 1], 0), A.queries) - begin, A.max_queries);
-    if (i >= n)
+    typedef Operand<__bf16>::type V;
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c, _Float16)
+{
+    typedef Operand<_Float16>::type V;
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
+}
+
+// Of each 16 lanes, lane 4 i + j has the address of 4 numbers of row i; lane c of them gets number c % 4 of lanes
+// c / 4, 4 + c / 4, 8 + c / 4 and 12 + c / 4: a column of the four rows.
+__device__ __forceinline__ u32x2 read_columns(const uint8_t *p)
+{
+    typedef short V __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) V *L;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((L)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)p));
+}
+
+constexpr int ROWS = 128;   // of a workgroup
+
+template <int DIM>
+struct Tile {
+    static constexpr int KEYS = 32;                                          // of a tile
+    static constexpr int ROW = 2 * DIM, PIECES = DIM / 8;                    // bytes and 16-byte pieces of a row
+    static constexpr int SIDE = KEYS * ROW, RING = 3;
+    static constexpr int COPIES = SIDE / 4096;                               // of a wave, for keys or values of a tile
+    static constexpr int LDS = 2 * RING * SIDE;
+    // where piece c of row t stands: 16 rows' pieces at one c are in different banks, and so are 64 bytes of 4 rows
+    static __device__ __forceinline__ int key_place(int t, int c) { return DIM == 64 ? c ^ (t >> 1 & 7) : c ^ (t & 15); }
+    static __device__ __forceinline__ int value_place(int t, int c) { return DIM == 64 ? c ^ (t << 1 & 4) : c ^ (t << 2 & 12); }
+};
+
+struct Span2 {
+    int begin, n, first, m;   // queries and keys
+};
+__device__ __forceinline__ Span2 sequence(const AttnArgs &A, int b)
+{
+    Span2 s;
+    s.begin = min(max(A.q_start[b], 0), A.queries);
+    s.n = min(min(max(A.q_start[b + 1], 0), A.queries) - s.begin, A.max_queries);
+    s.first = min(max(A.k_start[b], 0), A.keys);
+    s.m = max(min(max(A.k_start[b + 1], 0), A.keys) - s.first, 0);
+    return s;
+}
+__device__ __forceinline__ int seen_by(const AttnArgs &A, const Span2 &s, int query)
+{
+    return A.causal ? max(s.m - s.n + 1 + query, 0) : s.m;
+}
+
+// DIRECT: rows of keys and values start at multiples of 4 bytes
+template <typename T, int DIM, bool DIRECT>
+__global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_kernel(AttnArgs A, int tiles, int parts, int chunk)
+{
+    typedef Tile<DIM> S;
+    constexpr int U = DIM / 16, C = DIM / 32;
+    __shared__ __align__(16) uint8_t lds[S::LDS];
+    const int per = A.q_heads / A.heads;
+    int rest = blockIdx.x;
+    const int kv = rest % A.heads;
+    rest /= A.heads;
+    const int b = rest % A.batch;
+    rest /= A.batch;
+    // the longest rows first
+    const int part = rest % parts, row_tile = tiles - 1 - rest / parts;
+    const Span2 seq = sequence(A, b);
+    const int rows = seq.n * per, first_row = row_tile * ROWS;
+    if (first_row >= rows)
         return;
-    const int first = min(max(A.k_start[b], 0), A.keys), m = max(min(max(A.k_start[b + 1], 0), A.keys) - first, 0);
-    const int keys = A.causal ? max(m - n + 1 + i, 0) : m, kv = head / (A.q_heads / A.heads);
-    const T *q = (const T *)A.q + (begin + i) * A.q_token + head * A.q_head;
-    const T *k = (const T *)A.k + first * A.k_token + kv * A.k_head, *v = (const T *)A.v + first * A.v_token + kv * A.v_head;
-    T *y = (T *)A.y + (begin + i) * A.y_token + head * A.y_head;
-    row_attention<256>(
-        lds, A.dim, keys, A.scale, [&](int c) { return (float)q[c]; }, [&](int j, int c) { return (float)k[j * A.k_token + c]; },
-        [&](int j, int c) { return (float)v[j * A.v_token + c]; }, [&](int c, float f) { y[c] = (T)f; });
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+    const int limit = seen_by(A, seq, min((first_row + ROWS - 1) / per, seq.n - 1)), start = part * chunk, end = min(start + chunk, limit);
+    if (part && start >= limit)
+        return;
+    const int wave_row = first_row + 32 * wave;
+    // keys of the wave's last row; none for rows past the last one
+    const int wave_end = wave_row < rows ? min(end, seen_by(A, seq, min((wave_row + 32 - 1) / per, seq.n - 1))) : 0;
+    const int seen_least = seen_by(A, seq, min(wave_row / per, seq.n - 1));
+    const uint8_t *key_base = (const uint8_t *)((const T *)A.k + seq.first * A.k_token + kv * A.k_head);
+    const uint8_t *value_base = (const uint8_t *)((const T *)A.v + seq.first * A.v_token + kv * A.v_head);
+
+    // 16-byte piece i of a wave's share of a tile: row and place. Rows past the end are the last one again.
+    const int dim_pieces = A.dim / 8;
+    auto copy_side = [&](bool values, int tile, int at) {
+        uint8_t *to = lds + (values ? S::RING * S::SIDE : 0) + at;
+        const uint8_t *base = values ? value_base : key_base;
+        const long long stride = 2 * (values ? A.v_token : A.k_token);
+        const int t0 = start + tile * S::KEYS;
+#pragma unroll
+        for (int i = 0; i < S::COPIES; ++i) {
+            const int piece = (wave * S::COPIES + i) * 64 + lane, row = piece / S::PIECES, place = piece % S::PIECES;
+            const int c = values ? S::value_place(row, place) : S::key_place(row, place);
+            const uint8_t *from = base + min(t0 + row, end - 1) * stride + 16 * c;
+            if (c < dim_pieces) {
+                if constexpr (DIRECT) {
+                    dma16(from, lds_addr(to) + (wave * S::COPIES + i) * 1024);
+                } else {
+                    typedef uint32_t V __attribute__((ext_vector_type(4), aligned(2)));
+                    *(u32x4 *)(to + piece * 16) = *(const V *)from;
+                }
+            }
+        }
+    };
+    const int count = (end - start + S::KEYS - 1) / S::KEYS;   // tiles
+    if (A.dim < DIM) {
+        // channels past the last are never copied
+        for (int i = threadIdx.x; i < S::LDS / 16; i += 256)
+            ((u32x4 *)lds)[i] = u32x4{0, 0, 0, 0};
+        __syncthreads();
+    }
+
+    // queries as operands, the sign of the scale with them
+    u32x4 q[U];
+    const uint32_t flip = A.scale < 0.f ? 0x80008000u : 0u;
+    const int row = wave_row + r, query = seq.begin + row / per, head = kv * per + row % per;
+    const int seen = row < rows ? seen_by(A, seq, row / per) : 0;
+    {
+        const T *p = (const T *)A.q + query * A.q_token + head * A.q_head + 8 * h;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            typedef T V __attribute__((ext_vector_type(8), aligned(2)));
+            u32x4 w = {0, 0, 0, 0};
+            if (row < rows && 16 * u + 8 * h < A.dim)
+                w = __builtin_bit_cast(u32x4, *(const V *)(p + 16 * u));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                q[u][e] = w[e] ^ flip;
+        }
+    }
+    // (a scale of 0 would make -infinity * 0 of hidden scores)
+    const float scale = fmaxf(fabsf(A.scale) * LOG2E, 0x1p-100f);
+
+    if (count > 0) {
+        copy_side(false, 0, 0);
+        copy_side(true, 0, 0);
+    }
+    if (count > 1)
+        copy_side(false, 1, S::SIDE);
+
+    f32x16 o[C], s[2];   // sums, and the scores of this step and the next
+    u32x4 p[2];          // the last step's weights
+    float ref = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            o[c][e] = 0.f;
+    p[0] = p[1] = u32x4{0, 0, 0, 0};
+    // the first step has no weights before it: zeros times zeros
+    for (int i = threadIdx.x; i < S::SIDE / 16; i += 256)
+        ((u32x4 *)(lds + (2 * S::RING - 1) * S::SIDE))[i] = u32x4{0, 0, 0, 0};
+
+    // scores of a tile's keys
+    auto scores = [&](const uint8_t *keys, f32x16 &to) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            to[e] = 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            to = mfma32(*(const u32x4 *)(keys + r * S::ROW + 16 * S::key_place(r, 2 * u + h)), q[u], to, T());
+    };
+    // adds the last step's weights times its values
+    auto sums = [&](const uint8_t *values) {
+        // lane 16 a + 4 i + j: row 16 v + 4 h + i (and 8 further), channels 32 c + 16 (a % 2) + 4 j ..
+        const int i = lane >> 2 & 3, j = lane & 3, a = lane >> 4 & 1;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                const int row = 16 * v + 4 * h + i, piece = 4 * c + 2 * a + (j >> 1);
+                const u32x2 x = read_columns(values + row * S::ROW + 16 * S::value_place(row, piece) + 8 * (j & 1));
+                const u32x2 y = read_columns(values + (row + 8) * S::ROW + 16 * S::value_place(row + 8, piece) + 8 * (j & 1));
+                o[c] = mfma32(u32x4{x[0], x[1], y[0], y[1]}, p[v], o[c], T());
+            }
+    };
+    // hides the scores that the row does not see, keys t .. + 31
+    auto hide = [&](int t, f32x16 &s) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            s[e] = t + (e & 3) + 8 * (e >> 2) + 4 * h < seen ? s[e] : -INFINITY;
+    };
+    // weights of a step's scores into p and total, with the reference as it is
+    auto weights = [&](const f32x16 &s) {
+        const float zero = ref == -INFINITY ? 0.f : -ref;
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            const float x = exp2_fast(__builtin_fmaf(s[e], scale, zero)), y = exp2_fast(__builtin_fmaf(s[e + 1], scale, zero));
+            total += x;
+            total += y;
+            p[e / 8][e / 2 % 4] = pack2<T>(x, y);
+        }
+    };
+    // one step: the next one's scores, the last one's sums, this one's weights
+    auto step = [&](const uint8_t *next_keys, const uint8_t *last_values, const f32x16 &s, f32x16 &next) {
+        const float before = total;
+        scores(next_keys, next);
+        sums(last_values);
+        weights(s);
+        float top = s[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e)
+            top = fmaxf(top, s[e]);
+        if (__builtin_amdgcn_ballot_w64(top * scale > ref + 8.f)) {
+            // seldom: the reference moves, and the weights are made again
+            top = fmaxf(ref, fmaxf(top, __shfl_xor(top, 32)) * scale);
+            const float fade = top == -INFINITY ? 1.f : exp2_fast(ref - top);
+            ref = top;
+            total = before * fade;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    o[c][e] *= fade;
+            weights(s);
+        }
+    };
+
+    const int steps = (wave_end - start + 31) / 32;                      // of this wave
+    const int open = max(min((seen_least - start) / 32, steps), 0);     // the first of them hide nothing
+    // places in the ring of the next tile, this one and the last one
+    int next_at = S::SIDE, this_at = 0, last_at = (S::RING - 1) * S::SIDE;
+    auto run = [&](int tile, f32x16 &s, f32x16 &next) {
+        // keys of the next tile and values of this one have arrived, and no wave reads what the copies below replace
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (tile + 1 < count)
+            copy_side(true, tile + 1, next_at);
+        if (tile + 2 < count)
+            copy_side(false, tile + 2, last_at);
+        const uint8_t *last_values = lds + S::RING * S::SIDE + last_at;
+        if (tile == 0)
+            scores(lds, s);
+        if (tile < steps) {
+            if (tile >= open)
+                hide(start + 32 * tile, s);
+            step(lds + next_at, last_values, s, next);
+        } else if (tile == steps && steps > 0) {
+            sums(last_values);
+        }
+        last_at = this_at;
+        this_at = next_at;
+        next_at = next_at == (S::RING - 1) * S::SIDE ? 0 : next_at + S::SIDE;
+    };
+#pragma nounroll
+    for (int tile = 0; tile < count; tile += 2) {
+        run(tile, s[0], s[1]);
+        if (tile + 1 == count)
+            break;
+        run(tile + 1, s[1], s[0]);
+    }
+    if (steps > 0 && steps == count)
+        sums(lds + S::RING * S::SIDE + last_at);
+
+    total += __shfl_xor(total, 32);
+    float check = total;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            check += o[c][e] * 0.f;   // NaN from an infinity or a NaN
+    const bool number = check < INFINITY;
+    const float inverse = parts > 1 ? 1.f : total != 0.f ? 1.f / total : 0.f;
+    const long long all = (long long)A.queries * A.q_heads;
+    if (__builtin_amdgcn_ballot_w64(!number) == 0 && row < rows) {
+        T *y = (T *)A.y + query * A.y_token + head * A.y_head;
+        const long long id = ((long long)query * A.q_heads + head) * parts + part;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const int channel = 32 * c + 8 * (e / 4) + 4 * h;
+                if (channel >= A.dim)
+                    continue;
+                f32x4 f;
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    f[x] = o[c][e + x] * inverse;
+                if (parts > 1) {
+                    *(f32x4 *)(A.part + id * A.dim + channel) = f;
+                } else {
+                    typedef u32x2 V __attribute__((aligned(2)));
+                    *(V *)(y + channel) = u32x2{pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3])};
+                }
+            }
+        if (parts > 1 && h == 0) {
+            float *stat = A.part + all * parts * A.dim + 2 * id;
+            stat[0] = ref;
+            stat[1] = total;
+        }
+    }
+    // every wave is done with the ring: those whose rows are no numbers do them again in its memory
+    __syncthreads();
+    if (__builtin_amdgcn_ballot_w64(!number) == 0)
+        return;
+    RowScratch &scratch = ((RowScratch *)lds)[wave];
+    for (int row = wave_row; row < min(wave_row + 32, rows); ++row) {
+        const int i = row / per, query = seq.begin + i, head = kv * per + row % per;
+        const T *from = (const T *)A.q + query * A.q_token + head * A.q_head;
+        const T *k = (const T *)key_base, *v = (const T *)value_base;
+        T *y = (T *)A.y + query * A.y_token + head * A.y_head;
+        const long long id = ((long long)query * A.q_heads + head) * parts + part;
+        row_attention<DIM>(
+            scratch, A.dim, start, min(end, seen_by(A, seq, i)), A.scale, [&](int c) { return (float)from[c]; },
+            [&](int j, int c) { return (float)k[j * A.k_token + c]; }, [&](int j, int c) { return (float)v[j * A.v_token + c]; },
+            [&](int c, float sum, float reference, float weight) {
+                if (parts == 1) {
+                    y[c] = (T)(weight != 0.f ? sum / weight : 0.f);
+                    return;
+                }
+                A.part[id * A.dim + c] = sum;
+                float *stat = A.part + all * parts * A.dim + 2 * id;
+                if (c == 0) {
+                    stat[0] = reference;
+                    stat[1] = weight;
+                }
+            });
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs A, int parts, int chunk)
+{
+    __shared__ JoinScratch lds;
+    const int at = blockIdx.x, head = at % A.q_heads, i = at / A.q_heads % A.max_queries, b = at / A.q_heads / A.max_queries;
+    const Span2 seq = sequence(A, b);
+    if (i >= seq.n)
+        return;
+    // the parts that its workgroup's rows have
+    const int per = A.q_heads / A.heads, last_row = (i * per + head % per) / ROWS * ROWS + ROWS - 1;
+    const int limit = seen_by(A, seq, min(last_row / per, seq.n - 1)), used = max((limit + chunk - 1) / chunk, 1);
+    const long long query = seq.begin + i;
+    join_parts<T>(lds, A.part, (long long)A.queries * A.q_heads, query * A.q_heads + head, parts, used, A.dim,
+                  (T *)A.y + query * A.y_token + head * A.y_head);
+}
+
+int row_tiles(const AttnArgs &a) { return (int)(((long long)a.max_queries * (a.q_heads / a.heads) + ROWS - 1) / ROWS); }
+
+template <typename T, int DIM>
+hipError_t launch_rows(const AttnArgs &a, const AttnPlan &p, hipStream_t stream)
+{
+    const int tiles = row_tiles(a);
+    const dim3 grid((unsigned)(a.heads * tiles * p.parts * a.batch));
+    const bool direct = (((uintptr_t)a.k | (uintptr_t)a.v) & 3) == 0 && ((a.k_token | a.k_head | a.v_token | a.v_head) & 1) == 0;
+    if (direct)
+        hipLaunchKernelGGL((attn_kernel<T, DIM, true>), grid, dim3(256), 0, stream, a, tiles, p.parts, p.chunk);
+    else
+        hipLaunchKernelGGL((attn_kernel<T, DIM, false>), grid, dim3(256), 0, stream, a, tiles, p.parts, p.chunk);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_type(const AttnArgs &a, const AttnPlan &p, hipStream_t stream)
+{
+    const hipError_t e = a.dim <= 64    ? launch_rows<T, 64>(a, p, stream)
+                         : a.dim <= 128 ? launch_rows<T, 128>(a, p, stream)
+                                        : launch_rows<T, 256>(a, p, stream);
+    if (e != hipSuccess || p.parts == 1)
+        return e;
+    const long long all = (long long)a.batch * a.max_queries * a.q_heads;
+    hipLaunchKernelGGL(attn_join_kernel<T>, dim3((unsigned)all), dim3(256), 0, stream, a, p.parts, p.chunk);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 AttnPlan attn_plan(const AttnArgs &a, size_t room)
 {
-    (void)room;
-    return {1, a.max_keys, 0};
+    const int keys = a.max_keys;
+    const long long groups = (long long)a.batch * a.heads * row_tiles(a);
+    long long parts = std::max(1LL, std::min<long long>(512 / std::max(groups, 1LL), (keys + 255) / 256));
+    const long long one = (long long)a.queries * a.q_heads * (a.dim + 2) * 4;
+    parts = std::min(parts, (long long)room / std::max(one, 1LL));
+    if (parts > 1) {
+        const long long chunk = ((keys + parts - 1) / parts + 63) / 64 * 64;
+        parts = (keys + chunk - 1) / chunk;
+        if (parts > 1)
+            return {(int)parts, (int)chunk, (size_t)(one * parts)};
+    }
+    return {1, INT32_MAX - 65536, 0};
 }
 
 hipError_t launch_attn(const AttnArgs &a, const AttnPlan &plan, hipStream_t stream)
 {
-    (void)plan;
-    const dim3 grid((unsigned)(a.batch * a.q_heads * a.max_queries));
-    if (a.type == AQD_F16)
-        hipLaunchKernelGGL(attn_row_kernel<_Float16>, grid, dim3(64), 0, stream, a);
-    else
-        hipLaunchKernelGGL(attn_row_kernel<__bf16>, grid, dim3(64), 0, stream, a);
-    return hipGetLastError();
+    return a.type == AQD_F16 ? launch_type<_Float16>(a, plan, stream) : launch_type<__bf16>(a, plan, stream);
 }
 
 }  // namespace aqd
