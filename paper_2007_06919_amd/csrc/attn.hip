@@ -35,13 +35,17 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c, _Float16)
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
 }
 
-// Of each 16 lanes, lane 4 i + j has the address of 4 numbers of row i; lane c of them gets number c % 4 of lanes
+// 16 bytes of LDS at byte address `at`
+__device__ __forceinline__ u32x4 read_piece(uint32_t at)
+{
+    return *(const __attribute__((address_space(3))) u32x4 *)(uintptr_t)at;
+}
+// Of each 16 lanes, lane 4 i + j has the LDS byte address of 4 numbers of row i; lane c of them gets number c % 4 of lanes
 // c / 4, 4 + c / 4, 8 + c / 4 and 12 + c / 4: a column of the four rows.
-__device__ __forceinline__ u32x2 read_columns(const uint8_t *p)
+__device__ __forceinline__ u32x2 read_columns(uint32_t at)
 {
     typedef short V __attribute__((ext_vector_type(4)));
-    typedef __attribute__((address_space(3))) V *L;
-    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((L)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)p));
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) V *)(uintptr_t)at));
 }
 
 constexpr int ROWS = 128;   // of a workgroup
@@ -50,7 +54,7 @@ template <int DIM>
 struct Tile {
     static constexpr int KEYS = 32;                                          // of a tile
     static constexpr int ROW = 2 * DIM, PIECES = DIM / 8;                    // bytes and 16-byte pieces of a row
-    static constexpr int SIDE = KEYS * ROW, RING = 3;
+    static constexpr int SIDE = KEYS * ROW, RING = 4;
     static constexpr int COPIES = SIDE / 4096;                               // of a wave, for keys or values of a tile
     static constexpr int LDS = 2 * RING * SIDE;
     // where piece c of row t stands: 16 rows' pieces at one c are in different banks, and so are 64 bytes of 4 rows
@@ -105,25 +109,40 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
     const uint8_t *key_base = (const uint8_t *)((const T *)A.k + seq.first * A.k_token + kv * A.k_head);
     const uint8_t *value_base = (const uint8_t *)((const T *)A.v + seq.first * A.v_token + kv * A.v_head);
 
-    // 16-byte piece i of a wave's share of a tile: row and place. Rows past the end are the last one again.
+    // 16-byte piece i of a wave's share of a tile: row, channels, and offset from the tile's first row
     const int dim_pieces = A.dim / 8;
-    auto copy_side = [&](bool values, int tile, int at) {
-        uint8_t *to = lds + (values ? S::RING * S::SIDE : 0) + at;
-        const uint8_t *base = values ? value_base : key_base;
-        const long long stride = 2 * (values ? A.v_token : A.k_token);
-        const int t0 = start + tile * S::KEYS;
+    const long long key_stride = 2 * A.k_token, value_stride = 2 * A.v_token;
+    uint32_t key_from[S::COPIES], value_from[S::COPIES];
+#pragma unroll
+    for (int i = 0; i < S::COPIES; ++i) {
+        const int piece = (wave * S::COPIES + i) * 64 + lane, row = piece / S::PIECES, place = piece % S::PIECES;
+        key_from[i] = (uint32_t)row * (uint32_t)key_stride + 16 * S::key_place(row, place);
+        value_from[i] = (uint32_t)row * (uint32_t)value_stride + 16 * S::value_place(row, place);
+    }
+    const uint32_t lds_at = __builtin_amdgcn_readfirstlane(lds_addr(lds));
+    auto copy_side = [&](bool values, int tile, int slot) {
+        const int to = (values ? S::RING : 0) * S::SIDE + slot * S::SIDE;
+        const uint8_t *base = (values ? value_base : key_base) + (long long)(start + tile * S::KEYS) * (values ? value_stride : key_stride);
+        const int last = end - 1 - (start + tile * S::KEYS);   // row of the tile
+        const long long stride = values ? value_stride : key_stride;
+        int at = lane;
+        if (last < S::KEYS - 1 || A.dim < DIM || !DIRECT)
+            asm volatile("" : "+v"(at));   // (or what it takes below would take registers all the time)
 #pragma unroll
         for (int i = 0; i < S::COPIES; ++i) {
-            const int piece = (wave * S::COPIES + i) * 64 + lane, row = piece / S::PIECES, place = piece % S::PIECES;
+            const int first = (wave * S::COPIES + i) * 64, row = (first + at) / S::PIECES, place = (first + at) % S::PIECES;
             const int c = values ? S::value_place(row, place) : S::key_place(row, place);
-            const uint8_t *from = base + min(t0 + row, end - 1) * stride + 16 * c;
-            if (c < dim_pieces) {
-                if constexpr (DIRECT) {
-                    dma16(from, lds_addr(to) + (wave * S::COPIES + i) * 1024);
-                } else {
-                    typedef uint32_t V __attribute__((ext_vector_type(4), aligned(2)));
-                    *(u32x4 *)(to + piece * 16) = *(const V *)from;
-                }
+            uint32_t from = values ? value_from[i] : key_from[i];
+            // rows past the end are the last one again
+            if (last < S::KEYS - 1)
+                from = (uint32_t)min(row, last) * (uint32_t)stride + 16 * c;
+            if (A.dim < DIM && c >= dim_pieces)
+                continue;
+            if constexpr (DIRECT) {
+                copy16(base, from, lds_at + to + first * 16);
+            } else {
+                typedef uint32_t V __attribute__((ext_vector_type(4), aligned(2)));
+                *(u32x4 *)(lds + to + (first + at) * 16) = *(const V *)(base + from);
             }
         }
     };
@@ -138,9 +157,10 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
     // queries as operands, the sign of the scale with them
     u32x4 q[U];
     const uint32_t flip = A.scale < 0.f ? 0x80008000u : 0u;
-    const int row = wave_row + r, query = seq.begin + row / per, head = kv * per + row % per;
-    const int seen = row < rows ? seen_by(A, seq, row / per) : 0;
+    int seen;   // keys
     {
+        const int row = wave_row + r, query = seq.begin + row / per, head = kv * per + row % per;
+        seen = row < rows ? seen_by(A, seq, row / per) : 0;
         const T *p = (const T *)A.q + query * A.q_token + head * A.q_head + 8 * h;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -156,12 +176,17 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
     // (a scale of 0 would make -infinity * 0 of hidden scores)
     const float scale = fmaxf(fabsf(A.scale) * LOG2E, 0x1p-100f);
 
+    // in the order in which the tiles are waited for
     if (count > 0) {
         copy_side(false, 0, 0);
         copy_side(true, 0, 0);
     }
-    if (count > 1)
-        copy_side(false, 1, S::SIDE);
+    if (count > 1) {
+        copy_side(false, 1, 1);
+        copy_side(true, 1, 1);
+    }
+    if (count > 2)
+        copy_side(false, 2, 2);
 
     f32x16 o[C], s[2];   // sums, and the scores of this step and the next
     u32x4 p[2];          // the last step's weights
@@ -176,26 +201,39 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
     for (int i = threadIdx.x; i < S::SIDE / 16; i += 256)
         ((u32x4 *)(lds + (2 * S::RING - 1) * S::SIDE))[i] = u32x4{0, 0, 0, 0};
 
-    // scores of a tile's keys
-    auto scores = [&](const uint8_t *keys, f32x16 &to) {
+    // LDS addresses of the lane's pieces in the first tile of keys and of values: other tiles, rows and half rows are constants away.
+    // (The compiler would make each from the lane's number again.)
+    constexpr int KEY_AT = U < 8 ? U : 8, VALUE_AT = C < 4 ? C : 4;
+    uint32_t key_at[KEY_AT], value_at[VALUE_AT];
+#pragma unroll
+    for (int u = 0; u < KEY_AT; ++u) {
+        key_at[u] = lds_at + r * S::ROW + 16 * S::key_place(r, 2 * u + h);
+        asm("" : "+v"(key_at[u]));
+    }
+#pragma unroll
+    for (int c = 0; c < VALUE_AT; ++c) {
+        // lane 16 a + 4 i + j: row 4 h + i, channels 32 c + 16 (a % 2) + 4 j ..
+        const int row = 4 * h + (lane >> 2 & 3), j = lane & 3, piece = 4 * c + 2 * (lane >> 4 & 1) + (j >> 1);
+        value_at[c] = lds_at + S::RING * S::SIDE + row * S::ROW + 16 * S::value_place(row, piece) + 8 * (j & 1);
+        asm("" : "+v"(value_at[c]));
+    }
+    // scores of the keys of the tile at a place in the ring
+    auto scores = [&](int place, f32x16 &to) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
             to[e] = 0.f;
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            to = mfma32(*(const u32x4 *)(keys + r * S::ROW + 16 * S::key_place(r, 2 * u + h)), q[u], to, T());
+            to = mfma32(read_piece(key_at[u % KEY_AT] + place * S::SIDE + u / KEY_AT * 256), q[u], to, T());
     };
     // adds the last step's weights times its values
-    auto sums = [&](const uint8_t *values) {
-        // lane 16 a + 4 i + j: row 16 v + 4 h + i (and 8 further), channels 32 c + 16 (a % 2) + 4 j ..
-        const int i = lane >> 2 & 3, j = lane & 3, a = lane >> 4 & 1;
+    auto sums = [&](int place) {
 #pragma unroll
-        for (int c = 0; c < C; ++c)
+        for (int v = 0; v < 2; ++v)
 #pragma unroll
-            for (int v = 0; v < 2; ++v) {
-                const int row = 16 * v + 4 * h + i, piece = 4 * c + 2 * a + (j >> 1);
-                const u32x2 x = read_columns(values + row * S::ROW + 16 * S::value_place(row, piece) + 8 * (j & 1));
-                const u32x2 y = read_columns(values + (row + 8) * S::ROW + 16 * S::value_place(row + 8, piece) + 8 * (j & 1));
+            for (int c = 0; c < C; ++c) {
+                const uint32_t at = value_at[c % VALUE_AT] + place * S::SIDE + c / VALUE_AT * 256 + 16 * v * S::ROW;
+                const u32x2 x = read_columns(at), y = read_columns(at + 8 * S::ROW);
                 o[c] = mfma32(u32x4{x[0], x[1], y[0], y[1]}, p[v], o[c], T());
             }
     };
@@ -205,76 +243,90 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
         for (int e = 0; e < 16; ++e)
             s[e] = t + (e & 3) + 8 * (e >> 2) + 4 * h < seen ? s[e] : -INFINITY;
     };
-    // weights of a step's scores into p and total, with the reference as it is
+    // weights of a step's scores into p, with the reference as it is; returns their sum as rounded
     auto weights = [&](const f32x16 &s) {
         const float zero = ref == -INFINITY ? 0.f : -ref;
+        float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
             const float x = exp2_fast(__builtin_fmaf(s[e], scale, zero)), y = exp2_fast(__builtin_fmaf(s[e + 1], scale, zero));
-            total += x;
-            total += y;
             p[e / 8][e / 2 % 4] = pack2<T>(x, y);
+            sum = add2(p[e / 8][e / 2 % 4], sum, T());
         }
+        return sum;
     };
     // one step: the next one's scores, the last one's sums, this one's weights
-    auto step = [&](const uint8_t *next_keys, const uint8_t *last_values, const f32x16 &s, f32x16 &next) {
-        const float before = total;
-        scores(next_keys, next);
-        sums(last_values);
-        weights(s);
-        float top = s[0];
+    auto step = [&](int next_place, int last_place, const f32x16 &s, f32x16 &next) {
+        scores(next_place, next);
+        sums(last_place);
+        float sum = weights(s);
+        // the reference need not be the largest score: weights up to 2^12 are as good as up to 1
+        if (__builtin_amdgcn_ballot_w64(sum > 4096.f || ref == -INFINITY)) {
+            float top = s[0];
 #pragma unroll
-        for (int e = 1; e < 16; ++e)
-            top = fmaxf(top, s[e]);
-        if (__builtin_amdgcn_ballot_w64(top * scale > ref + 8.f)) {
-            // seldom: the reference moves, and the weights are made again
+            for (int e = 1; e < 16; ++e)
+                top = fmaxf(top, s[e]);
             top = fmaxf(ref, fmaxf(top, __shfl_xor(top, 32)) * scale);
             const float fade = top == -INFINITY ? 1.f : exp2_fast(ref - top);
             ref = top;
-            total = before * fade;
+            total *= fade;
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     o[c][e] *= fade;
-            weights(s);
+            sum = weights(s);
         }
+        total += sum;
     };
 
     const int steps = (wave_end - start + 31) / 32;                      // of this wave
     const int open = max(min((seen_least - start) / 32, steps), 0);     // the first of them hide nothing
-    // places in the ring of the next tile, this one and the last one
-    int next_at = S::SIDE, this_at = 0, last_at = (S::RING - 1) * S::SIDE;
-    auto run = [&](int tile, f32x16 &s, f32x16 &next) {
-        // keys of the next tile and values of this one have arrived, and no wave reads what the copies below replace
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (tile + 1 < count)
-            copy_side(true, tile + 1, next_at);
+    // Until keys of the next tile and values of this one have arrived (those of the tile behind may be under way), and no wave
+    // reads what is copied now.
+    auto arrive = [&](int tile, int far, int last) {
+        if (DIRECT && tile + 2 < count)
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * S::COPIES) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (tile + 2 < count)
-            copy_side(false, tile + 2, last_at);
-        const uint8_t *last_values = lds + S::RING * S::SIDE + last_at;
-        if (tile == 0)
-            scores(lds, s);
-        if (tile < steps) {
-            if (tile >= open)
-                hide(start + 32 * tile, s);
-            step(lds + next_at, last_values, s, next);
-        } else if (tile == steps && steps > 0) {
-            sums(last_values);
-        }
-        last_at = this_at;
-        this_at = next_at;
-        next_at = next_at == (S::RING - 1) * S::SIDE ? 0 : next_at + S::SIDE;
+            copy_side(true, tile + 2, far);
+        if (tile + 3 < count)
+            copy_side(false, tile + 3, last);
     };
-#pragma nounroll
-    for (int tile = 0; tile < count; tile += 2) {
-        run(tile, s[0], s[1]);
-        if (tile + 1 == count)
-            break;
-        run(tile + 1, s[1], s[0]);
+    // tile t, at place t % RING of the ring; whether it was the wave's last
+    auto run = [&](auto place, int tile, f32x16 &s, f32x16 &next) {
+        constexpr int AT = decltype(place)::value, NEXT = (AT + 1) % S::RING, FAR = (AT + 2) % S::RING, LAST = (AT + 3) % S::RING;
+        arrive(tile, FAR, LAST);
+        if (tile >= open)
+            hide(start + 32 * tile, s);
+        step(NEXT, LAST, s, next);
+        return tile + 1 == steps;
+    };
+    if (steps > 0) {
+        if (DIRECT && count > 2)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * S::COPIES) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
-    if (steps > 0 && steps == count)
-        sums(lds + S::RING * S::SIDE + last_at);
+    __syncthreads();
+    if (steps > 0) {
+        scores(0, s[0]);
+#pragma nounroll
+        for (int tile = 0;; tile += 4) {
+            if (run(std::integral_constant<int, 0>(), tile, s[0], s[1]) || run(std::integral_constant<int, 1>(), tile + 1, s[1], s[0]) ||
+                run(std::integral_constant<int, 2>(), tile + 2, s[0], s[1]) || run(std::integral_constant<int, 3>(), tile + 3, s[1], s[0]))
+                break;
+        }
+    }
+    // the other waves' tiles
+    int tile = max(steps, 0);
+    if (tile < count)
+        arrive(tile, (tile + 2) % S::RING, (tile + 3) % S::RING);
+    if (steps > 0)
+        sums((tile + 3) % S::RING);
+    for (++tile; tile < count; ++tile)
+        arrive(tile, (tile + 2) % S::RING, (tile + 3) % S::RING);
 
     total += __shfl_xor(total, 32);
     float check = total;
@@ -286,7 +338,10 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
     const bool number = check < INFINITY;
     const float inverse = parts > 1 ? 1.f : total != 0.f ? 1.f / total : 0.f;
     const long long all = (long long)A.queries * A.q_heads;
+    int row = wave_row + r;
+    asm volatile("" : "+v"(row));   // (made again here, not kept since the start)
     if (__builtin_amdgcn_ballot_w64(!number) == 0 && row < rows) {
+        const int query = seq.begin + row / per, head = kv * per + row % per;
         T *y = (T *)A.y + query * A.y_token + head * A.y_head;
         const long long id = ((long long)query * A.q_heads + head) * parts + part;
 #pragma unroll
@@ -360,13 +415,18 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs A, int parts, i
 
 int row_tiles(const AttnArgs &a) { return (int)(((long long)a.max_queries * (a.q_heads / a.heads) + ROWS - 1) / ROWS); }
 
+// whether the copies can take rows as they lie: at multiples of 4 bytes, a tile's within 32 bits
+bool direct(const AttnArgs &a)
+{
+    return (((uintptr_t)a.k | (uintptr_t)a.v) & 3) == 0 && ((a.k_token | a.k_head | a.v_token | a.v_head) & 1) == 0;
+}
+
 template <typename T, int DIM>
 hipError_t launch_rows(const AttnArgs &a, const AttnPlan &p, hipStream_t stream)
 {
     const int tiles = row_tiles(a);
     const dim3 grid((unsigned)(a.heads * tiles * p.parts * a.batch));
-    const bool direct = (((uintptr_t)a.k | (uintptr_t)a.v) & 3) == 0 && ((a.k_token | a.k_head | a.v_token | a.v_head) & 1) == 0;
-    if (direct)
+    if (direct(a))
         hipLaunchKernelGGL((attn_kernel<T, DIM, true>), grid, dim3(256), 0, stream, a, tiles, p.parts, p.chunk);
     else
         hipLaunchKernelGGL((attn_kernel<T, DIM, false>), grid, dim3(256), 0, stream, a, tiles, p.parts, p.chunk);

@@ -36,6 +36,18 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     return __builtin_bit_cast(uint32_t, v);
 }
 
+// sum + both numbers of a pair
+__device__ __forceinline__ float add2(uint32_t a, float sum, __bf16)
+{
+    typedef __bf16 V __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(V, a), V{(__bf16)1.f, (__bf16)1.f}, sum, false);
+}
+__device__ __forceinline__ float add2(uint32_t a, float sum, _Float16)
+{
+    typedef _Float16 V __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(V, a), V{(_Float16)1.f, (_Float16)1.f}, sum, false);
+}
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 constexpr float LOG2E = 1.44269504088896340736f;
@@ -118,6 +130,20 @@ __device__ __forceinline__ void join_parts(JoinScratch &lds, const float *part, 
         v[e] = (T)(sum[e] * inverse);
     *(V *)(y + c) = v;
 }
+
+// 16 or 4 bytes per lane from `offset` bytes past a wave-uniform address straight into LDS at la + 16 * lane
+// or 4 * lane (see dma16)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void copy16(const uint8_t *base, uint32_t offset, uint32_t la)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(la), "v"(offset), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void copy4(const uint8_t *base, uint32_t offset, uint32_t la)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(la), "v"(offset), "s"(base) : "memory", "m0");
+}
+#pragma clang diagnostic pop
 
 }  // namespace
 }  // namespace aqd

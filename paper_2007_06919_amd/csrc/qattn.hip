@@ -49,20 +49,6 @@ __device__ __forceinline__ uint32_t widen(uint32_t w, uint32_t mask, uint32_t ba
     return (w & mask) | base;
 }
 
-// 16 or 4 bytes per lane from `offset` bytes past a wave-uniform address straight into LDS at la + 16 * lane
-// or 4 * lane (see dma16)
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void copy16(const uint8_t *base, uint32_t offset, uint32_t la)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(la), "v"(offset), "s"(base) : "memory", "m0");
-}
-__device__ __forceinline__ void copy4(const uint8_t *base, uint32_t offset, uint32_t la)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(la), "v"(offset), "s"(base) : "memory", "m0");
-}
-#pragma clang diagnostic pop
-
 // two words at byte offsets of a wave-uniform address, through the scalar cache (a vector load would wait for the copies)
 __device__ __forceinline__ void scalar_loads(const int32_t *p, int a, int b, int &x, int &y)
 {
