@@ -147,12 +147,24 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
         }
     };
     const int count = (end - start + S::KEYS - 1) / S::KEYS;   // tiles
-    if (A.dim < DIM) {
-        // channels past the last are never copied
-        for (int i = threadIdx.x; i < S::LDS / 16; i += 256)
-            ((u32x4 *)lds)[i] = u32x4{0, 0, 0, 0};
+    // The first step has no weights before it: zeros times zeros, the values of a tile before the first. Channels past the last are
+    // never copied.
+    for (int i = (A.dim < DIM ? 0 : (2 * S::RING - 1) * S::SIDE / 16) + threadIdx.x; i < S::LDS / 16; i += 256)
+        ((u32x4 *)lds)[i] = u32x4{0, 0, 0, 0};
+    if (A.dim < DIM)
         __syncthreads();
+
+    // in the order in which the tiles are waited for
+    if (count > 0) {
+        copy_side(false, 0, 0);
+        copy_side(true, 0, 0);
     }
+    if (count > 1) {
+        copy_side(false, 1, 1);
+        copy_side(true, 1, 1);
+    }
+    if (count > 2)
+        copy_side(false, 2, 2);
 
     // queries as operands, the sign of the scale with them
     u32x4 q[U];
@@ -176,18 +188,6 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
     // (a scale of 0 would make -infinity * 0 of hidden scores)
     const float scale = fmaxf(fabsf(A.scale) * LOG2E, 0x1p-100f);
 
-    // in the order in which the tiles are waited for
-    if (count > 0) {
-        copy_side(false, 0, 0);
-        copy_side(true, 0, 0);
-    }
-    if (count > 1) {
-        copy_side(false, 1, 1);
-        copy_side(true, 1, 1);
-    }
-    if (count > 2)
-        copy_side(false, 2, 2);
-
     f32x16 o[C], s[2];   // sums, and the scores of this step and the next
     u32x4 p[2];          // the last step's weights
     float ref = -INFINITY, total = 0.f;
@@ -197,10 +197,6 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
         for (int e = 0; e < 16; ++e)
             o[c][e] = 0.f;
     p[0] = p[1] = u32x4{0, 0, 0, 0};
-    // the first step has no weights before it: zeros times zeros
-    for (int i = threadIdx.x; i < S::SIDE / 16; i += 256)
-        ((u32x4 *)(lds + (2 * S::RING - 1) * S::SIDE))[i] = u32x4{0, 0, 0, 0};
-
     // LDS addresses of the lane's pieces in the first tile of keys and of values: other tiles, rows and half rows are constants away.
     // (The compiler would make each from the lane's number again.)
     constexpr int KEY_AT = U < 8 ? U : 8, VALUE_AT = C < 4 ? C : 4;
@@ -217,25 +213,13 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
         value_at[c] = lds_at + S::RING * S::SIDE + row * S::ROW + 16 * S::value_place(row, piece) + 8 * (j & 1);
         asm("" : "+v"(value_at[c]));
     }
-    // scores of the keys of the tile at a place in the ring
-    auto scores = [&](int place, f32x16 &to) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-            to[e] = 0.f;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            to = mfma32(read_piece(key_at[u % KEY_AT] + place * S::SIDE + u / KEY_AT * 256), q[u], to, T());
-    };
-    // adds the last step's weights times its values
-    auto sums = [&](int place) {
-#pragma unroll
-        for (int v = 0; v < 2; ++v)
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const uint32_t at = value_at[c % VALUE_AT] + place * S::SIDE + c / VALUE_AT * 256 + 16 * v * S::ROW;
-                const u32x2 x = read_columns(at), y = read_columns(at + 8 * S::ROW);
-                o[c] = mfma32(u32x4{x[0], x[1], y[0], y[1]}, p[v], o[c], T());
-            }
+    // of the tiles at a place in the ring: 16 channels of the keys, and the operand of product i of 2 C of the values
+    auto key = [&](int place, int u) { return read_piece(key_at[u % KEY_AT] + place * S::SIDE + u / KEY_AT * 256); };
+    auto value = [&](int place, int i) {
+        const int v = i / C, c = i % C;
+        const uint32_t at = value_at[c % VALUE_AT] + place * S::SIDE + c / VALUE_AT * 256 + 16 * v * S::ROW;
+        const u32x2 x = read_columns(at), y = read_columns(at + 8 * S::ROW);
+        return u32x4{x[0], x[1], y[0], y[1]};
     };
     // hides the scores that the row does not see, keys t .. + 31
     auto hide = [&](int t, f32x16 &s) {
@@ -243,23 +227,46 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
         for (int e = 0; e < 16; ++e)
             s[e] = t + (e & 3) + 8 * (e >> 2) + 4 * h < seen ? s[e] : -INFINITY;
     };
-    // weights of a step's scores into p, with the reference as it is; returns their sum as rounded
-    auto weights = [&](const f32x16 &s) {
+    // weights of scores e, e + 1 (as exponents) into p; adds them to sum as rounded
+    auto weigh = [&](f32x16 &s, int e, float &sum) {
+        p[e / 8][e / 2 % 4] = pack2<T>(exp2_fast(s[e]), exp2_fast(s[e + 1]));
+        sum = add2(p[e / 8][e / 2 % 4], sum, T());
+    };
+    // one step: the next one's scores, the last one's sums, this one's weights, in the order in which they are issued: reads two
+    // products ahead, the exponentials of two weights under two matrix instructions
+    auto step = [&](int next_place, int last_place, f32x16 &s, f32x16 &next) {
+        constexpr int AHEAD = 2;
+        u32x4 keys[AHEAD + 1], values[AHEAD + 1];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            keys[u] = key(next_place, u);
+            values[u] = value(last_place, u);
+        }
+        const u32x4 last[2] = {p[0], p[1]};
         const float zero = ref == -INFINITY ? 0.f : -ref;
         float sum = 0.f;
+        f32x16 x;
 #pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-            const float x = exp2_fast(__builtin_fmaf(s[e], scale, zero)), y = exp2_fast(__builtin_fmaf(s[e + 1], scale, zero));
-            p[e / 8][e / 2 % 4] = pack2<T>(x, y);
-            sum = add2(p[e / 8][e / 2 % 4], sum, T());
+        for (int e = 0; e < 16; ++e) {
+            x[e] = __builtin_fmaf(s[e], scale, zero);
+            next[e] = 0.f;
         }
-        return sum;
-    };
-    // one step: the next one's scores, the last one's sums, this one's weights
-    auto step = [&](int next_place, int last_place, const f32x16 &s, f32x16 &next) {
-        scores(next_place, next);
-        sums(last_place);
-        float sum = weights(s);
+        __builtin_amdgcn_sched_barrier(0);
+        static_assert(U == 2 * C, "products in pairs");
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u + AHEAD < U) {
+                keys[(u + AHEAD) % (AHEAD + 1)] = key(next_place, u + AHEAD);
+                values[(u + AHEAD) % (AHEAD + 1)] = value(last_place, u + AHEAD);
+            }
+            next = mfma32(keys[u % (AHEAD + 1)], q[u], next, T());
+            o[u % C] = mfma32(values[u % (AHEAD + 1)], last[u / C], o[u % C], T());
+#pragma unroll
+            for (int e = 16 * u / U; e < 16 * (u + 1) / U; ++e)
+                if (e % 2 == 0)
+                    weigh(x, e, sum);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         // the reference need not be the largest score: weights up to 2^12 are as good as up to 1
         if (__builtin_amdgcn_ballot_w64(sum > 4096.f || ref == -INFINITY)) {
             float top = s[0];
@@ -275,7 +282,14 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     o[c][e] *= fade;
-            sum = weights(s);
+            const float shift = top == -INFINITY ? 0.f : -top;
+            sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                x[e] = __builtin_fmaf(s[e], scale, shift);
+#pragma unroll
+            for (int e = 0; e < 16; e += 2)
+                weigh(x, e, sum);
         }
         total += sum;
     };
@@ -303,15 +317,14 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
         step(NEXT, LAST, s, next);
         return tile + 1 == steps;
     };
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if (steps > 0) {
-        if (DIRECT && count > 2)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * S::COPIES) : "memory");
-        else
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    }
-    __syncthreads();
-    if (steps > 0) {
-        scores(0, s[0]);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            s[0][e] = 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            s[0] = mfma32(key(0, u), q[u], s[0], T());
 #pragma nounroll
         for (int tile = 0;; tile += 4) {
             if (run(std::integral_constant<int, 0>(), tile, s[0], s[1]) || run(std::integral_constant<int, 1>(), tile + 1, s[1], s[0]) ||
@@ -324,7 +337,9 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
     if (tile < count)
         arrive(tile, (tile + 2) % S::RING, (tile + 3) % S::RING);
     if (steps > 0)
-        sums((tile + 3) % S::RING);
+#pragma unroll
+        for (int i = 0; i < 2 * C; ++i)
+            o[i % C] = mfma32(value((tile + 3) % S::RING, i), p[i / C], o[i % C], T());
     for (++tile; tile < count; ++tile)
         arrive(tile, (tile + 2) % S::RING, (tile + 3) % S::RING);
 
