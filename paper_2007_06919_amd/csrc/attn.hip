@@ -412,11 +412,14 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
     }
 }
 
-template <typename T>
+template <typename T, int WAVES>
 __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs A, int parts, int chunk)
 {
-    __shared__ JoinScratch lds;
-    const int at = blockIdx.x, head = at % A.q_heads, i = at / A.q_heads % A.max_queries, b = at / A.q_heads / A.max_queries;
+    __shared__ JoinScratch<WAVES> lds;
+    const int at = WAVES > 1 ? blockIdx.x : blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (at >= A.batch * A.max_queries * A.q_heads)
+        return;
+    const int head = at % A.q_heads, i = at / A.q_heads % A.max_queries, b = at / A.q_heads / A.max_queries;
     const Span2 seq = sequence(A, b);
     if (i >= seq.n)
         return;
@@ -424,7 +427,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs A, int parts, i
     const int per = A.q_heads / A.heads, last_row = (i * per + head % per) / ROWS * ROWS + ROWS - 1;
     const int limit = seen_by(A, seq, min(last_row / per, seq.n - 1)), used = max((limit + chunk - 1) / chunk, 1);
     const long long query = seq.begin + i;
-    join_parts<T>(lds, A.part, (long long)A.queries * A.q_heads, query * A.q_heads + head, parts, used, A.dim,
+    join_parts<T, WAVES>(lds, A.part, (long long)A.queries * A.q_heads, query * A.q_heads + head, parts, used, A.dim,
                   (T *)A.y + query * A.y_token + head * A.y_head);
 }
 
@@ -456,27 +459,43 @@ hipError_t launch_type(const AttnArgs &a, const AttnPlan &p, hipStream_t stream)
                                         : launch_rows<T, 256>(a, p, stream);
     if (e != hipSuccess || p.parts == 1)
         return e;
-    const long long all = (long long)a.batch * a.max_queries * a.q_heads;
-    hipLaunchKernelGGL(attn_join_kernel<T>, dim3((unsigned)all), dim3(256), 0, stream, a, p.parts, p.chunk);
+    const unsigned all = (unsigned)a.batch * a.max_queries * a.q_heads;
+    if (p.parts <= JOIN_FEW)
+        hipLaunchKernelGGL((attn_join_kernel<T, 1>), dim3((all + 3) / 4), dim3(256), 0, stream, a, p.parts, p.chunk);
+    else
+        hipLaunchKernelGGL((attn_join_kernel<T, 4>), dim3(all), dim3(256), 0, stream, a, p.parts, p.chunk);
     return hipGetLastError();
 }
 
 }  // namespace
 
+// The split that a model of the time finds fastest, in us: a workgroup takes START and per 32 keys ALONE, or PAIR where two share a CU;
+// a second launch JOIN, a row's share of it, and the parts' bytes.
 AttnPlan attn_plan(const AttnArgs &a, size_t room)
 {
-    const int keys = a.max_keys;
-    const long long groups = (long long)a.batch * a.heads * row_tiles(a);
-    long long parts = std::max(1LL, std::min<long long>(512 / std::max(groups, 1LL), (keys + 255) / 256));
-    const long long one = (long long)a.queries * a.q_heads * (a.dim + 2) * 4;
-    parts = std::min(parts, (long long)room / std::max(one, 1LL));
-    if (parts > 1) {
-        const long long chunk = ((keys + parts - 1) / parts + 63) / 64 * 64;
-        parts = (keys + chunk - 1) / chunk;
-        if (parts > 1)
-            return {(int)parts, (int)chunk, (size_t)(one * parts)};
+    constexpr double START = 5.0, ALONE = 0.6, PAIR = 1.0, JOIN = 4.0, JOIN_ROW = 0.0004, MEMORY = 4e6;
+    constexpr int CUS = 256;
+    const int keys = a.max_keys, steps = (keys + 31) / 32;
+    const double groups = (double)a.batch * a.heads * row_tiles(a), rows = (double)a.queries * a.q_heads;
+    const double one = rows * (a.dim + 2) * 4;
+    AttnPlan best = {1, INT32_MAX - 65536, 0};
+    double least = 1e30;
+    for (int parts : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128}) {
+        if (parts > 1 && (one * parts > (double)room || steps < 2 * parts))
+            break;
+        const int each = (steps + parts - 1) / parts;
+        const double all = groups * parts;
+        const double t = (all <= CUS ? START + ALONE * each : std::max(1.0, all / (2 * CUS)) * (START + PAIR * each)) +
+                         (parts > 1 ? JOIN + JOIN_ROW * rows + 2 * one * parts / MEMORY : 0.0);
+        if (t < least) {
+            least = t;
+            if (parts > 1) {
+                const int used = (steps + each - 1) / each;
+                best = {used, 32 * each, (size_t)(one * used)};
+            }
+        }
     }
-    return {1, INT32_MAX - 65536, 0};
+    return best;
 }
 
 hipError_t launch_attn(const AttnArgs &a, const AttnPlan &plan, hipStream_t stream)

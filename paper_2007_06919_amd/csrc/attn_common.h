@@ -53,17 +53,23 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 constexpr float LOG2E = 1.44269504088896340736f;
 
 // The parts of one row, sums [parts][dim] and, behind all rows' sums, [parts][2] references and totals: the row is
-// sum_p o_p 2^(ref_p - ref) / sum_p l_p 2^(ref_p - ref), zeros where there is no weight at all. One workgroup of four waves: 64 lanes
-// have four channels each, or for shorter rows several parts at a time.
+// sum_p o_p 2^(ref_p - ref) / sum_p l_p 2^(ref_p - ref), zeros where there is no weight at all. WAVES waves (1 for few parts: rows
+// are many then, and a wave needs no barrier), of which 16, 32 or 64 lanes have four channels of a part each.
+template <int WAVES>
 struct JoinScratch {
-    float sum[256][4], most[4], total[4];
+    f32x4 sum[WAVES][64];
+    float most[WAVES], total[WAVES];
 };
-template <typename T>
-__device__ __forceinline__ void join_parts(JoinScratch &lds, const float *part, long long rows, long long row, int all, int parts, int dim, T *y)
+constexpr int JOIN_FEW = 16;   // parts that one wave joins
+
+template <typename T, int WAVES>
+__device__ __forceinline__ void join_parts(JoinScratch<WAVES> &lds, const float *part, long long rows, long long row, int all, int parts,
+                                           int dim, T *y)
 {
     const float *o = part + row * all * dim, *stat = part + rows * all * dim + row * all * 2;
-    const int lanes = (dim + 3) / 4, each = 256 / lanes, c = threadIdx.x % lanes * 4;
-    const int first = (int)threadIdx.x < each * lanes ? threadIdx.x / lanes : parts;
+    const int lanes = dim <= 64 ? 16 : dim <= 128 ? 32 : 64, each = 64 * WAVES / lanes;
+    const int thread = WAVES > 1 ? threadIdx.x : threadIdx.x & 63, wave = thread >> 6;
+    const int c = thread % lanes * 4, first = c < dim ? thread / lanes : parts;
     // the first loads of the sums are under way with those of the references
     constexpr int EARLY = 4;
     f32x4 early[EARLY];
@@ -81,47 +87,58 @@ __device__ __forceinline__ void join_parts(JoinScratch &lds, const float *part, 
         }
     }
     float ref = -INFINITY;
-    for (int p = threadIdx.x; p < parts; p += 256)
+    for (int p = thread; p < parts; p += 64 * WAVES)
         ref = fmaxf(ref, stat[2 * p]);
     for (int d = 32; d; d >>= 1)
         ref = fmaxf(ref, __shfl_xor(ref, d));
-    if ((threadIdx.x & 63) == 0)
-        lds.most[threadIdx.x >> 6] = ref;
-    __syncthreads();
-    ref = fmaxf(fmaxf(lds.most[0], lds.most[1]), fmaxf(lds.most[2], lds.most[3]));
+    if constexpr (WAVES > 1) {
+        if ((thread & 63) == 0)
+            lds.most[wave] = ref;
+        __syncthreads();
+        for (int w = 0; w < WAVES; ++w)
+            ref = fmaxf(ref, lds.most[w]);
+    }
     const float base = ref == -INFINITY ? 0.f : ref;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
     float total = 0.f;
-#pragma unroll
-    for (int u = 0; u < EARLY; ++u) {
-        const float f = exp2_fast(early_ref[u] - base);
-        total += f * early_total[u];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            sum[e] += f * early[u][e];
-    }
-#pragma unroll 4
-    for (int p = first + EARLY * each; p < parts; p += each) {
-        const float f = exp2_fast(stat[2 * p] - base);
-        const f32x4 v = *(const f32x4 *)(o + (long long)p * dim + c);
-        total += f * stat[2 * p + 1];
+    auto add = [&](float r, float l, f32x4 v) {
+        const float f = exp2_fast(r - base);
+        total += f * l;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             sum[e] += f * v[e];
+    };
+#pragma unroll
+    for (int u = 0; u < EARLY; ++u)
+        add(early_ref[u], early_total[u], early[u]);
+#pragma unroll 4
+    for (int p = first + EARLY * each; p < parts; p += each)
+        add(stat[2 * p], stat[2 * p + 1], *(const f32x4 *)(o + (long long)p * dim + c));
+    // over the lanes of one channel
+    for (int d = lanes; d < 64; d <<= 1) {
+        total += __shfl_xor(total, d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            sum[e] += __shfl_xor(sum[e], d);
     }
-    *(f32x4 *)lds.sum[threadIdx.x] = sum;
-    // every lane of a part has its total; those of the first channels are added
-    float mine = c == 0 ? total : 0.f;
-    for (int d = 32; d; d >>= 1)
-        mine += __shfl_xor(mine, d);
-    if ((threadIdx.x & 63) == 0)
-        lds.total[threadIdx.x >> 6] = mine;
-    __syncthreads();
-    if ((int)threadIdx.x >= lanes)
+    if constexpr (WAVES > 1) {
+        lds.sum[wave][thread & 63] = sum;
+        if ((thread & 63) == 0)
+            lds.total[wave] = total;
+        __syncthreads();
+        if (wave)
+            return;
+        total = lds.total[0];
+        for (int w = 1; w < WAVES; ++w) {
+            total += lds.total[w];
+            const f32x4 more = lds.sum[w][thread];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                sum[e] += more[e];
+        }
+    }
+    if (thread >= lanes || c >= dim)
         return;
-    for (int i = 1; i < each; ++i)
-        sum += *(const f32x4 *)lds.sum[threadIdx.x + i * lanes];
-    total = lds.total[0] + lds.total[1] + lds.total[2] + lds.total[3];
     const float inverse = total != 0.f ? 1.f / total : 0.f;
     typedef T V __attribute__((ext_vector_type(4), aligned(2)));
     V v;

@@ -413,11 +413,14 @@ __global__ void __launch_bounds__(256, DIM == 256 ? (R == 2 || GROUP == 32 ? 1 :
     }
 }
 
-template <typename T>
+template <typename T, int WAVES>
 __global__ void __launch_bounds__(256) qattn_join_kernel(QattnArgs A, int rows, int parts, int chunk)
 {
-    __shared__ JoinScratch lds;
-    const int at = blockIdx.x, head = at % A.q_heads, i = at / A.q_heads % A.max_queries, b = at / A.q_heads / A.max_queries;
+    __shared__ JoinScratch<WAVES> lds;
+    const int at = WAVES > 1 ? blockIdx.x : blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (at >= A.batch * A.max_queries * A.q_heads)
+        return;
+    const int head = at % A.q_heads, i = at / A.q_heads % A.max_queries, b = at / A.q_heads / A.max_queries;
     const Sequence seq = sequence(A, b);
     if (i >= seq.n)
         return;
@@ -425,7 +428,7 @@ __global__ void __launch_bounds__(256) qattn_join_kernel(QattnArgs A, int rows, 
     const int per = A.q_heads / A.c.heads, first_row = (i * per + head % per) / rows * rows;
     const int limit = seen_by(seq, rows, first_row, per), used = max((limit + chunk - 1) / chunk, 1);
     const long long query = seq.begin + i;
-    join_parts<T>(lds, A.part, (long long)A.queries * A.q_heads, query * A.q_heads + head, parts, used, A.c.dim,
+    join_parts<T, WAVES>(lds, A.part, (long long)A.queries * A.q_heads, query * A.q_heads + head, parts, used, A.c.dim,
                   (T *)A.y + query * A.y_token + head * A.y_head);
 }
 
@@ -464,8 +467,11 @@ hipError_t launch_type(const QattnArgs &a, const AttnPlan &p, hipStream_t stream
                                           : launch_dim<T, 256>(a, p, stream);
     if (e != hipSuccess || p.parts == 1)
         return e;
-    const long long all = (long long)a.batch * a.max_queries * a.q_heads;
-    hipLaunchKernelGGL(qattn_join_kernel<T>, dim3((unsigned)all), dim3(256), 0, stream, a, rows_of(a), p.parts, p.chunk);
+    const unsigned all = (unsigned)a.batch * a.max_queries * a.q_heads;
+    if (p.parts <= JOIN_FEW)
+        hipLaunchKernelGGL((qattn_join_kernel<T, 1>), dim3((all + 3) / 4), dim3(256), 0, stream, a, rows_of(a), p.parts, p.chunk);
+    else
+        hipLaunchKernelGGL((qattn_join_kernel<T, 4>), dim3(all), dim3(256), 0, stream, a, rows_of(a), p.parts, p.chunk);
     return hipGetLastError();
 }
 
