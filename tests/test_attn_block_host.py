@@ -1,0 +1,161 @@
+"""Host logic of the attention block (attn.CachedAttention, attn.PagedCache), without a GPU: the library's calls are recorded, not
+run, so what the kernels would be given is checked on CPU tensors."""
+import pytest
+import torch
+
+from paper_2007_06919_amd import aqd, attn, ffn
+
+HIDDEN, Q_HEADS, HEADS, DIM, PAGE = 96, 4, 2, 64, 16
+RUNS = ("qrows_run", "qnorm_run", "qlin_run", "heads_run", "qcache_write", "qcache_read", "qattn_run", "attn_run")
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The library's calls in order, as (name, arguments); tensors of the host pass for tensors of the GPU."""
+    for module in (ffn, attn):
+        monkeypatch.setattr(module, "DEVICE", "cpu")
+        monkeypatch.setattr(module, "_finish", lambda device, all=False: None)
+    monkeypatch.setattr(aqd, "_stream", lambda s: 0 if s is None else s if isinstance(s, int) else s.cuda_stream)
+    made = []
+    for name in RUNS:
+        monkeypatch.setattr(aqd, name, lambda *a, _name=name, **kw: made.append((_name, a)))
+    return made
+
+
+def weights(dtype=torch.bfloat16):
+    w = dict(norm_weight=(HIDDEN,), wq=(Q_HEADS * DIM, HIDDEN), wk=(HEADS * DIM, HIDDEN), wv=(HEADS * DIM, HIDDEN), wo=(HIDDEN, Q_HEADS * DIM),
+             q_norm=(DIM,), k_norm=(DIM,))
+    return dict({n: torch.ones(s, dtype=dtype) for n, s in w.items()}, table=torch.zeros(100, 32, dtype=torch.float32))
+
+
+def cache(pages=20):
+    return attn.PagedCache(HEADS, DIM, pages, group=32, page=PAGE)
+
+
+def rows_of(n):
+    return torch.zeros(n, HIDDEN, dtype=torch.bfloat16)
+
+
+def test_pages_are_taken_and_given_back(calls):
+    c = cache(5)
+    a, b = c.add(), c.add()
+    step = c.step([a, b], [17, 16])
+    assert [len(c.pages_of[i]) for i in (a, b)] == [2, 1] and len(set(c.pages_of[a] + c.pages_of[b])) == 3
+    assert step.prompts and step.rows == 33 and step.max_queries == step.max_keys == 17
+    pa, pb = c.pages_of[a], c.pages_of[b]
+    assert step.slots.tolist() == [pa[0] * PAGE + t for t in range(16)] + [pa[1] * PAGE] + [pb[0] * PAGE + t for t in range(16)]
+    assert step.position.tolist() == list(range(17)) + list(range(16)) and step.start.tolist() == [0, 17, 33] and step.lengths.tolist() == [17, 16]
+    step = c.step([b, a], [1, 2])
+    assert not step.prompts and step.max_queries == 2 and step.max_keys == 19 and step.lengths.tolist() == [17, 19]
+    assert step.position.tolist() == [16, 17, 18] and step.ld_table == 2 and step.tables.tolist() == c.pages_of[b] + c.pages_of[a]
+    for t in (step.position, step.slots, step.start, step.lengths, step.tables):
+        assert t.dtype == torch.int32
+    # one page is left
+    lengths, pages = dict(c.lengths), {i: list(p) for i, p in c.pages_of.items()}
+    with pytest.raises(MemoryError):
+        c.step([a, b], [16, 16])
+    assert c.lengths == lengths and c.pages_of == pages and len(c.free) == 1
+    c.remove(a)
+    assert len(c.free) == 3
+    c.step([b], [16])
+    with pytest.raises(KeyError):
+        c.remove(a)
+
+
+@pytest.mark.parametrize("ids, counts", [([0], [1, 2]), ([0, 0], [1, 1]), ([7], [1]), ([0], [-1])])
+def test_steps_that_name_no_sequences_are_refused(calls, ids, counts):
+    c = cache()
+    c.add()
+    with pytest.raises(ValueError):
+        c.step(ids, counts)
+
+
+def test_a_pass_is_these_calls(calls):
+    c = cache()
+    block = attn.CachedAttention(c, max_rows=40, **weights())
+    a, b = c.add(), c.add()
+    del calls[:]
+    x, residual, y, total = (torch.zeros(30, HIDDEN + 8 * i, dtype=torch.bfloat16)[:, :HIDDEN] for i in range(4))
+    block.forward(x, residual, y, total, c.step([a, b], [20, 10]))
+    assert [n for n, _ in calls] == ["qnorm_run", "qlin_run", "heads_run", "qcache_write", "attn_run", "qrows_run", "qlin_run"]
+    norm, _, heads, write, prompt, _, last = [args for _, args in calls]
+    assert (norm[5], norm[7], norm[10]) == (HIDDEN, HIDDEN + 8, HIDDEN + 24) and last[13] == HIDDEN + 16
+    wide, size = (Q_HEADS + 2 * HEADS) * DIM, 2
+    at = block.qkv.data_ptr()
+    assert heads[:8] == (30, Q_HEADS, HEADS, DIM, 32, aqd.PAIRS_HALVES, aqd.BF16, 100)
+    assert [t.data_ptr() for t in (heads[9], heads[12], heads[19], heads[22])] == [at, at + Q_HEADS * DIM * size] * 2
+    assert write[3].data_ptr() == at + Q_HEADS * DIM * size and write[6].data_ptr() == at + (Q_HEADS + HEADS) * DIM * size and write[4] == write[7] == wide
+    assert prompt[:10] == (2, Q_HEADS, HEADS, DIM, 30, 30, 20, 20, True, aqd.BF16)
+    # from then on from the cache, a new sequence among them too
+    del calls[:]
+    d = c.add()
+    block.forward(rows_of(7), None, rows_of(7), None, c.step([b, d], [2, 5]))
+    assert [n for n, _ in calls] == ["qnorm_run", "qlin_run", "heads_run", "qcache_write", "qattn_run", "qrows_run", "qlin_run"]
+    decode = calls[4][1]
+    assert decode[1:7] == (2, Q_HEADS, 7, 5, 12, aqd.BF16) and decode[0].pages == 20
+    assert calls[0][1][6] is None and calls[0][1][9] is None
+
+
+def test_what_does_not_fit_is_refused(calls):
+    c = cache()
+    block = attn.CachedAttention(c, max_rows=10, **weights())
+    a = c.add()
+    del calls[:]
+    step = c.step([a], [4])
+    good = [rows_of(4) for _ in range(4)]
+    row = torch.zeros(1, HIDDEN, dtype=torch.bfloat16).expand(4, HIDDEN)
+    for at in range(4):
+        for bad in (row, rows_of(5), rows_of(4).half(), torch.zeros(4, 2 * HIDDEN, dtype=torch.bfloat16)[:, ::2]):
+            tensors = list(good)
+            tensors[at] = bad
+            with pytest.raises(ValueError):
+                block.forward(*tensors, step)
+    with pytest.raises(ValueError):
+        block.forward(good[0], good[1], good[2], good[2], step)             # total over y
+    with pytest.raises(ValueError):
+        block.forward(*[rows_of(11)] * 2, rows_of(11), None, c.step([a], [11]))   # more rows than buffers
+    other = cache()
+    with pytest.raises(ValueError):
+        block.forward(*good, other.step([other.add()], [4]))
+    with pytest.raises(ValueError):
+        block.forward(rows_of(4), None, rows_of(4), None, c.step([a], [90]))     # past the table's 100 positions
+    assert not calls
+
+
+@pytest.mark.parametrize("name, value", [
+    ("wq", torch.ones(Q_HEADS * DIM - 8, HIDDEN, dtype=torch.bfloat16)), ("wk", torch.ones(DIM, HIDDEN, dtype=torch.bfloat16)),
+    ("wq", torch.ones(3 * DIM, HIDDEN, dtype=torch.bfloat16)), ("wo", torch.ones(HIDDEN, DIM, dtype=torch.bfloat16)), ("q_norm", torch.ones(DIM + 1, dtype=torch.bfloat16)),
+    ("norm_weight", torch.ones(HIDDEN)), ("k_norm", torch.ones(DIM)), ("table", torch.zeros(100, 32, dtype=torch.bfloat16)), ("table", torch.zeros(100, 66)),
+    ("table", torch.zeros(100)), ("max_rows", 0),
+])
+def test_weights_that_make_no_block_are_refused(calls, name, value):
+    with pytest.raises(ValueError):
+        attn.CachedAttention(cache(), **dict(weights(), **{name: value}))
+
+
+def test_fp32_blocks_are_refused(calls):
+    with pytest.raises(ValueError):
+        attn.CachedAttention(cache(), **weights(torch.float32))
+
+
+def test_tensors_of_the_host_are_refused():
+    """On the host, with the block's device a GPU: no address of the host may reach a kernel."""
+    with pytest.raises(ValueError):
+        attn.PagedCache(HEADS, DIM, 4, device="cpu")
+
+
+def test_cache_shapes_are_checked(calls):
+    with pytest.raises(aqd.AqdError):
+        attn.PagedCache(HEADS, 96, 4)
+    with pytest.raises(aqd.AqdError):
+        attn.PagedCache(HEADS, DIM, 4, page=24)
+
+
+def test_scales_have_32_bits_whatever_the_default_type(calls):
+    torch.set_default_dtype(torch.float64)
+    try:
+        block = attn.CachedAttention(cache(), max_rows=4, **weights())
+        table = attn.rotary_table(10, 8)
+    finally:
+        torch.set_default_dtype(torch.float32)
+    assert all(t.dtype == torch.float32 for t in (block.q1, block.q2, block.s1, block.s2, table))
