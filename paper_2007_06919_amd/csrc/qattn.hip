@@ -149,6 +149,13 @@ __global__ void __launch_bounds__(256, DIM == 256 ? (R == 2 || GROUP == 32 ? 1 :
         return bad;
     };
 
+    uint32_t bads = 0;   // two bits per step in flight, the next one lowest
+    const int t_first = start + 32 * wave;
+#pragma unroll
+    for (int i = 0; i < S::RING; ++i)
+        if (t_first + 128 * i < end)
+            bads |= copy(t_first + 128 * i, i) << (2 * i);
+
     // queries as operands, the sign of the scale with them; rows past the last are zeros
     u32x4 q[R][U];
     int seen[R];
@@ -169,13 +176,6 @@ __global__ void __launch_bounds__(256, DIM == 256 ? (R == 2 || GROUP == 32 ? 1 :
                 q[k][u][e] = w[e] ^ flip;
         }
     }
-    uint32_t bads = 0;   // two bits per step in flight, the next one lowest
-    const int t_first = start + 32 * wave;
-#pragma unroll
-    for (int i = 0; i < S::RING; ++i)
-        if (t_first + 128 * i < end)
-            bads |= copy(t_first + 128 * i, i) << (2 * i);
-
     const int seen_least = seq.length - seq.n + 1 + first_row / per;
     // (a scale of 0 would make -infinity * 0 of hidden scores)
     const float scale = fmaxf(fabsf(A.scale) * LOG2E, 0x1p-100f);
