@@ -472,7 +472,8 @@ aqd_status_t qcache_read(const qcache_rows_desc_t *desc, const void *cache, cons
  * `type` for the matrix product: each term within half a unit of its last place.
  * max_queries and max_keys bound the sequences' queries and lengths, which sizes the launch; of a longer sequence
  * the first max_queries queries and max_keys tokens count (and no more than ld_table pages). Queries that see a token whose page
- * number is outside of 0 .. pages - 1 are NaN. What lies in a page past a sequence's end does not matter.
+ * number is outside of 0 .. pages - 1 are NaN. What lies in a page past a sequence's end does not matter. No row of q may be
+ * two sequences'.
  * q, y: AQD_F16 or AQD_BF16 (UNSUPPORTED: AQD_F32), [queries][q_heads][dim].
  *
  * workspace (device, 16-byte aligned, ws_bytes): with it, the tokens of long sequences are split between workgroups, which
@@ -500,7 +501,8 @@ aqd_status_t qattn_run(const qattn_desc_t *desc, const void *q, const int32_t *q
  * infinities and NaN included. max_queries and max_keys bound the sequences' rows, which sizes the launch; of a longer
  * sequence the first max_queries queries and all keys count. Starts are taken as if within 0 .. queries and 0 .. keys,
  * and a sequence whose start lies behind its end as empty; no row of q may be two sequences'.
- * dim: a multiple of 8 up to 256 (UNSUPPORTED above); AQD_F16 or AQD_BF16 (UNSUPPORTED: AQD_F32).
+ * dim: a multiple of 8 up to 256 (UNSUPPORTED above); AQD_F16 or AQD_BF16 (UNSUPPORTED: AQD_F32); k_token and v_token
+ * at most 2^26 elements (UNSUPPORTED above).
  * workspace as qattn_run's (aqd_attn_workspace): few queries over many keys are split. */
 typedef struct {
     int batch, q_heads, heads, dim;   /* q_heads a multiple of heads */

@@ -404,8 +404,8 @@ def qcache_read(cache, tokens, type, data, slots, k, k_token, k_head, v, v_token
 
 def qattn_workspace(cache, batch, q_heads, queries, max_queries, max_keys, type) -> int:
     """Workspace bytes with which qattn_run splits long sequences (0: it does not; at most ATTN_WORKSPACE_BYTES)."""
-    row = q_heads * cache.dim
-    d = QattnDesc(cache, batch, q_heads, queries, max_queries, max_keys, type, 1.0, 1, row, cache.dim, row, cache.dim)
+    row, ld_table = q_heads * cache.dim, max(1, -(-max_keys // max(cache.page, 1)))
+    d = QattnDesc(cache, batch, q_heads, queries, max_queries, max_keys, type, 1.0, ld_table, row, cache.dim, row, cache.dim)
     b = ctypes.c_size_t(0)
     _check(lib().qattn_workspace(ctypes.byref(d), ctypes.byref(b)))
     return b.value

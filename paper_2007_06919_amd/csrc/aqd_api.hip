@@ -2102,13 +2102,17 @@ aqd_status_t attn_args(const aqd_attn_desc_t *d, AttnArgs &a)
     a.max_queries = std::min(d->max_queries, d->queries);
     a.max_keys = std::min(d->max_keys, d->keys);
     a.causal = d->causal, a.type = d->type, a.scale = d->scale;
+    // a workgroup has 128 rows, and a launch less than 2^32 threads (keys are split where the rows make less than 512 workgroups)
     REQUIRE(a.keys <= INT32_MAX - 65536 && (long long)a.queries * a.q_heads <= INT32_MAX - 65536 &&
-                (double)a.batch * a.q_heads * (a.max_queries + 16.0) <= INT32_MAX - 65536, "too many queries or keys");
+                (double)a.batch * a.heads * ((double)a.max_queries * (a.q_heads / a.heads) / 128 + 1) <= 1 << 23, "too many queries or keys");
     a.q_token = d->q_token, a.q_head = d->q_head, a.k_token = d->k_token, a.k_head = d->k_head;
     a.v_token = d->v_token, a.v_head = d->v_head, a.y_token = d->y_token, a.y_head = d->y_head;
     REQUIRE(strides_ok(a.q_token, a.q_head, a.queries, a.q_heads, a.dim) && strides_ok(a.k_token, a.k_head, a.keys, a.heads, a.dim) &&
                 strides_ok(a.v_token, a.v_head, a.keys, a.heads, a.dim) && strides_ok(a.y_token, a.y_head, a.queries, a.q_heads, a.dim),
             "strides by which elements could share memory, or too large");
+    // offsets of the 32 rows of a tile are 32-bit numbers
+    if (a.k_token > 1 << 26 || a.v_token > 1 << 26)
+        return fail(AQD_ERR_UNSUPPORTED, "token strides of k and v must be at most 2^26");
     return AQD_OK;
 }
 

@@ -186,3 +186,34 @@ def test_the_workspaces_have_a_bound(batch, dim):
                 assert 0 <= b <= aqd.ATTN_WORKSPACE_BYTES
                 b = aqd.attn_workspace(batch, q_heads, 8, dim, batch * each, min(batch * keys, 1 << 30), each, keys, True, aqd.F16)
                 assert 0 <= b <= aqd.ATTN_WORKSPACE_BYTES
+
+
+def test_keys_far_from_one_another_are_not_there():
+    """Offsets within a tile of 32 keys are 32-bit numbers."""
+    far = (1 << 26) + 2
+    refused(attn_call, aqd.AQD_ERR_UNSUPPORTED, k_token=far, k=1 << 40)
+    refused(attn_call, aqd.AQD_ERR_UNSUPPORTED, v_token=far, v=1 << 40)
+    # one key has no stride
+    attn_call(keys=1, k_token=far, v_token=far, max_queries=0)
+
+
+@pytest.mark.parametrize("sizes", [
+    dict(batch=1 << 20, max_queries=65, heads=4), dict(batch=1 << 23, max_queries=1, heads=1), dict(queries=1 << 28, max_queries=1 << 28, batch=2, heads=4),
+    dict(batch=1, queries=1 << 29, max_queries=1 << 29),
+])
+def test_launches_have_a_bound(sizes):
+    """A workgroup has 128 rows (16 of single tokens), and a launch less than 2^32 threads of 256 a workgroup."""
+    few = dict(queries=sizes.get("queries", 70))
+    refused(attn_call, y_token=256, y=1 << 44, **{**few, **sizes})
+    refused(qattn_call, y=1 << 44, q_start=ADDR["q_start"], **{**few, **sizes})
+
+
+def test_long_sequences_have_a_workspace():
+    """The sizes that qattn_run splits by: a row's dim sums and two more numbers for each part."""
+    cache = aqd.QcacheDesc(2, 128, 64, 64, 200)
+    row = 6 * (128 + 2) * 4
+    for queries, keys in ((1, 9000), (4, 9000), (1, 600)):
+        b = aqd.qattn_workspace(cache, 1, 6, queries, queries, keys, aqd.BF16)
+        assert b and b % (row * queries) == 0 and b <= -(-keys // 128) * row * queries
+    assert aqd.qattn_workspace(cache, 1, 6, 1, 1, 100, aqd.BF16) == 0
+    assert aqd.attn_workspace(1, 6, 2, 128, 4, 9000, 4, 9000, True, aqd.BF16) % (row * 4) == 0
