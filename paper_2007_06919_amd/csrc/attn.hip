@@ -99,7 +99,9 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
     if (first_row >= rows)
         return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
-    const int limit = seen_by(A, seq, min((first_row + ROWS - 1) / per, seq.n - 1)), start = part * chunk, end = min(start + chunk, limit);
+    const int limit = seen_by(A, seq, min((first_row + ROWS - 1) / per, seq.n - 1)), start = part * chunk;
+    // (a sequence may have more keys than max_keys: the last part takes them all)
+    const int end = part + 1 < parts ? min(start + chunk, limit) : limit;
     if (part && start >= limit)
         return;
     const int wave_row = first_row + 32 * wave;
@@ -425,7 +427,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs A, int parts, i
         return;
     // the parts that its workgroup's rows have
     const int per = A.q_heads / A.heads, last_row = (i * per + head % per) / ROWS * ROWS + ROWS - 1;
-    const int limit = seen_by(A, seq, min(last_row / per, seq.n - 1)), used = max((limit + chunk - 1) / chunk, 1);
+    const int limit = seen_by(A, seq, min(last_row / per, seq.n - 1)), used = min(max((limit + chunk - 1) / chunk, 1), parts);
     const long long query = seq.begin + i;
     join_parts<T, WAVES>(lds, A.part, (long long)A.queries * A.q_heads, query * A.q_heads + head, parts, used, A.dim,
                   (T *)A.y + query * A.y_token + head * A.y_head);
@@ -433,7 +435,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs A, int parts, i
 
 int row_tiles(const AttnArgs &a) { return (int)(((long long)a.max_queries * (a.q_heads / a.heads) + ROWS - 1) / ROWS); }
 
-// whether the copies can take rows as they lie: at multiples of 4 bytes, a tile's within 32 bits
+// whether the copies can take rows as they lie: at multiples of 4 bytes
 bool direct(const AttnArgs &a)
 {
     return (((uintptr_t)a.k | (uintptr_t)a.v) & 3) == 0 && ((a.k_token | a.k_head | a.v_token | a.v_head) & 1) == 0;
