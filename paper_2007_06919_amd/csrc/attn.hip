@@ -79,9 +79,95 @@ __device__ __forceinline__ int seen_by(const AttnArgs &A, const Span2 &s, int qu
     return A.causal ? max(s.m - s.n + 1 + query, 0) : s.m;
 }
 
-// DIRECT: rows of keys and values start at multiples of 4 bytes
+// sum over a wave's lanes
+__device__ __forceinline__ int wave_sum(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);   // the lanes 1, 2, 4 and 8 below, in 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // lane 15 of the 16 below
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // lane 31
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
+// Where sequences differ in length, most of a grid of the longest one's row tiles for each would have no rows. Row tile `item` of all
+// sequences' instead: those of up to 256 sequences by their number in the sequence, the highest first (they see most keys);
+// those of more one sequence after the other. False past the last one.
+__device__ __forceinline__ bool find_tile(const AttnArgs &A, int per, int tiles, int item, int &sequence_at, int &tile)
+{
+    const int lane = threadIdx.x & 63;
+    auto tiles_of = [&](int b) { return b < A.batch ? (max(sequence(A, b).n, 0) * per + ROWS - 1) / ROWS : 0; };
+    if (A.batch <= 256) {
+        int count[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            count[k] = 64 * k < A.batch ? tiles_of(64 * k + lane) : 0;
+        // how many have the number `least` or a higher one
+        auto from = [&](int least) {
+            int n = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                n += max(count[k] - least, 0);
+            return wave_sum(n);
+        };
+        if (item >= from(0))
+            return false;
+        int low = 0, high = tiles, above = 0;   // from(low) > item >= from(high) == above
+        while (high - low > 1) {
+            const int middle = (low + high) / 2, n = from(middle);
+            if (n > item) {
+                low = middle;
+            } else {
+                high = middle;
+                above = n;
+            }
+        }
+        int rest = item - above;
+        tile = low;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint64_t has = __builtin_amdgcn_ballot_w64(count[k] > low);
+            const int n = __builtin_popcountll(has);
+            if (rest >= 0 && rest < n) {
+                const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0));
+                sequence_at = 64 * k + __builtin_ctzll(__builtin_amdgcn_ballot_w64(count[k] > low && before == rest));
+                return true;
+            }
+            rest -= n;
+        }
+        return false;
+    }
+    // a lane has `each` sequences, then those of the lane that has the item are the lanes'
+    int first = 0, last = A.batch, rest = item;
+    for (;;) {
+        const int each = (last - first + 63) / 64, begin = min(first + lane * each, last), end = min(begin + each, last);
+        int n = 0;
+        for (int b = begin; b < end; ++b)
+            n += tiles_of(b);
+        int upto = n;   // with the lanes below
+        for (int d = 1; d < 64; d <<= 1) {
+            const int x = __shfl_up(upto, d);
+            upto += lane >= d ? x : 0;
+        }
+        const uint64_t past = __builtin_amdgcn_ballot_w64(upto > rest);
+        if (!past)
+            return false;
+        const int at = __builtin_ctzll(past);
+        rest -= __builtin_amdgcn_readlane(upto - n, at);
+        first = __builtin_amdgcn_readlane(begin, at);
+        last = __builtin_amdgcn_readlane(end, at);
+        if (each == 1) {
+            sequence_at = first;
+            tile = __builtin_amdgcn_readlane(n, at) - 1 - rest;
+            return true;
+        }
+    }
+}
+
+// DIRECT: rows of keys and values start at multiples of 4 bytes. tiles: of the longest sequence
 template <typename T, int DIM, bool DIRECT>
-__global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_kernel(AttnArgs A, int tiles, int parts, int chunk)
+__global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_kernel(AttnArgs A, int tiles, int parts, int chunk, bool packed)
 {
     typedef Tile<DIM> S;
     constexpr int U = DIM / 16, C = DIM / 32;
@@ -90,10 +176,17 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
     int rest = blockIdx.x;
     const int kv = rest % A.heads;
     rest /= A.heads;
-    const int b = rest % A.batch;
-    rest /= A.batch;
-    // the longest rows first
-    const int part = rest % parts, row_tile = tiles - 1 - rest / parts;
+    // the rows with most keys first
+    int part = 0, row_tile, b;
+    if (packed) {
+        if (!find_tile(A, per, tiles, rest, b, row_tile))
+            return;
+    } else {
+        b = rest % A.batch;
+        rest /= A.batch;
+        part = rest % parts;
+        row_tile = tiles - 1 - rest / parts;
+    }
     const Span2 seq = sequence(A, b);
     const int rows = seq.n * per, first_row = row_tile * ROWS;
     if (first_row >= rows)
@@ -445,11 +538,14 @@ template <typename T, int DIM>
 hipError_t launch_rows(const AttnArgs &a, const AttnPlan &p, hipStream_t stream)
 {
     const int tiles = row_tiles(a);
-    const dim3 grid((unsigned)(a.heads * tiles * p.parts * a.batch));
+    // row tiles that sequences of `queries` rows together can have, each but one of a sequence full
+    const long long all = (long long)a.batch * tiles, most = (long long)a.queries * (a.q_heads / a.heads) / ROWS + a.batch;
+    const bool packed = p.parts == 1 && 4 * all > 5 * most;
+    const dim3 grid((unsigned)(a.heads * (packed ? most : all * p.parts)));
     if (direct(a))
-        hipLaunchKernelGGL((attn_kernel<T, DIM, true>), grid, dim3(256), 0, stream, a, tiles, p.parts, p.chunk);
+        hipLaunchKernelGGL((attn_kernel<T, DIM, true>), grid, dim3(256), 0, stream, a, tiles, p.parts, p.chunk, packed);
     else
-        hipLaunchKernelGGL((attn_kernel<T, DIM, false>), grid, dim3(256), 0, stream, a, tiles, p.parts, p.chunk);
+        hipLaunchKernelGGL((attn_kernel<T, DIM, false>), grid, dim3(256), 0, stream, a, tiles, p.parts, p.chunk, packed);
     return hipGetLastError();
 }
 

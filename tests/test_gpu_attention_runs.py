@@ -293,3 +293,36 @@ def test_recorded_calls():
         torch.cuda.synchronize()
         for g in graphs:
             aqd.graph_destroy(g)
+
+
+@pytest.mark.parametrize("dim, heads, per, causal, few, batch", [(64, 2, 3, True, 700, 7), (128, 1, 8, True, 333, 70), (64, 1, 1, False, 1500, 256),
+                                                                (128, 2, 2, True, 900, 257), (256, 1, 4, True, 200, 3000)])
+def test_attn_of_sequences_of_unlike_lengths(dim, heads, per, causal, few, batch):
+    """Some long sequences among many short ones and empty ones: the bits of the sequences by themselves, and rows of none left alone."""
+    import torch
+    t = "bf16"
+    rng = np.random.Generator(np.random.PCG64(batch))
+    n = rng.integers(0, 6, batch)
+    n[rng.integers(0, batch, 3)] = few
+    n[batch // 2], n[-1], n[0] = 129, 0, few // 2
+    m = n + rng.integers(0, 50, batch)
+    m[1] = 0
+    qs, ks = [np.concatenate([[0], np.cumsum(x)]).tolist() for x in (n, m)]
+    q, (k, v) = reals(torch, rng, qs[-1] + 5, heads * per, dim, t=t), [reals(torch, rng, ks[-1], heads, dim, t=t) for _ in range(2)]
+    qd, kd, vd = q.cuda(), k.cuda(), v.cuda()
+    y = torch.full_like(qd, 77)
+    run_attn(torch, qd, kd, vd, qs, ks, causal, t, y)
+    assert bool((y[qs[-1]:] == 77).all())
+    alone = torch.full_like(qd, 77)
+    some = np.flatnonzero(n > 5).tolist() + spread(rng, batch, 20)
+    for b in some:
+        run_attn(torch, qd, kd, vd, qs[b:b + 2], ks[b:b + 2], causal, t, alone, 0)
+        a, z = slice(qs[b], qs[b + 1]), slice(ks[b], ks[b + 1])
+        assert torch.equal(y[a], alone[a]), b
+        if n[b]:
+            check_rows(y[a].double().cpu().numpy(), q[a].double().numpy(), k[z].double().numpy(), v[z].double().numpy(), spread(rng, int(n[b]), 3), causal, t)
+    if batch > 256:
+        run_attn(torch, qd, kd, vd, qs, ks, causal, t, alone, max_queries=130)      # of longer ones the first 130
+        for b in some:
+            a = slice(qs[b], min(qs[b] + 130, qs[b + 1]))
+            assert bool((alone[a] == alone[a]).all())
