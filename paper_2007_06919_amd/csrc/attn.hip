@@ -79,18 +79,6 @@ __device__ __forceinline__ int seen_by(const AttnArgs &A, const Span2 &s, int qu
     return A.causal ? max(s.m - s.n + 1 + query, 0) : s.m;
 }
 
-// sum over a wave's lanes
-__device__ __forceinline__ int wave_sum(int x)
-{
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);   // the lanes 1, 2, 4 and 8 below, in 16
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // lane 15 of the 16 below
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // lane 31
-    return __builtin_amdgcn_readlane(x, 63);
-}
-
 // Where sequences differ in length, most of a grid of the longest one's row tiles for each would have no rows. Row tile `item` of all
 // sequences' instead: those of up to 256 sequences by their number in the sequence, the highest first (they see most keys);
 // those of more one sequence after the other. False past the last one.
@@ -522,8 +510,8 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs A, int parts, i
     const int per = A.q_heads / A.heads, last_row = (i * per + head % per) / ROWS * ROWS + ROWS - 1;
     const int limit = seen_by(A, seq, min(last_row / per, seq.n - 1)), used = min(max((limit + chunk - 1) / chunk, 1), parts);
     const long long query = seq.begin + i;
-    join_parts<T, WAVES>(lds, A.part, (long long)A.queries * A.q_heads, query * A.q_heads + head, parts, used, A.dim,
-                  (T *)A.y + query * A.y_token + head * A.y_head);
+    const long long row = (query * A.q_heads + head) * parts, all = (long long)A.queries * A.q_heads * parts;
+    join_parts<T, WAVES>(lds, A.part + row * A.dim, A.part + all * A.dim + 2 * row, 1, used, A.dim, (T *)A.y + query * A.y_token + head * A.y_head);
 }
 
 int row_tiles(const AttnArgs &a) { return (int)(((long long)a.max_queries * (a.q_heads / a.heads) + ROWS - 1) / ROWS); }
@@ -576,7 +564,7 @@ AttnPlan attn_plan(const AttnArgs &a, size_t room)
     const int keys = a.max_keys, steps = (keys + 31) / 32;
     const double groups = (double)a.batch * a.heads * row_tiles(a), rows = (double)a.queries * a.q_heads;
     const double one = rows * (a.dim + 2) * 4;
-    AttnPlan best = {1, INT32_MAX - 65536, 0};
+    AttnPlan best = {1, INT32_MAX - 65536, 0, 0};
     double least = 1e30;
     for (int parts : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128}) {
         if (parts > 1 && (one * parts > (double)room || steps < 2 * parts))
@@ -589,7 +577,7 @@ AttnPlan attn_plan(const AttnArgs &a, size_t room)
             least = t;
             if (parts > 1) {
                 const int used = (steps + each - 1) / each;
-                best = {used, 32 * each, (size_t)(one * used)};
+                best = {used, 32 * each, (size_t)(one * used), 0};
             }
         }
     }

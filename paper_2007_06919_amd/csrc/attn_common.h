@@ -52,7 +52,20 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 
 constexpr float LOG2E = 1.44269504088896340736f;
 
-// The parts of one row, sums [parts][dim] and, behind all rows' sums, [parts][2] references and totals: the row is
+// sums over the lanes up to one's own
+__device__ __forceinline__ int wave_scan(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);   // the lanes 1, 2, 4 and 8 below, in 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // lane 15 of the 16 below
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // lane 31
+    return x;
+}
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
+
+// The parts of one row, sums o [dim] and references and totals stat [2], `step` rows from part to part: the row is
 // sum_p o_p 2^(ref_p - ref) / sum_p l_p 2^(ref_p - ref), zeros where there is no weight at all. WAVES waves (1 for few parts: rows
 // are many then, and a wave needs no barrier), of which 16, 32 or 64 lanes have four channels of a part each.
 template <int WAVES>
@@ -63,10 +76,9 @@ struct JoinScratch {
 constexpr int JOIN_FEW = 16;   // parts that one wave joins
 
 template <typename T, int WAVES>
-__device__ __forceinline__ void join_parts(JoinScratch<WAVES> &lds, const float *part, long long rows, long long row, int all, int parts,
-                                           int dim, T *y)
+__device__ __forceinline__ void join_parts(JoinScratch<WAVES> &lds, const float *o, const float *stat, long long step, int parts, int dim, T *y)
 {
-    const float *o = part + row * all * dim, *stat = part + rows * all * dim + row * all * 2;
+    const long long o_step = step * dim, stat_step = step * 2;
     const int lanes = dim <= 64 ? 16 : dim <= 128 ? 32 : 64, each = 64 * WAVES / lanes;
     const int thread = WAVES > 1 ? threadIdx.x : threadIdx.x & 63, wave = thread >> 6;
     const int c = thread % lanes * 4, first = c < dim ? thread / lanes : parts;
@@ -81,14 +93,14 @@ __device__ __forceinline__ void join_parts(JoinScratch<WAVES> &lds, const float 
         early_ref[u] = -INFINITY;
         early_total[u] = 0.f;
         if (p < parts) {
-            early[u] = *(const f32x4 *)(o + (long long)p * dim + c);
-            early_ref[u] = stat[2 * p];
-            early_total[u] = stat[2 * p + 1];
+            early[u] = *(const f32x4 *)(o + p * o_step + c);
+            early_ref[u] = stat[p * stat_step];
+            early_total[u] = stat[p * stat_step + 1];
         }
     }
     float ref = -INFINITY;
     for (int p = thread; p < parts; p += 64 * WAVES)
-        ref = fmaxf(ref, stat[2 * p]);
+        ref = fmaxf(ref, stat[p * stat_step]);
     for (int d = 32; d; d >>= 1)
         ref = fmaxf(ref, __shfl_xor(ref, d));
     if constexpr (WAVES > 1) {
@@ -113,7 +125,7 @@ __device__ __forceinline__ void join_parts(JoinScratch<WAVES> &lds, const float 
         add(early_ref[u], early_total[u], early[u]);
 #pragma unroll 4
     for (int p = first + EARLY * each; p < parts; p += each)
-        add(stat[2 * p], stat[2 * p + 1], *(const f32x4 *)(o + (long long)p * dim + c));
+        add(stat[p * stat_step], stat[p * stat_step + 1], *(const f32x4 *)(o + p * o_step + c));
     // over the lanes of one channel
     for (int d = lanes; d < 64; d <<= 1) {
         total += __shfl_xor(total, d);

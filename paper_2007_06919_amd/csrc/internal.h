@@ -277,6 +277,7 @@ struct AttnPlan {
     int parts;      // workgroups that share a sequence's keys
     int chunk;      // keys of each
     size_t bytes;   // their results in the workspace
+    int slots;      // attention over the cache: workgroups (of a key head and row tile) that all sequences share by their lengths, or 0
 };
 struct QattnArgs {
     QcacheShape c;

@@ -59,20 +59,86 @@ __device__ __forceinline__ void scalar_loads(const int32_t *p, int a, int b, int
 struct Sequence {
     int begin, n, length;
 };
+__device__ __forceinline__ int length_of(const QattnArgs &A, int b)
+{
+    return (int)max(min((long long)min(A.lengths[b], A.max_keys), A.ld_table * A.c.page), 0LL);
+}
 __device__ __forceinline__ Sequence sequence(const QattnArgs &A, int b)
 {
     Sequence s;
     s.begin = A.q_start ? min(max(A.q_start[b], 0), A.queries) : b;
     const int end = A.q_start ? min(max(A.q_start[b + 1], 0), A.queries) : b + 1;
     s.n = min(end - s.begin, A.max_queries);
-    s.length = (int)max(min((long long)min(A.lengths[b], A.max_keys), A.ld_table * A.c.page), 0LL);
+    s.length = length_of(A, b);
     return s;
 }
+// Sequences of unlike lengths share `slots` workgroups (of a key head and row tile) by their tokens: a workgroup has
+// `chunk` of them at most, such that sum(floor(length / chunk) + 1) <= slots. Their results are numbered by sequence.
+struct Share {
+    int b, chunk, first, parts, full;   // a sequence; its slots, and how many of them are whole chunks
+};
+constexpr int SHARED = 1024, LEAST = 256;   // most sequences; least tokens of a chunk
+struct Shared {
+    const QattnArgs &A;
+    int lane, near, units;   // near: tokens of the first 64 sequences, in units of 128; units: a chunk
+
+    __device__ __forceinline__ Shared(const QattnArgs &args, int slots) : A(args), lane(threadIdx.x & 63)
+    {
+        near = lane < A.batch ? (length_of(A, lane) + 127) / 128 : 0;
+        int total = near;
+#pragma unroll 4
+        for (int k = 64; k < A.batch; k += 64)
+            total += tokens(k);
+        units = max((wave_sum(total) + slots - A.batch - 1) / (slots - A.batch), LEAST / 128);
+    }
+    __device__ __forceinline__ int tokens(int k) const { return k ? (k + lane < A.batch ? (length_of(A, k + lane) + 127) / 128 : 0) : near; }
+    __device__ __forceinline__ Share of(int b) const
+    {
+        int before = 0, k = 0;
+        for (; k + 64 <= b; k += 64)
+            before += wave_sum(max((int)((unsigned)(tokens(k) + units - 1) / units), 1));
+        const int n = tokens(k), parts = max((int)((unsigned)(n + units - 1) / units), 1), upto = wave_scan(parts);
+        const int at = __builtin_amdgcn_readfirstlane(b - k), own = __builtin_amdgcn_readlane(parts, at);
+        return {b, 128 * units, before + __builtin_amdgcn_readlane(upto, at) - own, own, (int)((unsigned)__builtin_amdgcn_readlane(n, at) / units)};
+    }
+    // of workgroup `at`: all full chunks come first, then what is left of each sequence
+    __device__ __forceinline__ bool find(int at, Share &s, int &part) const
+    {
+        int before = 0, b = -1;
+        part = -1;
+        for (int k = 0; k < A.batch; k += 64) {
+            const int full = (unsigned)tokens(k) / units, upto = wave_scan(full) + before;
+            const uint64_t has = __builtin_amdgcn_ballot_w64(upto > at);
+            if (has) {
+                const int from = __builtin_ctzll(has);
+                b = k + from;
+                part = at - __builtin_amdgcn_readlane(upto - full, from);
+                break;
+            }
+            before = __builtin_amdgcn_readlane(upto, 63);
+        }
+        if (b < 0)
+            b = at - before;
+        if (b >= A.batch)
+            return false;
+        s = of(b);
+        if (part >= 0)
+            return true;
+        part = s.parts - 1;
+        return s.parts > s.full;
+    }
+};
 // how many tokens a workgroup's rows see at most
 __device__ __forceinline__ int seen_by(const Sequence &s, int rows, int first_row, int per)
 {
     const int last = min((first_row + rows - 1) / per, s.n - 1);
     return max(s.length - s.n + 1 + last, 0);
+}
+
+// Rows of the workspace: [queries][q_heads][parts], or [slots][max_queries][q_heads] of shared slots.
+__device__ __forceinline__ long long part_rows(const QattnArgs &A, int slots, int parts)
+{
+    return slots ? (long long)slots * A.max_queries * A.q_heads : (long long)A.queries * A.q_heads * parts;
 }
 
 template <int DIM, int GROUP, int R>
@@ -88,7 +154,7 @@ struct Shape {
 };
 
 template <typename T, int DIM, int GROUP, int R>
-__global__ void __launch_bounds__(256, DIM == 256 ? (R == 2 || GROUP == 32 ? 1 : 2) : DIM == 128 && R == 2 ? 2 : 3) qattn_kernel(QattnArgs A, int tiles, int parts, int chunk)
+__global__ void __launch_bounds__(256, DIM == 256 ? (R == 2 || GROUP == 32 ? 1 : 2) : DIM == 128 && R == 2 ? 2 : 3) qattn_kernel(QattnArgs A, int tiles, int parts, int chunk, int slots)
 {
     typedef Shape<DIM, GROUP, R> S;
     constexpr int G = S::GROUPS, U = DIM / 32, TILES = DIM / 16;
@@ -99,7 +165,17 @@ __global__ void __launch_bounds__(256, DIM == 256 ? (R == 2 || GROUP == 32 ? 1 :
     int rest = blockIdx.x / A.c.heads;
     const int row_tile = rest % tiles;
     rest /= tiles;
-    const int part = rest % parts, b = rest / parts;
+    int part, b;
+    int slot = 0;
+    if (slots) {
+        Share s;
+        if (!Shared(A, slots).find(rest, s, part))
+            return;
+        b = s.b, slot = s.first + part, parts = s.parts, chunk = s.chunk;
+    } else {
+        part = rest % parts;
+        b = rest / parts;
+    }
     const Sequence seq = sequence(A, b);
     const int first_row = row_tile * 16 * R, rows = seq.n * per;
     if (first_row >= rows)
@@ -401,10 +477,10 @@ __global__ void __launch_bounds__(256, DIM == 256 ? (R == 2 || GROUP == 32 ? 1 :
                     v[e] = (T)(sum[e] * inverse);
                 *(V *)((T *)A.y + query * A.y_token + head * A.y_head + c) = v;
             } else {
-                const long long all = (long long)A.queries * A.q_heads, id = ((long long)query * A.q_heads + head) * parts + part;
+                const long long id = slots ? ((long long)slot * A.max_queries + row / per) * A.q_heads + head : ((long long)query * A.q_heads + head) * parts + part;
                 *(f32x4 *)(A.part + id * DIM + c) = sum;
                 if (c == 0) {
-                    float *stat = A.part + all * parts * DIM + 2 * id;
+                    float *stat = A.part + part_rows(A, slots, parts) * DIM + 2 * id;
                     stat[0] = most;
                     stat[1] = l;
                 }
@@ -414,22 +490,31 @@ __global__ void __launch_bounds__(256, DIM == 256 ? (R == 2 || GROUP == 32 ? 1 :
 }
 
 template <typename T, int WAVES>
-__global__ void __launch_bounds__(256) qattn_join_kernel(QattnArgs A, int rows, int parts, int chunk)
+__global__ void __launch_bounds__(256) qattn_join_kernel(QattnArgs A, int rows, int parts, int chunk, int slots)
 {
     __shared__ JoinScratch<WAVES> lds;
     const int at = WAVES > 1 ? blockIdx.x : blockIdx.x * 4 + (threadIdx.x >> 6);
     if (at >= A.batch * A.max_queries * A.q_heads)
         return;
     const int head = at % A.q_heads, i = at / A.q_heads % A.max_queries, b = at / A.q_heads / A.max_queries;
+    Share s = {b, chunk, 0, parts, 0};
+    if (slots) {
+        if (length_of(A, b) <= LEAST)
+            return;   // one part, in y
+        s = Shared(A, slots).of(b);
+        if (s.parts == 1)
+            return;
+    }
     const Sequence seq = sequence(A, b);
     if (i >= seq.n)
         return;
     // the parts that its workgroups' rows have
     const int per = A.q_heads / A.c.heads, first_row = (i * per + head % per) / rows * rows;
-    const int limit = seen_by(seq, rows, first_row, per), used = max((limit + chunk - 1) / chunk, 1);
-    const long long query = seq.begin + i;
-    join_parts<T, WAVES>(lds, A.part, (long long)A.queries * A.q_heads, query * A.q_heads + head, parts, used, A.c.dim,
-                  (T *)A.y + query * A.y_token + head * A.y_head);
+    const int limit = seen_by(seq, rows, first_row, per), used = max((limit + s.chunk - 1) / s.chunk, 1);
+    const long long query = seq.begin + i, step = slots ? (long long)A.max_queries * A.q_heads : 1;
+    const long long row = slots ? ((long long)s.first * A.max_queries + i) * A.q_heads + head : (query * A.q_heads + head) * parts;
+    join_parts<T, WAVES>(lds, A.part + row * A.c.dim, A.part + part_rows(A, slots, parts) * A.c.dim + 2 * row, step, used, A.c.dim,
+                         (T *)A.y + query * A.y_token + head * A.y_head);
 }
 
 int row_tiles(const QattnArgs &a, int rows) { return (a.max_queries * (a.q_heads / a.c.heads) + rows - 1) / rows; }
@@ -439,8 +524,8 @@ template <typename T, int DIM, int GROUP, int R>
 hipError_t launch_rows(const QattnArgs &a, const AttnPlan &p, hipStream_t stream)
 {
     const int tiles = row_tiles(a, 16 * R);
-    const dim3 grid((unsigned)(a.c.heads * tiles * p.parts * a.batch));
-    hipLaunchKernelGGL((qattn_kernel<T, DIM, GROUP, R>), grid, dim3(256), 0, stream, a, tiles, p.parts, p.chunk);
+    const dim3 grid((unsigned)(a.c.heads * tiles * (p.slots ? p.slots : p.parts * a.batch)));
+    hipLaunchKernelGGL((qattn_kernel<T, DIM, GROUP, R>), grid, dim3(256), 0, stream, a, tiles, p.parts, p.chunk, p.slots);
     return hipGetLastError();
 }
 
@@ -465,13 +550,13 @@ hipError_t launch_type(const QattnArgs &a, const AttnPlan &p, hipStream_t stream
     const hipError_t e = a.c.dim == 64    ? launch_dim<T, 64>(a, p, stream)
                          : a.c.dim == 128 ? launch_dim<T, 128>(a, p, stream)
                                           : launch_dim<T, 256>(a, p, stream);
-    if (e != hipSuccess || p.parts == 1)
+    if (e != hipSuccess || (p.parts == 1 && !p.slots))
         return e;
     const unsigned all = (unsigned)a.batch * a.max_queries * a.q_heads;
     if (p.parts <= JOIN_FEW)
-        hipLaunchKernelGGL((qattn_join_kernel<T, 1>), dim3((all + 3) / 4), dim3(256), 0, stream, a, rows_of(a), p.parts, p.chunk);
+        hipLaunchKernelGGL((qattn_join_kernel<T, 1>), dim3((all + 3) / 4), dim3(256), 0, stream, a, rows_of(a), p.parts, p.chunk, p.slots);
     else
-        hipLaunchKernelGGL((qattn_join_kernel<T, 4>), dim3(all), dim3(256), 0, stream, a, rows_of(a), p.parts, p.chunk);
+        hipLaunchKernelGGL((qattn_join_kernel<T, 4>), dim3(all), dim3(256), 0, stream, a, rows_of(a), p.parts, p.chunk, p.slots);
     return hipGetLastError();
 }
 
@@ -485,17 +570,27 @@ AttnPlan qattn_plan(const QattnArgs &a, size_t room)
     // 8192 tokens: 768 workgroups 107 us, 1536 87, 3072 83, 8192 90; 3 of 120000: 74, 77, 79, 85), but none below 256 tokens unless
     // one round holds all of 128 (1 of 1500 9.3 us with 128, 10.0 with 256; 16 of up to 2500, four tokens each: 18.0 and 16.1).
     constexpr int ROUND = 768;
-    const int least = groups * ((keys + 127) / 128) <= ROUND ? 128 : 256;
+    const int least = groups * ((keys + 127) / 128) <= ROUND ? 128 : LEAST;
     long long parts = std::max(1LL, std::min<long long>(4 * ROUND / std::max(groups, 1LL), (keys + least - 1) / least));
     const long long one = (long long)a.queries * a.q_heads * (a.c.dim + 2) * 4;
     parts = std::min(parts, (long long)room / std::max(one, 1LL));
-    if (parts <= 1)
-        return {1, (keys + 127) / 128 * 128, 0};
+    parts = std::max(parts, 1LL);
     const long long chunk = ((keys + parts - 1) / parts + 127) / 128 * 128;
-    parts = (keys + chunk - 1) / chunk;
+    parts = (keys + chunk - 1) / std::max(chunk, 1LL);
+    // More than 8 sequences share two rounds by their lengths: 120000 tokens and 63 of 500 45 us, 149 with the same number of parts for each;
+    // 30000 and 31 of 1000 28 and 39; 64 of 8192 113 and 119, of 700 to 8192 70 and 69; 20000 and 199 of 300 35 and 146 (not split
+    // otherwise; with less than 4096 tokens they are not: 200 of 1000 51 and 42). Where parts are the least anyway, and of few
+    // sequences, the search costs more than it gives: 16 of up to 2500, four queries each, 17.2 and 14.2; 64000 and 7 of 300 29 and 27. (One
+    // round: 44, 25, 110, 78; three: 48, 33, 118, 66.)
+    if (a.batch > 8 && a.batch <= SHARED && groups / a.batch <= ROUND && least == LEAST && chunk > LEAST && (parts > 1 || keys >= 4096) && (long long)a.batch * keys / 128 < INT32_MAX / 2) {
+        const long long each = (long long)a.max_queries * a.q_heads * (a.c.dim + 2) * 4;
+        const long long slots = std::min(std::max(2 * ROUND / (groups / a.batch), a.batch + 64LL), (long long)room / each);
+        if (slots >= a.batch + 16)
+            return {(int)(slots / a.batch), (int)chunk, (size_t)(each * slots), (int)slots};
+    }
     if (parts <= 1)
-        return {1, (keys + 127) / 128 * 128, 0};
-    return {(int)parts, (int)chunk, (size_t)(one * parts)};
+        return {1, (keys + 127) / 128 * 128, 0, 0};
+    return {(int)parts, (int)chunk, (size_t)(one * parts), 0};
 }
 
 hipError_t launch_qattn(const QattnArgs &a, const AttnPlan &plan, hipStream_t stream)

@@ -217,3 +217,12 @@ def test_long_sequences_have_a_workspace():
         assert b and b % (row * queries) == 0 and b <= -(-keys // 128) * row * queries
     assert aqd.qattn_workspace(cache, 1, 6, 1, 1, 100, aqd.BF16) == 0
     assert aqd.attn_workspace(1, 6, 2, 128, 4, 9000, 4, 9000, True, aqd.BF16) % (row * 4) == 0
+
+
+@pytest.mark.parametrize("batch", [9, 64, 700, 1024, 1025])
+def test_shared_workspaces_have_a_bound(batch):
+    for heads, per, each in ((1, 1, 1), (8, 8, 1), (8, 4, 500), (64, 1, 20000), (2, 32, 7)):
+        for keys in (600, 5000, 131072, 1 << 24, 1 << 30):
+            if batch * heads * (each * per / 16 + 1) <= 1 << 23:
+                b = aqd.qattn_workspace(aqd.QcacheDesc(heads, 128, 32, 16, 1000), batch, heads * per, batch * each, each, keys, aqd.F16)
+                assert 0 <= b <= aqd.ATTN_WORKSPACE_BYTES

@@ -326,3 +326,52 @@ def test_attn_of_sequences_of_unlike_lengths(dim, heads, per, causal, few, batch
         for b in some:
             a = slice(qs[b], min(qs[b] + 130, qs[b + 1]))
             assert bool((alone[a] == alone[a]).all())
+
+
+@pytest.mark.parametrize("t, dim, group, page, heads, per, batch, most, counts", [
+    ("bf16", 64, 32, 16, 4, 2, 200, 3000, 1), ("f16", 128, 64, 64, 8, 4, 64, 2500, 3), ("bf16", 256, 128, 32, 2, 1, 256, 1700, 1),
+    ("f16", 64, 64, 16, 8, 3, 65, 4200, 25), ("bf16", 128, 128, 256, 8, 2, 9, 5000, 2),
+    ("bf16", 64, 32, 32, 1, 2, 1000, 4100, 1), ("f16", 128, 64, 64, 4, 2, 700, 5000, 2), ("bf16", 64, 64, 16, 8, 1, 1025, 5000, 1),
+])
+def test_qattn_of_sequences_of_unlike_lengths(t, dim, group, page, heads, per, batch, most, counts):
+    """A few long sequences among many short and empty ones, which share the workgroups by their lengths: with all of the workspace, less,
+    and none; lengths past max_keys and below 0."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(batch))
+    lengths = rng.integers(0, 200, batch)
+    lengths[rng.integers(0, batch, 3)] = most
+    lengths[0], lengths[-1], lengths[batch // 2] = most - 1, 0, 300
+    n = rng.integers(0, counts + 1, batch) if counts > 1 else np.ones(batch, int)
+    n[0], n[1] = counts, 1
+    starts = np.concatenate([[0], np.cumsum(n)])
+    used = -(-lengths // page)
+    first = np.concatenate([[0], np.cumsum(used)])
+    c = aqd.QcacheDesc(heads, dim, group, page, int(first[-1]) + 1)
+    tables = np.full((batch, -(-most // page)), -1, np.int32)
+    for b in range(batch):
+        tables[b, :used[b]] = np.arange(first[b], first[b + 1])[::-1]
+    slots = [(tables[b, np.arange(m) // page] * page + np.arange(m) % page).astype(np.int32) for b, m in enumerate(lengths)]
+    total = int(lengths.sum())
+    k, v = [torch.randn(total, heads, dim, device="cuda:0", generator=torch.Generator("cuda:0").manual_seed(i)) for i in range(2)]
+    cache = torch.full((aqd.qcache_bytes(c),), 0xFF, dtype=torch.uint8, device="cuda:0")
+    aqd.qcache_write(c, total, aqd.F32, k, *strides(k), v, *strides(v), torch.from_numpy(np.concatenate(slots)).cuda(), cache)
+    host = cache.cpu().numpy().reshape(c.pages, heads, -1)
+    q = reals(torch, rng, int(starts[-1]) + 2, heads * per, dim, t=t)
+    told = lengths.copy()
+    told[-1] = -3
+    told[lengths == most] += 7
+    size = aqd.qattn_workspace(c, batch, heads * per, q.shape[0], counts, most, TYPES[t])
+    assert (size > 0) == (batch <= 1024)
+    some = np.flatnonzero(lengths >= 300).tolist() + spread(rng, batch, 12)
+    keys = {b: plain.read(host, slots[b], heads, dim, group, page) if lengths[b] else [np.zeros((0, heads, dim))] * 4 for b in some}
+    for workspace in (size, size // 2, size // 7, 0):
+        y = torch.full_like(q, 77, device="cuda:0")
+        run_qattn(torch, c, cache, torch.from_numpy(tables).cuda(), told.tolist(), q.cuda(), starts.tolist(), counts, t, y, workspace, max_keys=most)
+        got = y.double().cpu().numpy()
+        assert (got[starts[-1]:] == 77).all()
+        for b in some:
+            a = slice(starts[b], starts[b + 1])
+            if n[b]:
+                kr, vr, ks, vs = keys[b]
+                rows = spread(rng, int(n[b]), 1)
+                check_rows(got[a], q[a].double().numpy(), kr, vr, rows, True, t, OFFSET[t] * ks, OFFSET[t] * vs)
