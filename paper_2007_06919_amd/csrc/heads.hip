@@ -6,7 +6,8 @@
 // the only thing that crosses lanes. fp32 throughout, one rounding at the store.
 //
 // Bound by HBM: a head is read and written once, the table's row and the weights come
-// from the caches.
+// from the caches. 16384 tokens of 40 heads, dim 128, bf16: 336 MB in 69 us, 4.9 TB/s (a copy of that
+// size 5.4). One token: 6 us, the launch.
 
 #include "internal.h"
 
@@ -35,7 +36,8 @@ __device__ __forceinline__ void store(T *p, const float *f)
 #pragma unroll
     for (int e = 0; e < N; ++e)
         v[e] = (T)f[e];
-    *(typename Some<T, N>::type *)p = v;
+    // past the L2: 16384 tokens of 40 heads, dim 128, bf16 69.4 us, 73.6 through it
+    __builtin_nontemporal_store(v, (typename Some<T, N>::type *)p);
 }
 
 // N pairs are a unit, 1 << LOG lanes hold a head and each has up to V units of it. Rotated
@@ -152,27 +154,30 @@ void launch_units(const HeadsArgs &a, hipStream_t stream)
         hipLaunchKernelGGL((heads_kernel<T, N, V, false>), grid, dim3(256), 0, stream, a, log);
 }
 
-// as many pairs at once as 16 bytes hold, where their number divides the rotated pairs and the others
+template <typename T, int N>
+void launch_width(const HeadsArgs &a, hipStream_t stream)
+{
+    constexpr int MOST = N < 8 ? 8 / N : 1;   // units of a lane of 64, of heads of 1024
+    if (a.dim <= 128 * N)
+        launch_units<T, N, 1>(a, stream);
+    else
+        launch_units<T, N, MOST>(a, stream);
+}
+
+// As many pairs at once as 16 bytes hold, or fewer where their number does not divide the rotated pairs and the others: 16384 tokens of
+// 40 heads, dim 128, bf16, in eights (128 channels rotated) 70 us, in fours (120) 90, in twos (124) 160, one by one (126) 264.
 template <typename T>
 void launch_type(const HeadsArgs &a, hipStream_t stream)
 {
-    constexpr int N = 16 / (int)sizeof(T);
     const int both = (a.rot / 2) | ((a.dim - a.rot) / 2);   // its lowest bit set is that of the two
-    if (both % N == 0) {
-        if (a.dim <= 128 * N)
-            launch_units<T, N, 1>(a, stream);
-        else
-            launch_units<T, N, 1024 / 128 / N + 1>(a, stream);
-    } else if (both % 2 == 0) {
-        if (a.dim <= 256)
-            launch_units<T, 2, 1>(a, stream);
-        else
-            launch_units<T, 2, 4>(a, stream);
-    } else if (a.dim <= 128) {
-        launch_units<T, 1, 1>(a, stream);
-    } else {
-        launch_units<T, 1, 8>(a, stream);
-    }
+    if (sizeof(T) == 2 && both % 8 == 0)
+        launch_width<T, 16 / (int)sizeof(T)>(a, stream);
+    else if (both % 4 == 0)
+        launch_width<T, 4>(a, stream);
+    else if (both % 2 == 0)
+        launch_width<T, 2>(a, stream);
+    else
+        launch_width<T, 1>(a, stream);
 }
 
 }  // namespace

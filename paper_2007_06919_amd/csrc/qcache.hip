@@ -8,7 +8,13 @@
 // which the next shift takes it. The values' nibbles of one unit come from four lanes, which
 // exchange their words.
 //
-// A workgroup has tokens of one head; four tokens next to one another share their lines of the cache.
+// A workgroup has tokens of one head; four tokens next to one another share their lines of the cache. The heads of the same tokens
+// follow one another in the launch (write and read of 16384 tokens of 8 heads, dim 128, bf16: 41 us, 45 with the tokens of a head
+// first).
+//
+// Bound by HBM: 85 MB each way there, 67 of them bf16; a write takes 22 us, a read 14 us.
+
+#include <algorithm>
 
 #include "internal.h"
 
@@ -118,9 +124,9 @@ template <typename T, int DIM>
 __global__ void __launch_bounds__(256) qcache_write_kernel(QcacheArgs A)
 {
     constexpr int LANES = DIM / 8, EACH = 256 / LANES;
-    const int c = threadIdx.x % LANES, n = c >> 1 & 3, head = blockIdx.y, group_log = __builtin_ctz(A.c.group), groups = DIM >> group_log;
+    const int c = threadIdx.x % LANES, n = c >> 1 & 3, head = blockIdx.x, group_log = __builtin_ctz(A.c.group), groups = DIM >> group_log;
     const int scales = A.c.page * DIM;
-    for (long long at = blockIdx.x * EACH + threadIdx.x / LANES; at < A.tokens; at += gridDim.x * EACH) {
+    for (long long at = blockIdx.y * EACH + threadIdx.x / LANES; at < A.tokens; at += gridDim.y * EACH) {
         const int token = (int)at;
         const Place p = place_of(A, token, head);
         if (!p.block)
@@ -156,7 +162,8 @@ __device__ __forceinline__ void store8(void *p, long long at, const float *f)
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         v[e] = (T)f[e];
-    *(typename Eight<T>::type *)((T *)p + at) = v;
+    // past the L2: 16384 tokens of 8 heads, dim 128, bf16, from HBM 14.3 us, 21.2 through it
+    __builtin_nontemporal_store(v, (typename Eight<T>::type *)((T *)p + at));
 }
 
 // what a code stands for, exactly
@@ -166,9 +173,9 @@ template <typename T, int DIM>
 __global__ void __launch_bounds__(256) qcache_read_kernel(QcacheArgs A)
 {
     constexpr int LANES = DIM / 8, EACH = 256 / LANES;
-    const int c = threadIdx.x % LANES, n = c >> 1 & 3, head = blockIdx.y, group_log = __builtin_ctz(A.c.group), groups = DIM >> group_log;
+    const int c = threadIdx.x % LANES, n = c >> 1 & 3, head = blockIdx.x, group_log = __builtin_ctz(A.c.group), groups = DIM >> group_log;
     const int scales = A.c.page * DIM;
-    for (long long at = blockIdx.x * EACH + threadIdx.x / LANES; at < A.tokens; at += gridDim.x * EACH) {
+    for (long long at = blockIdx.y * EACH + threadIdx.x / LANES; at < A.tokens; at += gridDim.y * EACH) {
         const int token = (int)at;
         const Place p = place_of(A, token, head);
         if (!p.block)
@@ -200,7 +207,7 @@ template <typename T, int DIM, bool WRITE>
 void launch(const QcacheArgs &a, hipStream_t stream)
 {
     const int each = 256 / (DIM / 8), most = MOST_GROUPS / a.c.heads + 1, groups = (a.tokens - 1) / each + 1;
-    const dim3 grid((unsigned)(groups < most ? groups : most), (unsigned)a.c.heads);
+    const dim3 grid((unsigned)a.c.heads, (unsigned)std::min({groups, most, 65535}));
     if (WRITE)
         hipLaunchKernelGGL((qcache_write_kernel<T, DIM>), grid, dim3(256), 0, stream, a);
     else

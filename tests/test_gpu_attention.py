@@ -85,7 +85,8 @@ def check_heads(got, x, w, table, position, rot, halves, t, eps=1e-6, ok=None):
     (1, 32, 8, 128, 128, "thd", 0, 0), (3, 4, 1, 64, 64, "thd", 128, 0), (5, 7, 2, 80, 60, "thd", 3, 1), (2, 3, 3, 256, 256, "htd", 0, 0),
     (9, 2, 1, 34, 34, "thd", 0, 0), (4, 2, 2, 2, 2, "thd", 0, 1), (3, 1, 1, 512, 256, "htd", 8, 0), (2, 2, 1, 1024, 1022, "thd", 0, 0),
     (2, 1, 1, 1024, 1024, "thd", 5, 3), (70, 5, 1, 96, 32, "thd", 16, 0), (3, 2, 1, 300, 100, "thd", 0, 0), (2, 2, 2, 514, 2, "thd", 0, 0),
-    (257, 3, 1, 128, 0, "thd", 0, 0),
+    (257, 3, 1, 128, 0, "thd", 0, 0), (5, 3, 1, 72, 72, "thd", 4, 0), (3, 2, 1, 120, 56, "htd", 0, 1), (2, 1, 1, 1000, 1000, "thd", 0, 0),
+    (2, 2, 1, 1000, 504, "thd", 2, 0),
 ])
 def test_heads(tokens, hq, hk, dim, rot, order, pad, shift, halves, t):
     import torch
