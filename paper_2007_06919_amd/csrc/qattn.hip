@@ -566,12 +566,13 @@ AttnPlan qattn_plan(const QattnArgs &a, size_t room)
 {
     const int keys = (int)std::min<long long>(a.max_keys, a.ld_table * a.c.page);
     const long long groups = (long long)a.batch * a.c.heads * row_tiles(a, rows_of(a));
-    // Three workgroups to a CU, of 128 tokens at a time. Four rounds of them, since the sequences may be of any length (64 of 700 to
-    // 8192 tokens: 768 workgroups 107 us, 1536 87, 3072 83, 8192 90; 3 of 120000: 74, 77, 79, 85), but none below 256 tokens unless
-    // one round holds all of 128 (1 of 1500 9.3 us with 128, 10.0 with 256; 16 of up to 2500, four tokens each: 18.0 and 16.1).
+    // Three workgroups to a CU, of 128 tokens at a time, and as many rounds of them as there are sequences, up to four, since one may have
+    // all the tokens: one of 120000 34 us in one round, 41 in four; 64000 and 7 of 300 49 in one round, 27 in four; 3 of 40000 34 and 38.
+    // But none below 256 tokens unless one round holds all of 128 (1 of 1500 9.3 us with 128, 10.0 with 256; 16 of up to 2500, four
+    // tokens each: 18.0 and 16.1).
     constexpr int ROUND = 768;
     const int least = groups * ((keys + 127) / 128) <= ROUND ? 128 : LEAST;
-    long long parts = std::max(1LL, std::min<long long>(4 * ROUND / std::max(groups, 1LL), (keys + least - 1) / least));
+    long long parts = std::max(1LL, std::min<long long>(std::min(a.batch, 4) * ROUND / groups, (keys + least - 1) / least));
     const long long one = (long long)a.queries * a.q_heads * (a.c.dim + 2) * 4;
     parts = std::min(parts, (long long)room / std::max(one, 1LL));
     parts = std::max(parts, 1LL);
@@ -582,7 +583,8 @@ AttnPlan qattn_plan(const QattnArgs &a, size_t room)
     // otherwise; with less than 4096 tokens they are not: 200 of 1000 51 and 42). Where parts are the least anyway, and of few
     // sequences, the search costs more than it gives: 16 of up to 2500, four queries each, 17.2 and 14.2; 64000 and 7 of 300 29 and 27. (One
     // round: 44, 25, 110, 78; three: 48, 33, 118, 66.)
-    if (a.batch > 8 && a.batch <= SHARED && groups / a.batch <= ROUND && least == LEAST && chunk > LEAST && (parts > 1 || keys >= 4096) && (long long)a.batch * keys / 128 < INT32_MAX / 2) {
+    if (a.batch > 8 && a.batch <= SHARED && groups / a.batch <= ROUND && least == LEAST && chunk > LEAST && (parts > 1 || keys >= 4096) &&
+        (long long)a.batch * keys / 128 < INT32_MAX / 2) {
         const long long each = (long long)a.max_queries * a.q_heads * (a.c.dim + 2) * 4;
         const long long slots = std::min(std::max(2 * ROUND / (groups / a.batch), a.batch + 64LL), (long long)room / each);
         if (slots >= a.batch + 16)
