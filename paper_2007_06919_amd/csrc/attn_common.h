@@ -73,7 +73,8 @@ struct JoinScratch {
     f32x4 sum[WAVES][64];
     float most[WAVES], total[WAVES];
 };
-constexpr int JOIN_FEW = 16;   // parts that one wave joins
+// Parts that one wave joins: 192 rows of 10 parts 14.8 us with what makes them, 16.6 with four waves a row; 192 of 90 87 and 83.
+constexpr int JOIN_FEW = 16;
 
 template <typename T, int WAVES>
 __device__ __forceinline__ void join_parts(JoinScratch<WAVES> &lds, const float *o, const float *stat, long long step, int parts, int dim, T *y)
