@@ -85,80 +85,6 @@ __device__ __forceinline__ int seen_by(const AttnArgs &A, const Span2 &s, int qu
     return A.causal ? max(s.m - s.n + 1 + query, 0) : s.m;
 }
 
-// Where sequences differ in length, most of a grid of the longest one's row tiles for each would have no rows. Row tile `item` of all
-// sequences' instead: those of up to 256 sequences by their number in the sequence, the highest first (they see most keys);
-// those of more one sequence after the other. False past the last one.
-__device__ __forceinline__ bool find_tile(const AttnArgs &A, int per, int tiles, int item, int &sequence_at, int &tile)
-{
-    const int lane = threadIdx.x & 63;
-    auto tiles_of = [&](int b) { return b < A.batch ? (max(sequence(A, b).n, 0) * per + ROWS - 1) / ROWS : 0; };
-    if (A.batch <= 256) {
-        int count[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            count[k] = 64 * k < A.batch ? tiles_of(64 * k + lane) : 0;
-        // how many have the number `least` or a higher one
-        auto from = [&](int least) {
-            int n = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                n += max(count[k] - least, 0);
-            return wave_sum(n);
-        };
-        if (item >= from(0))
-            return false;
-        int low = 0, high = tiles, above = 0;   // from(low) > item >= from(high) == above
-        while (high - low > 1) {
-            const int middle = (low + high) / 2, n = from(middle);
-            if (n > item) {
-                low = middle;
-            } else {
-                high = middle;
-                above = n;
-            }
-        }
-        int rest = item - above;
-        tile = low;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint64_t has = __builtin_amdgcn_ballot_w64(count[k] > low);
-            const int n = __builtin_popcountll(has);
-            if (rest >= 0 && rest < n) {
-                const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0));
-                sequence_at = 64 * k + __builtin_ctzll(__builtin_amdgcn_ballot_w64(count[k] > low && before == rest));
-                return true;
-            }
-            rest -= n;
-        }
-        return false;
-    }
-    // a lane has `each` sequences, then those of the lane that has the item are the lanes'
-    int first = 0, last = A.batch, rest = item;
-    for (;;) {
-        const int each = (last - first + 63) / 64, begin = min(first + lane * each, last), end = min(begin + each, last);
-        int n = 0;
-        for (int b = begin; b < end; ++b)
-            n += tiles_of(b);
-        int upto = n;   // with the lanes below
-        for (int d = 1; d < 64; d <<= 1) {
-            const int x = __shfl_up(upto, d);
-            upto += lane >= d ? x : 0;
-        }
-        const uint64_t past = __builtin_amdgcn_ballot_w64(upto > rest);
-        if (!past)
-            return false;
-        const int at = __builtin_ctzll(past);
-        rest -= __builtin_amdgcn_readlane(upto - n, at);
-        first = __builtin_amdgcn_readlane(begin, at);
-        last = __builtin_amdgcn_readlane(end, at);
-        if (each == 1) {
-            sequence_at = first;
-            tile = __builtin_amdgcn_readlane(n, at) - 1 - rest;
-            return true;
-        }
-    }
-}
-
 // DIRECT: rows of keys and values start at multiples of 4 bytes. tiles: of the longest sequence
 template <typename T, int DIM, bool DIRECT>
 __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_kernel(AttnArgs A, int tiles, int parts, int chunk, bool packed)
@@ -173,7 +99,7 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
     // the rows with most keys first
     int part = 0, row_tile, b;
     if (packed) {
-        if (!find_tile(A, per, tiles, rest, b, row_tile))
+        if (!find_tile(A.batch, tiles, rest, [&](int i) { return (max(sequence(A, i).n, 0) * per + ROWS - 1) / ROWS; }, b, row_tile))
             return;
     } else {
         b = rest % A.batch;

@@ -65,6 +65,80 @@ __device__ __forceinline__ int wave_scan(int x)
 }
 __device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
 
+// Where sequences differ in length, most of a grid of the longest one's row tiles for each would have no rows. Row tile `item` of all
+// sequences' (tiles_of(b) each, `tiles` at most) instead: those of up to 256 sequences by their number in the sequence, the highest first (they see most keys);
+// those of more one sequence after the other. False past the last one.
+template <typename F>
+__device__ __forceinline__ bool find_tile(int batch, int tiles, int item, F tiles_of, int &sequence_at, int &tile)
+{
+    const int lane = threadIdx.x & 63;
+    if (batch <= 256) {
+        int count[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            count[k] = 64 * k + lane < batch ? tiles_of(64 * k + lane) : 0;
+        // how many have the number `least` or a higher one
+        auto from = [&](int least) {
+            int n = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                n += max(count[k] - least, 0);
+            return wave_sum(n);
+        };
+        if (item >= from(0))
+            return false;
+        int low = 0, high = tiles, above = 0;   // from(low) > item >= from(high) == above
+        while (high - low > 1) {
+            const int middle = (low + high) / 2, n = from(middle);
+            if (n > item) {
+                low = middle;
+            } else {
+                high = middle;
+                above = n;
+            }
+        }
+        int rest = item - above;
+        tile = low;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint64_t has = __builtin_amdgcn_ballot_w64(count[k] > low);
+            const int n = __builtin_popcountll(has);
+            if (rest >= 0 && rest < n) {
+                const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0));
+                sequence_at = 64 * k + __builtin_ctzll(__builtin_amdgcn_ballot_w64(count[k] > low && before == rest));
+                return true;
+            }
+            rest -= n;
+        }
+        return false;
+    }
+    // a lane has `each` sequences, then those of the lane that has the item are the lanes'
+    int first = 0, last = batch, rest = item;
+    for (;;) {
+        const int each = (last - first + 63) / 64, begin = min(first + lane * each, last), end = min(begin + each, last);
+        int n = 0;
+        for (int b = begin; b < end; ++b)
+            n += tiles_of(b);
+        int upto = n;   // with the lanes below
+        for (int d = 1; d < 64; d <<= 1) {
+            const int x = __shfl_up(upto, d);
+            upto += lane >= d ? x : 0;
+        }
+        const uint64_t past = __builtin_amdgcn_ballot_w64(upto > rest);
+        if (!past)
+            return false;
+        const int at = __builtin_ctzll(past);
+        rest -= __builtin_amdgcn_readlane(upto - n, at);
+        first = __builtin_amdgcn_readlane(begin, at);
+        last = __builtin_amdgcn_readlane(end, at);
+        if (each == 1) {
+            sequence_at = first;
+            tile = __builtin_amdgcn_readlane(n, at) - 1 - rest;
+            return true;
+        }
+    }
+}
+
 // The parts of one row, sums o [dim] and references and totals stat [2], `step` rows from part to part: the row is
 // sum_p o_p 2^(ref_p - ref) / sum_p l_p 2^(ref_p - ref), zeros where there is no weight at all. WAVES waves (1 for few parts: rows
 // are many then, and a wave needs no barrier), of which 16, 32 or 64 lanes have four channels of a part each.

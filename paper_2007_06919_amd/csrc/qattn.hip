@@ -77,6 +77,10 @@ __device__ __forceinline__ Sequence sequence(const QattnArgs &A, int b)
     s.length = length_of(A, b);
     return s;
 }
+__device__ __forceinline__ int tiles_of(const QattnArgs &A, int b, int rows)
+{
+    return (max(sequence(A, b).n, 0) * (A.q_heads / A.c.heads) + rows - 1) / rows;
+}
 // Sequences of unlike lengths share `slots` workgroups (of a key head and row tile) by their tokens: a workgroup has
 // `chunk` of them at most, such that sum(floor(length / chunk) + 1) <= slots. Their results are numbered by sequence.
 struct Share {
@@ -159,7 +163,7 @@ struct Shape {
 };
 
 template <typename T, int DIM, int GROUP, int R>
-__global__ void __launch_bounds__(256, DIM == 256 ? (R == 2 || GROUP == 32 ? 1 : 2) : DIM == 128 && R == 2 ? 2 : 3) qattn_kernel(QattnArgs A, int tiles, int parts, int chunk, int slots)
+__global__ void __launch_bounds__(256, DIM == 256 ? (R == 2 || GROUP == 32 ? 1 : 2) : DIM == 128 && R == 2 ? 2 : 3) qattn_kernel(QattnArgs A, int tiles, int parts, int chunk, int slots, bool packed)
 {
     typedef Shape<DIM, GROUP, R> S;
     constexpr int G = S::GROUPS, U = DIM / 32, TILES = DIM / 16;
@@ -168,18 +172,23 @@ __global__ void __launch_bounds__(256, DIM == 256 ? (R == 2 || GROUP == 32 ? 1 :
     const int per = A.q_heads / A.c.heads;
     const int kv = blockIdx.x % A.c.heads;
     int rest = blockIdx.x / A.c.heads;
-    const int row_tile = rest % tiles;
-    rest /= tiles;
-    int part, b;
-    int slot = 0;
-    if (slots) {
-        Share s;
-        if (!Shared(A, slots).find(rest, s, part))
-            return;
-        b = s.b, slot = s.first + part, parts = s.parts, chunk = s.chunk;
-    } else {
+    int part, b, row_tile, slot = 0;
+    if (packed) {
         part = rest % parts;
-        b = rest / parts;
+        if (!find_tile(A.batch, tiles, rest / parts, [&](int i) { return tiles_of(A, i, 16 * R); }, b, row_tile))
+            return;
+    } else {
+        row_tile = rest % tiles;
+        rest /= tiles;
+        if (slots) {
+            Share s;
+            if (!Shared(A, slots).find(rest, s, part))
+                return;
+            b = s.b, slot = s.first + part, parts = s.parts, chunk = s.chunk;
+        } else {
+            part = rest % parts;
+            b = rest / parts;
+        }
     }
     const Sequence seq = sequence(A, b);
     const int first_row = row_tile * 16 * R, rows = seq.n * per;
@@ -494,6 +503,20 @@ __global__ void __launch_bounds__(256, DIM == 256 ? (R == 2 || GROUP == 32 ? 1 :
     }
 }
 
+// query i of sequence b
+template <typename T, int WAVES>
+__device__ __forceinline__ void join_row(JoinScratch<WAVES> &lds, const QattnArgs &A, const Sequence &seq, const Share &s, int i, int head, int rows, int parts,
+                                         int slots)
+{
+    // the parts that its workgroups' rows have
+    const int per = A.q_heads / A.c.heads, first_row = (i * per + head % per) / rows * rows;
+    const int limit = seen_by(seq, rows, first_row, per), used = max((limit + s.chunk - 1) / s.chunk, 1);
+    const long long query = seq.begin + i, step = slots ? (long long)A.max_queries * A.q_heads : 1;
+    const long long row = slots ? ((long long)s.first * A.max_queries + i) * A.q_heads + head : (query * A.q_heads + head) * parts;
+    join_parts<T, WAVES>(lds, A.part + row * A.c.dim, A.part + part_rows(A, slots, parts) * A.c.dim + 2 * row, step, used, A.c.dim,
+                         (T *)A.y + query * A.y_token + head * A.y_head);
+}
+
 template <typename T, int WAVES>
 __global__ void __launch_bounds__(256) qattn_join_kernel(QattnArgs A, int rows, int parts, int chunk, int slots)
 {
@@ -511,26 +534,38 @@ __global__ void __launch_bounds__(256) qattn_join_kernel(QattnArgs A, int rows, 
             return;
     }
     const Sequence seq = sequence(A, b);
-    if (i >= seq.n)
+    if (i < seq.n)
+        join_row<T, WAVES>(lds, A, seq, s, i, head, rows, parts, slots);
+}
+
+// the same where row tiles are packed: a workgroup has those of one tile and key head, a wave every fourth row
+template <typename T>
+__global__ void __launch_bounds__(256) qattn_join_packed_kernel(QattnArgs A, int tiles, int rows, int parts, int chunk)
+{
+    __shared__ JoinScratch<1> lds;
+    int b, row_tile;
+    if (!find_tile(A.batch, tiles, blockIdx.x / A.c.heads, [&](int i) { return tiles_of(A, i, rows); }, b, row_tile))
         return;
-    // the parts that its workgroups' rows have
-    const int per = A.q_heads / A.c.heads, first_row = (i * per + head % per) / rows * rows;
-    const int limit = seen_by(seq, rows, first_row, per), used = max((limit + s.chunk - 1) / s.chunk, 1);
-    const long long query = seq.begin + i, step = slots ? (long long)A.max_queries * A.q_heads : 1;
-    const long long row = slots ? ((long long)s.first * A.max_queries + i) * A.q_heads + head : (query * A.q_heads + head) * parts;
-    join_parts<T, WAVES>(lds, A.part + row * A.c.dim, A.part + part_rows(A, slots, parts) * A.c.dim + 2 * row, step, used, A.c.dim,
-                         (T *)A.y + query * A.y_token + head * A.y_head);
+    const Sequence seq = sequence(A, b);
+    const int per = A.q_heads / A.c.heads, kv = blockIdx.x % A.c.heads, end = min((row_tile + 1) * rows, seq.n * per);
+    for (int row = row_tile * rows + (threadIdx.x >> 6); row < end; row += 4)
+        join_row<T, 1>(lds, A, seq, {b, chunk, 0, parts, 0}, row / per, kv * per + row % per, rows, parts, 0);
 }
 
 int row_tiles(const QattnArgs &a, int rows) { return (a.max_queries * (a.q_heads / a.c.heads) + rows - 1) / rows; }
+// Row tiles that `queries` rows of sequences together can have, each but one of a sequence full; with those of the longest one for each where
+// that is a quarter more, a launch is packed (2000 tokens each: 512 queries of one sequence and one of 63 others 106 us, 203 otherwise).
+long long most_tiles(const QattnArgs &a, int rows) { return (long long)a.queries * (a.q_heads / a.c.heads) / rows + a.batch; }
+bool packed(const QattnArgs &a, int rows) { return 4LL * a.batch * row_tiles(a, rows) > 5 * most_tiles(a, rows); }
 int rows_of(const QattnArgs &a) { return a.max_queries * (a.q_heads / a.c.heads) <= 16 ? 16 : 32; }
 
 template <typename T, int DIM, int GROUP, int R>
 hipError_t launch_rows(const QattnArgs &a, const AttnPlan &p, hipStream_t stream)
 {
     const int tiles = row_tiles(a, 16 * R);
-    const dim3 grid((unsigned)(a.c.heads * tiles * (p.slots ? p.slots : p.parts * a.batch)));
-    hipLaunchKernelGGL((qattn_kernel<T, DIM, GROUP, R>), grid, dim3(256), 0, stream, a, tiles, p.parts, p.chunk, p.slots);
+    const bool few = packed(a, 16 * R);
+    const dim3 grid((unsigned)(a.c.heads * (few ? most_tiles(a, 16 * R) * p.parts : (long long)tiles * (p.slots ? p.slots : p.parts * a.batch))));
+    hipLaunchKernelGGL((qattn_kernel<T, DIM, GROUP, R>), grid, dim3(256), 0, stream, a, tiles, p.parts, p.chunk, p.slots, few);
     return hipGetLastError();
 }
 
@@ -558,10 +593,14 @@ hipError_t launch_type(const QattnArgs &a, const AttnPlan &p, hipStream_t stream
     if (e != hipSuccess || (p.parts == 1 && !p.slots))
         return e;
     const unsigned all = (unsigned)a.batch * a.max_queries * a.q_heads;
-    if (p.parts <= JOIN_FEW)
-        hipLaunchKernelGGL((qattn_join_kernel<T, 1>), dim3((all + 3) / 4), dim3(256), 0, stream, a, rows_of(a), p.parts, p.chunk, p.slots);
+    const int rows = rows_of(a);
+    if (packed(a, rows))
+        hipLaunchKernelGGL((qattn_join_packed_kernel<T>), dim3((unsigned)(a.c.heads * most_tiles(a, rows))), dim3(256), 0, stream, a, row_tiles(a, rows), rows,
+                           p.parts, p.chunk);
+    else if (p.parts <= JOIN_FEW)
+        hipLaunchKernelGGL((qattn_join_kernel<T, 1>), dim3((all + 3) / 4), dim3(256), 0, stream, a, rows, p.parts, p.chunk, p.slots);
     else
-        hipLaunchKernelGGL((qattn_join_kernel<T, 4>), dim3(all), dim3(256), 0, stream, a, rows_of(a), p.parts, p.chunk, p.slots);
+        hipLaunchKernelGGL((qattn_join_kernel<T, 4>), dim3(all), dim3(256), 0, stream, a, rows, p.parts, p.chunk, p.slots);
     return hipGetLastError();
 }
 
@@ -570,7 +609,8 @@ hipError_t launch_type(const QattnArgs &a, const AttnPlan &p, hipStream_t stream
 AttnPlan qattn_plan(const QattnArgs &a, size_t room)
 {
     const int keys = (int)std::min<long long>(a.max_keys, a.ld_table * a.c.page);
-    const long long groups = (long long)a.batch * a.c.heads * row_tiles(a, rows_of(a));
+    const int rows = rows_of(a);
+    const long long groups = a.c.heads * (packed(a, rows) ? most_tiles(a, rows) : (long long)a.batch * row_tiles(a, rows));
     // Three workgroups to a CU, of 128 tokens at a time, and as many rounds of them as there are sequences, up to four, since one may have
     // all the tokens: one of 120000 34 us in one round, 41 in four; 64000 and 7 of 300 49 in one round, 27 in four; 3 of 40000 34 and 38.
     // But none below 256 tokens unless one round holds all of 128 (1 of 1500 9.3 us with 128, 10.0 with 256; 16 of up to 2500, four
@@ -588,7 +628,7 @@ AttnPlan qattn_plan(const QattnArgs &a, size_t room)
     // otherwise; with less than 4096 tokens they are not: 200 of 1000 51 and 42). Where parts are the least anyway, and of few
     // sequences, the search costs more than it gives: 16 of up to 2500, four queries each, 17.2 and 14.2; 64000 and 7 of 300 29 and 27. (One
     // round: 44, 25, 110, 78; three: 48, 33, 118, 66.)
-    if (a.batch > 8 && a.batch <= SHARED && groups / a.batch <= ROUND && least == LEAST && chunk > LEAST && (parts > 1 || keys >= 4096) &&
+    if (!packed(a, rows) && a.batch > 8 && a.batch <= SHARED && groups / a.batch <= ROUND && least == LEAST && chunk > LEAST && (parts > 1 || keys >= 4096) &&
         (long long)a.batch * keys / 128 < INT32_MAX / 2) {
         const long long each = (long long)a.max_queries * a.q_heads * (a.c.dim + 2) * 4;
         const long long slots = std::min(std::max(2 * ROUND / (groups / a.batch), a.batch + 64LL), (long long)room / each);

@@ -375,3 +375,37 @@ def test_qattn_of_sequences_of_unlike_lengths(t, dim, group, page, heads, per, b
                 kr, vr, ks, vs = keys[b]
                 rows = spread(rng, int(n[b]), 1)
                 check_rows(got[a], q[a].double().numpy(), kr, vr, rows, True, t, OFFSET[t] * ks, OFFSET[t] * vs)
+
+
+@pytest.mark.parametrize("t, dim, group, heads, per, batch, many, most", [
+    ("bf16", 128, 64, 4, 4, 33, 200, 1500), ("f16", 64, 32, 1, 1, 300, 150, 900), ("bf16", 256, 128, 2, 3, 6, 70, 3000), ("bf16", 64, 64, 8, 2, 3, 120, 500),
+])
+def test_qattn_of_unlike_numbers_of_queries(t, dim, group, heads, per, batch, many, most):
+    """One sequence with many queries among others with one or none, split and whole."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(many))
+    n = rng.integers(0, 3, batch)
+    n[batch // 3], n[-1] = many, 2
+    lengths = np.maximum(rng.integers(0, most + 1, batch), n)
+    lengths[0] = 0
+    n[0] = 1
+    lengths[batch // 3] = most
+    starts = np.concatenate([[0], np.cumsum(n)])
+    s = Both(torch, 20, t=t, dim=dim, heads=heads, per=per, n=most, queries=2)        # its cache: all sequences have the same pages
+    if group != s.c.group:
+        s.c = aqd.QcacheDesc(heads, dim, group, s.c.page, s.c.pages)
+        s.cache = torch.zeros(aqd.qcache_bytes(s.c), dtype=torch.uint8, device="cuda:0")
+    s.write()
+    host = s.cache.cpu().numpy().reshape(s.c.pages, heads, -1)
+    kr, vr, ks, vs = plain.read(host, np.arange(most), heads, dim, group, s.c.page)
+    q = reals(torch, rng, int(starts[-1]) + 3, heads * per, dim, t=t)
+    tables = s.table.repeat(batch, 1).contiguous()
+    for workspace in (aqd.ATTN_WORKSPACE_BYTES, 0):
+        y = torch.full_like(q, 77, device="cuda:0")
+        run_qattn(torch, s.c, s.cache, tables, lengths.tolist(), q.cuda(), starts.tolist(), many, t, y, workspace)
+        got = y.double().cpu().numpy()
+        assert (got[starts[-1]:] == 77).all()
+        for b in {batch // 3, batch - 1, 0, *spread(rng, batch, 8)}:
+            a, m = slice(starts[b], starts[b + 1]), lengths[b]
+            if n[b]:
+                check_rows(got[a], q[a].double().numpy(), kr[:m], vr[:m], spread(rng, int(n[b]), 4), True, t, OFFSET[t] * ks[:m], OFFSET[t] * vs[:m])
