@@ -96,7 +96,7 @@ class PagedCache:
             raise ValueError("a step names sequences of the cache, each once, and a count for each")
         if any(n < 0 for n in counts):
             raise ValueError("a count is negative")
-        need = [-(-(self.lengths[i] + n) // self.page) - len(self.pages_of[i]) for i, n in zip(ids, counts)]
+        need = [max(0, -(-(self.lengths[i] + n) // self.page) - len(self.pages_of[i])) for i, n in zip(ids, counts)]
         if sum(need) > len(self.free):
             raise MemoryError(f"{sum(need)} pages are needed, {len(self.free)} are free")
         for i, n in zip(ids, need):

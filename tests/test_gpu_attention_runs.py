@@ -409,3 +409,71 @@ def test_qattn_of_unlike_numbers_of_queries(t, dim, group, heads, per, batch, ma
             a, m = slice(starts[b], starts[b + 1]), lengths[b]
             if n[b]:
                 check_rows(got[a], q[a].double().numpy(), kr[:m], vr[:m], spread(rng, int(n[b]), 4), True, t, OFFSET[t] * ks[:m], OFFSET[t] * vs[:m])
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("scale", [0.0, -0.0, -0.11, 1.0, 1e-30])
+def test_scales(scale, t):
+    """None (every key the same weight), negative and large ones; keys hidden or not."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(21))
+    dim, page = 64, 16
+    q, (k, v) = reals(torch, rng, 20, 4, dim, t=t), [reals(torch, rng, 90, 2, dim, t=t) for _ in range(2)]
+    n64 = [x.double().numpy() for x in (q, k, v)]
+    c = aqd.QcacheDesc(2, dim, 32, page, 6)
+    cache = torch.zeros(aqd.qcache_bytes(c), dtype=torch.uint8, device="cuda:0")
+    slots = torch.arange(90, dtype=torch.int32, device="cuda:0")
+    kd, vd = k.cuda(), v.cuda()
+    aqd.qcache_write(c, 90, TYPES[t], kd, *strides(kd), vd, *strides(vd), slots, cache)
+    kr, vr, ks, vs = plain.read(cache.cpu().numpy().reshape(6, 2, -1), np.arange(90), 2, dim, 32, page)
+    y = torch.zeros_like(q, device="cuda:0")
+    for workspace in (aqd.ATTN_WORKSPACE_BYTES, 0):
+        for causal in (True, False):
+            run_attn(torch, q.cuda(), kd, vd, [0, 20], [0, 90], causal, t, y, workspace, scale=scale)
+            check_attention(y.double().cpu().numpy(), *n64, scale, causal, t, name=f"prompt {causal}")
+        for count in (20, 1):                                                  # 32 and 16 rows a workgroup
+            some = q[:count].cuda()
+            run_qattn(torch, c, cache, slots[:6].view(1, 6), [90], some, [0, count], count, t, y[:count], workspace, scale=scale)
+            check_attention(y[:count].double().cpu().numpy(), n64[0][:count], kr, vr, scale, True, t, OFFSET[t] * ks, OFFSET[t] * vs, name=f"cache {count}")
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("dim, order, pad, shift", [(128, "thd", 2, 2), (64, "htd", 6, 4), (256, "thd", 2, 6), (72, "htd", 2, 2)])
+def test_attn_of_rows_at_multiples_of_four_bytes(dim, order, pad, shift, t):
+    """Rows that the copies take as they lie, though not at multiples of 16 bytes."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(dim + pad))
+    q, (k, v) = reals(torch, rng, 150, 4, dim, t=t), [reals(torch, rng, 170, 2, dim, t=t) for _ in range(2)]
+    views = [device(torch, x, order, pad, shift, float("nan"))[1] for x in (q, k, v)]
+    yb, y = device(torch, torch.full_like(q, 77), order, pad, shift)
+    run_attn(torch, *views, [0, 150], [0, 170], True, t, y)
+    check_attention(y.double().cpu().numpy(), *(x.double().numpy() for x in (q, k, v)), dim ** -0.5, True, t)
+    y.fill_(77)
+    assert bool((yb == 77).all())
+
+
+def test_slots_that_repeat():
+    """A read may name a slot twice, and pages may be of several sequences."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(22))
+    t, heads, dim, group, page = "bf16", 2, 64, 64, 32
+    c = aqd.QcacheDesc(heads, dim, group, page, 4)
+    cache = torch.zeros(aqd.qcache_bytes(c), dtype=torch.uint8, device="cuda:0")
+    k, v = [reals(torch, rng, 100, heads, dim, t=t).cuda() for _ in range(2)]
+    aqd.qcache_write(c, 100, TYPES[t], k, *strides(k), v, *strides(v), torch.arange(100, dtype=torch.int32, device="cuda:0"), cache)
+    slots = torch.tensor(([3, 3, 77, -5, 3, 128, 0] * 9), dtype=torch.int32, device="cuda:0")
+    ko, vo = [torch.full((len(slots), heads, dim), 77.0, device="cuda:0") for _ in range(2)]
+    aqd.qcache_read(c, len(slots), aqd.F32, cache, slots, ko, *strides(ko), vo, *strides(vo))
+    kr, vr, ks, vs = plain.read(cache.cpu().numpy().reshape(4, heads, -1), np.arange(100), heads, dim, group, page)
+    for i, s in enumerate(slots.tolist()):
+        for out, want in ((ko, kr), (vo, vr)):
+            assert np.array_equal(out[i].cpu().numpy(), want[s]) if 0 <= s < 100 else bool((out[i] == 77).all())
+    tables = torch.tensor([[0, 1, 1, 2], [0, 1, 2, 3], [0, 0, 0, 0]], dtype=torch.int32, device="cuda:0")
+    lengths = [97, 100, 65]
+    q = reals(torch, rng, 3, heads * 2, dim, t=t)
+    y = torch.zeros_like(q, device="cuda:0")
+    run_qattn(torch, c, cache, tables, lengths, q.cuda(), None, 1, t, y)
+    for b, m in enumerate(lengths):
+        at = tables[b].cpu().numpy()[np.arange(m) // page] * page + np.arange(m) % page
+        check_attention(y[b:b + 1].double().cpu().numpy(), q[b:b + 1].double().numpy(), kr[at], vr[at], dim ** -0.5, True, t, OFFSET[t] * ks[at],
+                        OFFSET[t] * vs[at], name=f"sequence {b}")
