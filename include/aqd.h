@@ -478,7 +478,8 @@ aqd_status_t qcache_read(const qcache_rows_desc_t *desc, const void *cache, cons
  *
  * workspace (device, 16-byte aligned, ws_bytes): with it, the tokens of long sequences are split between workgroups, which
  * is what makes few sequences fast. qattn_workspace gives the size for a call (never more than AQD_ATTN_WORKSPACE_BYTES); with
- * less, or NULL, the launch splits less or not at all. Calls that share a workspace must not overlap in time. */
+ * less, or NULL, the launch splits less or not at all. The split goes by the sizes here and by all lengths: a call gives the same
+ * bits each time, a sequence in another batch need not. Calls that share a workspace must not overlap in time. */
 #define AQD_ATTN_WORKSPACE_BYTES (64u << 20)
 typedef struct {
     qcache_desc_t cache;

@@ -1,5 +1,5 @@
-// What the two attention kernels share: operands of the matrix cores, exchanges between the
-// lanes of a column, and the sum of the parts of split keys.
+// What the two attention kernels share: operands of the matrix cores, the row tiles of sequences that
+// differ in length, copies into LDS, and the sum of the parts of split keys.
 #pragma once
 
 #include "internal.h"

@@ -159,3 +159,22 @@ def test_scales_have_32_bits_whatever_the_default_type(calls):
     finally:
         torch.set_default_dtype(torch.float32)
     assert all(t.dtype == torch.float32 for t in (block.q1, block.q2, block.s1, block.s2, table))
+
+
+def test_a_step_that_fails_leaves_its_pages_for_the_next(calls, monkeypatch):
+    c = cache(4)
+    a, b = c.add(), c.add()
+
+    def fails(*args):
+        raise RuntimeError("no memory for the step")
+
+    with monkeypatch.context() as m:
+        m.setattr(attn, "Step", fails)
+        with pytest.raises(RuntimeError):
+            c.step([a], [40])                       # three pages, of which the next step needs one
+    assert c.lengths[a] == 0
+    c.step([a], [10])
+    with pytest.raises(MemoryError):
+        c.step([a, b], [1, 32])
+    step = c.step([a, b], [30, 16])
+    assert step.rows == 46 and not c.free
