@@ -16,8 +16,8 @@
 // of the cycles, the matrix cores 16%. With groups of 128 and 3 of 120000 (64 heads on 8) 74 us and 8 for the second launch.
 // 64 of 8192 with groups of 64 take 111 us, 5.1 TB/s. One sequence of 1500: 9.2 us, two launches of 5.2 and 4.2.
 //
-// fp16 weights have few exponents: there the softmax's reference is the largest score plus the exponent of the values'
-// scales, so that the product of weight and scale is near 1 whatever the values' size.
+// fp16 weights have few exponents: there the softmax's reference is the largest sum of a score and the exponent of its value's
+// scales, so that the largest product of weight and scale is near 1 whatever the values' sizes.
 
 #include <algorithm>
 
@@ -383,30 +383,43 @@ __global__ void __launch_bounds__(256, DIM == 256 ? (R == 2 || GROUP == 32 ? 1 :
                     }
                 }
         }
-        // exponent of the largest value scale of the lane's tokens that is a number
-        float size = 0.f;
+        // of each token the exponent of its largest value scale that is a number (for 32 sequences of 8192 one for each lane's eight would be 2 to
+        // 7% faster, but takes the bits of small values next to large ones that weigh little or are hidden)
+        float size[8];
         if constexpr (Code<T>::NARROW) {
-            uint32_t top = 0;
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int i = 0; i < 2 * G; ++i) {
-                    // without its sign, and with a carry that takes infinity and NaN below all numbers
+                for (int i = 0; i < 4; ++i) {
+                    // without its sign, and with a carry that takes infinity and NaN below all numbers: the exponent + 128 in bits 8 to 15
                     typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-                    const u16x2 x = __builtin_bit_cast(u16x2, vs[half][i]) * (unsigned short)2 + (unsigned short)0x100;
-                    top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, __builtin_bit_cast(u16x2, top)));
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int j = i * G / 2; j <= ((i + 1) * G - 1) / 2; ++j) {
+                        const u16x2 x = __builtin_bit_cast(u16x2, vs[half][j]) * (unsigned short)2 + (unsigned short)0x100;
+                        top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, __builtin_bit_cast(u16x2, top)));
+                    }
+                    const float low = (float)(top >> 8 & 255u), high = (float)(top >> 24), e = G == 1 ? (i & 1 ? high : low) : fmaxf(low, high);
+                    // (weights of values that T rounds to 0 need not be near 1, and their sum has to stay a number)
+                    size[4 * half + i] = __builtin_amdgcn_fmed3f(e - 128.f, -40.f, 100.f);
                 }
-            const int e = (int)max(top >> 24, (top & 0xFFFFu) >> 8) - 1 - 127;
-            // (weights of values that T rounds to 0 need not be near 1, and their sum has to stay a number)
-            size = (float)min(max(e, -40), 100);
         }
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            float top = s[k][0];
+            // the largest weight, or product of a weight and a scale
+            float top;
+            if constexpr (Code<T>::NARROW) {
+                top = __builtin_fmaf(s[k][0], scale, size[0]);
 #pragma unroll
-            for (int i = 1; i < 8; ++i)
-                top = fmaxf(top, s[k][i]);
-            top = __builtin_fmaf(top, scale, size);
+                for (int i = 1; i < 8; ++i)
+                    top = fmaxf(top, __builtin_fmaf(s[k][i], scale, size[i]));
+            } else {
+                top = s[k][0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i)
+                    top = fmaxf(top, s[k][i]);
+                top *= scale;
+            }
             // weights up to 2^8 are as good as up to 1: the reference moves seldom
             if (__builtin_amdgcn_ballot_w64(top > ref[k] + 8.f)) {
                 top = fmaxf(top, __shfl_xor(top, 16));

@@ -477,3 +477,47 @@ def test_slots_that_repeat():
         at = tables[b].cpu().numpy()[np.arange(m) // page] * page + np.arange(m) % page
         check_attention(y[b:b + 1].double().cpu().numpy(), q[b:b + 1].double().numpy(), kr[at], vr[at], dim ** -0.5, True, t, OFFSET[t] * ks[at],
                         OFFSET[t] * vs[at], name=f"sequence {b}")
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("count", [1, 12])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_values_of_unlike_sizes(group, count, t):
+    """Tokens whose values are a million times as large as their neighbours', hidden from most queries or of hardly any weight, leave
+    the others' bits alone. (Products of a weight and a scale are within half a step of T, or of its smallest numbers where the row's
+    largest product is between 1/2 and 2^9: 2^-24 of that for each token, times codes up to 8.)"""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(group + count))
+    heads, per, dim, page, n = 2, 4, 128, 16, 200
+    c = aqd.QcacheDesc(heads, dim, group, page, -(-n // page))
+    q = reals(torch, rng, count, heads * per, dim, t=t)
+    k, v = [torch.from_numpy(rng.standard_normal((n, heads, dim))).float() for _ in range(2)]
+    v[::7] *= 1e6
+    k[::7] = -3.0 * q[:, ::per].float().mean(0, keepdim=True)                  # their scores are low
+    v *= 1e-4
+    v[n - count // 2:n - count // 2 + 3] *= 1e4                                # seen by the last queries only
+    k, v = k.cuda(), v.cuda()
+    cache = torch.zeros(aqd.qcache_bytes(c), dtype=torch.uint8, device="cuda:0")
+    slots = torch.arange(n, dtype=torch.int32, device="cuda:0")
+    aqd.qcache_write(c, n, aqd.F32, k, *strides(k), v, *strides(v), slots, cache)
+    kr, vr, ks, vs = plain.read(cache.cpu().numpy().reshape(c.pages, heads, -1), np.arange(n), heads, dim, group, page)
+    y = torch.zeros_like(q, device="cuda:0")
+    for workspace in (aqd.ATTN_WORKSPACE_BYTES, 0):
+        run_qattn(torch, c, cache, slots[:c.pages].view(1, -1), [n], q.cuda(), [0, count], count, t, y, workspace, scale=1.0)
+        got, q64 = y.double().cpu().numpy(), q.double().numpy()
+        for i in range(count):
+            m = n - count + 1 + i
+            want, rest, size, most = plain.attention(q64[i:i + 1], kr[:m], vr[:m], 1.0, False, OFFSET[t] * ks[:m], OFFSET[t] * vs[:m])
+            weights = plain.attention(q64[i:i + 1], kr[:m], vr[:m], 1.0, False)[2]
+            s = np.einsum("thd,hpd->thp", kr[:m], q64[i].reshape(heads, per, dim))
+            p = np.exp(s - s.max(0))
+            largest = (p / p.sum(0) * vs[:m].max(-1)[:, :, None]).max(0).reshape(-1)   # product of a weight and a scale
+            tol = (dim / 8 + 2) * 2 * 2.0 ** -24 * most[..., None] * rest + (plain.HALF[t] + 8 * 2.0 ** -24) * weights + \
+                (m / 8 + 8) * 2 * 2.0 ** -24 * size + plain.HALF[t] * np.abs(want) * 1.01 + plain.LEAST[t]
+            if t == "f16":
+                tol = tol + m * 2.0 ** -24 * largest[None, :, None] * 8
+            one = got[i:i + 1]
+            # fp16 rounds what is 65520 or more, half a step past its largest number, to infinity
+            past = (t == "f16") & np.isinf(one) & (one * want > 0) & (np.abs(want) + tol >= 65520)
+            off = np.abs(np.where(past, want, one) - want)
+            assert (off <= tol).all(), (i, float((off / tol).max()))
