@@ -12,8 +12,8 @@
 // scores of the group in fp32, a value's scale its weights before they are rounded to T.
 //
 // Bound by the vector units, and by how even the workgroups are: 64 sequences of 700 to 8192 tokens, 32 query heads on 8, dim 128, groups of 32
-// take 82 us, 334 MB at 4.0 TB/s; 380 vector instructions a step of 32 tokens (112 of them make operands of codes, 150 apply scales) are 52%
-// of the cycles, the matrix cores 16%. With groups of 128 and 3 of 120000 (64 heads on 8) 74 us and 8 for the second launch.
+// take 82 us, 334 MB at 4.0 TB/s; 368 vector instructions a step of 32 tokens (112 of them make operands of codes, 150 apply scales) are 54%
+// of the cycles, the matrix cores 14%. With groups of 128 and 3 of 120000 (64 heads on 8) 74 us and 8 for the second launch.
 // 64 of 8192 with groups of 64 take 111 us, 5.1 TB/s. One sequence of 1500: 9.2 us, two launches of 5.2 and 4.2.
 //
 // fp16 weights have few exponents: there the softmax's reference is the largest sum of a score and the exponent of its value's
