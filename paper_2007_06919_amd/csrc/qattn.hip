@@ -1,6 +1,6 @@
 // Attention over the 4-bit cache. Definition and layout: include/aqd.h.
 //
-// A workgroup has one sequence, one key head, 16 or 32 rows (the query heads of the key head, times
+// A workgroup has one sequence, one key head, 16 rows (32 of dim 64 where there are so many: the query heads of the key head, times
 // the sequence's queries) and a range of tokens; its four waves take 32 tokens in turn, each with a
 // softmax of its own, joined at the end. With S^T = K Q^T and O^T = V^T P^T (16 x 16 x 32 products) the
 // scores' lanes are the weights' lanes: lane (r, g) has the scores of tokens 4 g .. 4 g + 3 of a tile of 16 for row r,
@@ -163,7 +163,7 @@ struct Shape {
 };
 
 template <typename T, int DIM, int GROUP, int R>
-__global__ void __launch_bounds__(256, DIM == 256 ? (R == 2 || GROUP == 32 ? 1 : 2) : DIM == 128 && R == 2 ? 2 : 3) qattn_kernel(QattnArgs A, int tiles, int parts, int chunk, int slots, bool packed)
+__global__ void __launch_bounds__(256, DIM == 256 ? (GROUP == 32 ? 1 : 2) : 3) qattn_kernel(QattnArgs A, int tiles, int parts, int chunk, int slots, bool packed)
 {
     typedef Shape<DIM, GROUP, R> S;
     constexpr int G = S::GROUPS, U = DIM / 32, TILES = DIM / 16;
@@ -581,10 +581,13 @@ __global__ void __launch_bounds__(256) qattn_join_packed_kernel(QattnArgs A, int
 
 int row_tiles(const QattnArgs &a, int rows) { return (a.max_queries * (a.q_heads / a.c.heads) + rows - 1) / rows; }
 // Row tiles that `queries` rows of sequences together can have, each but one of a sequence full; with those of the longest one for each where
-// that is a quarter more, a launch is packed (2000 tokens each: 512 queries of one sequence and one of 63 others 106 us, 203 otherwise).
+// that is a quarter more, a launch is packed (2000 tokens each: 512 queries of one sequence and one of 63 others 106 us, 203 otherwise,
+// with 32 rows a workgroup; 62 with 16).
 long long most_tiles(const QattnArgs &a, int rows) { return (long long)a.queries * (a.q_heads / a.c.heads) / rows + a.batch; }
 bool packed(const QattnArgs &a, int rows) { return 4LL * a.batch * row_tiles(a, rows) > 5 * most_tiles(a, rows); }
-int rows_of(const QattnArgs &a) { return a.max_queries * (a.q_heads / a.c.heads) <= 16 ? 16 : 32; }
+// Rows of a workgroup: 32 of dim 64 where there are as many (8 queries each over 32 sequences of 8192, 32 query heads on 8: 62 us, 66 with 16;
+// dim 128 98 and 97, dim 256 253 and 183, where 32 rows leave one workgroup on a CU).
+int rows_of(const QattnArgs &a) { return a.c.dim == 64 && a.max_queries * (a.q_heads / a.c.heads) > 16 ? 32 : 16; }
 
 template <typename T, int DIM, int GROUP, int R>
 hipError_t launch_rows(const QattnArgs &a, const AttnPlan &p, hipStream_t stream)
@@ -599,7 +602,10 @@ hipError_t launch_rows(const QattnArgs &a, const AttnPlan &p, hipStream_t stream
 template <typename T, int DIM, int GROUP>
 hipError_t launch_group(const QattnArgs &a, const AttnPlan &p, hipStream_t stream)
 {
-    return rows_of(a) == 16 ? launch_rows<T, DIM, GROUP, 1>(a, p, stream) : launch_rows<T, DIM, GROUP, 2>(a, p, stream);
+    if constexpr (DIM == 64)
+        if (rows_of(a) == 32)
+            return launch_rows<T, DIM, GROUP, 2>(a, p, stream);
+    return launch_rows<T, DIM, GROUP, 1>(a, p, stream);
 }
 
 template <typename T, int DIM>
