@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
     const int limit = seen_by(A, seq, min((first_row + ROWS - 1) / per, seq.n - 1)), start = part * chunk;
     // (a sequence may have more keys than max_keys: the last part takes them all)
-    const int end = part + 1 < parts ? min(start + chunk, limit) : limit;
+    const int end = part + 1 < parts ? start + min(chunk, limit - start) : limit;
     if (part && start >= limit)
         return;
     const int wave_row = first_row + 32 * wave;
@@ -440,7 +440,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs A, int parts, i
         return;
     // the parts that its workgroup's rows have
     const int per = A.q_heads / A.heads, last_row = (i * per + head % per) / ROWS * ROWS + ROWS - 1;
-    const int limit = seen_by(A, seq, min(last_row / per, seq.n - 1)), used = min(max((limit + chunk - 1) / chunk, 1), parts);
+    const int limit = seen_by(A, seq, min(last_row / per, seq.n - 1)), used = min(parts_of(limit, chunk), parts);
     const long long query = seq.begin + i;
     const long long row = (query * A.q_heads + head) * parts, all = (long long)A.queries * A.q_heads * parts;
     join_parts<T, WAVES>(lds, A.part + row * A.dim, A.part + all * A.dim + 2 * row, 1, used, A.dim, (T *)A.y + query * A.y_token + head * A.y_head);

@@ -139,6 +139,9 @@ __device__ __forceinline__ bool find_tile(int batch, int tiles, int item, F tile
     }
 }
 
+// How many parts of `chunk` keys the first `limit` are in, one at least. (limit + chunk may pass 32 bits.)
+__device__ __forceinline__ int parts_of(int limit, int chunk) { return limit > 0 ? (limit - 1) / chunk + 1 : 1; }
+
 // The parts of one row, sums o [dim] and references and totals stat [2], `step` rows from part to part: the row is
 // sum_p o_p 2^(ref_p - ref) / sum_p l_p 2^(ref_p - ref), zeros where there is no weight at all. WAVES waves (1 for few parts: rows
 // are many then, and a wave needs no barrier), of which 16, 32 or 64 lanes have four channels of a part each.

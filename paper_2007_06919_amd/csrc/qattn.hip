@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(256, DIM == 256 ? (GROUP == 32 ? 1 : 2) : 3) q
     const int first_row = row_tile * 16 * R, rows = seq.n * per;
     if (first_row >= rows)
         return;
-    const int limit = seen_by(seq, 16 * R, first_row, per), start = part * chunk, end = min(start + chunk, limit);
+    const int limit = seen_by(seq, 16 * R, first_row, per), start = part * chunk, end = start + min(chunk, limit - start);
     if (part && start >= limit)
         return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
@@ -537,7 +537,7 @@ __device__ __forceinline__ void join_row(JoinScratch<WAVES> &lds, const QattnArg
 {
     // the parts that its workgroups' rows have
     const int per = A.q_heads / A.c.heads, first_row = (i * per + head % per) / rows * rows;
-    const int limit = seen_by(seq, rows, first_row, per), used = max((limit + s.chunk - 1) / s.chunk, 1);
+    const int limit = seen_by(seq, rows, first_row, per), used = parts_of(limit, s.chunk);
     const long long query = seq.begin + i, step = slots ? (long long)A.max_queries * A.q_heads : 1;
     const long long row = slots ? ((long long)s.first * A.max_queries + i) * A.q_heads + head : (query * A.q_heads + head) * parts;
     join_parts<T, WAVES>(lds, A.part + row * A.c.dim, A.part + part_rows(A, slots, parts) * A.c.dim + 2 * row, step, used, A.c.dim,

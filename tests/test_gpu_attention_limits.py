@@ -1,0 +1,59 @@
+"""The attention operators at the ends of what their arguments may be: keys next to 2^31, values and scores next to fp32's largest
+numbers. Tolerances: test_gpu_attention.py."""
+import numpy as np
+import pytest
+
+import attention_plain as plain
+from paper_2007_06919_amd import aqd
+from test_gpu_attention import OFFSET, U, Sequences, check_attention, close, reals, run_attn, run_qattn, strides
+
+pytestmark = pytest.mark.gpu
+
+MOST_KEYS = 2 ** 31 - 1 - 65536
+
+
+def test_qattn_of_as_many_tokens_as_there_may_be():
+    """One page again and again, and another at the end, whose tokens have nearly all of the weight: e^40 each, the others 1."""
+    import torch
+    dim, page, last, t = 64, 256, 100, "bf16"
+    c = aqd.QcacheDesc(1, dim, 64, page, 2)
+    rng = np.random.Generator(np.random.PCG64(31))
+    k, v = np.zeros((2 * page, 1, dim), np.float32), rng.standard_normal((2 * page, 1, dim)).astype(np.float32)
+    k[page:] = 0.625                                                  # a group's largest element is kept: -5/64 in bf16, and -8
+    v[page:] += 3
+    cache = np.zeros((2, 1, plain.block_bytes(dim, 64, page)), np.uint8)
+    slots = np.arange(2 * page)
+    plain.write(cache, slots, k, v, 1, dim, 64, page)
+    kr, vr, ks, vs = plain.read(cache, slots, 1, dim, 64, page)
+    tables = torch.zeros(1, -(-MOST_KEYS // page), dtype=torch.int32, device="cuda:0")
+    tables[0, -last:] = 1
+    q = torch.ones(1, 1, dim).bfloat16()
+    y = torch.zeros_like(q, device="cuda:0")
+    run_qattn(torch, c, torch.from_numpy(cache).cuda(), tables, [MOST_KEYS], q.cuda(), None, 1, t, y, scale=1.0)
+    end = MOST_KEYS - (MOST_KEYS - 1) // page * page                  # tokens of the last page
+    mean = ((last - 1) * vr[page:].sum(0) + vr[page:page + end].sum(0)) / ((last - 1) * page + end)
+    size = vs[page:].max(0)                                           # a value is 8 of it at most, and 280 in the sum of code + 128
+    # the others: 2^31 of e^-40 by the last pages' 25000
+    others = 2.0 ** 31 * np.exp(-40.0) / (last * page) * 2 * np.abs(vr).max()
+    close(y.double().cpu().numpy()[0], mean, (plain.HALF[t] + 8 * U) * 8 * size + (last * page / 8 + 8) * 2 * U * OFFSET[t] * size +
+          1.01 * plain.HALF[t] * np.abs(mean) + others)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_attn_of_as_many_keys_as_there_may_be(causal):
+    import torch
+    dim, t = 8, "bf16"
+    rng = np.random.Generator(np.random.PCG64(32))
+    k = torch.zeros(MOST_KEYS, 1, dim, dtype=torch.bfloat16, device="cuda:0")   # and the values
+    tail = 1 + reals(torch, rng, 5, 1, dim, t=t, scale=0.125)
+    k[-5:] = tail.cuda()
+    q = 5 + reals(torch, rng, 2, 3, dim, t=t, scale=0.125)
+    y = torch.zeros_like(q, device="cuda:0")
+    run_attn(torch, q.cuda(), k, k, [0, 2], [0, MOST_KEYS], causal, t, y, scale=1.0)
+    del k
+    got = y.double().cpu().numpy()
+    for i in range(2):
+        seen = tail[:4 + i if causal else 5].double().numpy()
+        want, rest, size, most = plain.attention(q[i:i + 1].double().numpy(), seen, seen, 1.0, False)
+        others = 2.0 ** 31 * np.exp(-(q[i].double().numpy() @ seen[:, 0].T).max())   # their share of the weight, and no value
+        close(got[i], want[0], (dim / 8 + 2) * 2 * U * most[0][:, None] * rest[0] + (plain.HALF[t] + 24 * U + others) * size[0] + 1.01 * plain.HALF[t] * np.abs(want[0]))
