@@ -18,7 +18,8 @@
 // end (3 us) are as long as 10 of its steps. 64 rows a wave do not fit the registers.
 //
 // The weights of hidden keys are 0, but 0 times an infinity or a NaN is not: rows whose result is no number are done
-// again one by one with nothing hidden in their sums.
+// again one by one with nothing hidden in their sums. So are those whose sums pass the largest number, or, of split keys, 2^100, as up to
+// 128 parts are added.
 
 #include <algorithm>
 
@@ -359,13 +360,13 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
         arrive(tile, (tile + 2) % S::RING, (tile + 3) % S::RING);
 
     total += __shfl_xor(total, 32);
-    float check = total;
+    uint32_t largest = __float_as_uint(total);   // magnitude; infinity and NaN are above all numbers
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-            check += o[c][e] * 0.f;   // NaN from an infinity or a NaN
-    const bool number = check < INFINITY;
+            largest = max(largest, __float_as_uint(o[c][e]) & 0x7FFFFFFFu);
+    const bool number = largest < __float_as_uint(parts > 1 ? 0x1p100f : INFINITY);
     const float inverse = parts > 1 ? 1.f : total != 0.f ? 1.f / total : 0.f;
     const long long all = (long long)A.queries * A.q_heads;
     int row = wave_row + r;

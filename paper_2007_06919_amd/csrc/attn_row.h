@@ -14,8 +14,8 @@ struct RowScratch {
 };
 
 // query(c), key(j, c), value(j, c): element c of the query, and of key and value j; keys first .. end - 1 are seen.
-// out(c, sum, reference, total): sums of weights 2^(score - reference) and of their products. Lanes of a wave in step; the scratch
-// is the wave's own.
+// out(c, sum, reference, total): sums of weights 2^(score - reference) and of their products. Weights are at most 2^-32, so that 2^31 of them
+// times fp32's largest values are a number. Lanes of a wave in step; the scratch is the wave's own.
 template <int DIM, typename Query, typename Key, typename Value, typename Out>
 __device__ __forceinline__ void row_attention(RowScratch &lds, int dim, int first, int end, float scale, Query query, Key key, Value value, Out out)
 {
@@ -25,6 +25,7 @@ __device__ __forceinline__ void row_attention(RowScratch &lds, int dim, int firs
     for (int c = lane; c < dim; c += 64)
         lds.q[c] = query(c) * scale;
     __builtin_amdgcn_wave_barrier();
+    constexpr float LOW = 32.f;
     float y[V] = {}, most = -INFINITY, total = 0.f;
     for (int t = first; t < end; t += 64) {
         const int j = t + lane;
@@ -40,7 +41,7 @@ __device__ __forceinline__ void row_attention(RowScratch &lds, int dim, int firs
             top = fmaxf(top, __shfl_xor(top, d));
         // -infinity while no score is above it: weights 0 until then (an infinite or NaN score gives NaN below)
         const float next = fmaxf(most, top), base = next == -INFINITY ? 0.f : next;
-        const float fade = exp2_fast(most - base), p = j < end ? exp2_fast(s - base) : 0.f;
+        const float fade = exp2_fast(most - base), p = j < end ? exp2_fast(s - base - LOW) : 0.f;
         float sum = p;
         for (int d = 32; d; d >>= 1)
             sum += __shfl_xor(sum, d);
@@ -64,7 +65,7 @@ __device__ __forceinline__ void row_attention(RowScratch &lds, int dim, int firs
 #pragma unroll
     for (int v = 0; v < V; ++v)
         if (lane + 64 * v < dim)
-            out(lane + 64 * v, y[v], most, total);
+            out(lane + 64 * v, y[v], most + LOW, total);
 }
 
 }  // namespace

@@ -5,7 +5,7 @@ import pytest
 
 import attention_plain as plain
 from paper_2007_06919_amd import aqd
-from test_gpu_attention import OFFSET, U, Sequences, check_attention, close, reals, run_attn, run_qattn, strides
+from test_gpu_attention import OFFSET, U, check_attention, close, reals, run_attn, run_qattn
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +57,25 @@ def test_attn_of_as_many_keys_as_there_may_be(causal):
         want, rest, size, most = plain.attention(q[i:i + 1].double().numpy(), seen, seen, 1.0, False)
         others = 2.0 ** 31 * np.exp(-(q[i].double().numpy() @ seen[:, 0].T).max())   # their share of the weight, and no value
         close(got[i], want[0], (dim / 8 + 2) * 2 * U * most[0][:, None] * rest[0] + (plain.HALF[t] + 24 * U + others) * size[0] + 1.01 * plain.HALF[t] * np.abs(want[0]))
+
+
+@pytest.mark.parametrize("dim, heads, per, nq, nk", [(128, 1, 2, [3, 70], [900, 70]), (64, 2, 1, [1], [3000]), (256, 1, 1, [40], [40]), (72, 1, 3, [5], [2500])])
+@pytest.mark.parametrize("size", [1e34, 7e37])
+def test_attn_of_values_next_to_the_largest(size, dim, heads, per, nq, nk):
+    import torch
+    t = "bf16"
+    rng = np.random.Generator(np.random.PCG64(34 + dim))
+    qs, ks = [0] + list(np.cumsum(nq)), [0] + list(np.cumsum(nk))
+    q, k = reals(torch, rng, qs[-1], heads * per, dim, t=t), reals(torch, rng, ks[-1], heads, dim, t=t)
+    v = torch.from_numpy(rng.uniform(-4.5, 4.5, (ks[-1], heads, dim)) * size)
+    v[..., 0] = 4.5 * size
+    v[..., 32:] = torch.from_numpy(rng.standard_normal(v[..., 32:].shape))
+    v = v.bfloat16()
+    for workspace in (aqd.ATTN_WORKSPACE_BYTES, 0):
+        for causal in (True, False):
+            y = torch.zeros_like(q, device="cuda:0")
+            run_attn(torch, q.cuda(), k.cuda(), v.cuda(), qs, ks, causal, t, y, workspace)
+            got = y.double().cpu().numpy()
+            for b in range(len(nq)):
+                a, z = slice(qs[b], qs[b + 1]), slice(ks[b], ks[b + 1])
+                check_attention(got[a], q[a].double().numpy(), k[z].double().numpy(), v[z].double().numpy(), dim ** -0.5, causal, t, name=f"sequence {b}")
