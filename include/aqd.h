@@ -469,7 +469,8 @@ aqd_status_t qcache_read(const qcache_rows_desc_t *desc, const void *cache, cons
  *   y = sum over those of softmax(scale * q . k) v
  * for query head h with key head h / (q_heads / heads). A query that sees no token (an empty sequence) has zeros. Rows of
  * q outside of every sequence are left as they were. fp32 scores and sums; the weights times the values' scales are rounded to
- * `type` for the matrix product: each term within half a unit of its last place (fp16: or 2^-24 of the row's largest).
+ * `type` for the matrix product: each term within half a unit of its last place (fp16: or 2^-24 of the row's largest; bf16: where the cache
+ * holds values of 2^90 and more, those below 2^-75 may count as 0).
  * max_queries and max_keys bound the sequences' queries and lengths, which sizes the launch; of a longer sequence
  * the first max_queries queries and max_keys tokens count (and no more than ld_table pages). Queries that see a token whose page
  * number is outside of 0 .. pages - 1 are NaN. What lies in a page past a sequence's end does not matter. No row of q may be

@@ -293,14 +293,18 @@ __global__ void __launch_bounds__(256, DIM == 256 ? (GROUP == 32 ? 1 : 2) : 3) q
 
     f32x4 o[R][TILES];
     float ref[R], total[R];
+    auto clear = [&] {
 #pragma unroll
-    for (int k = 0; k < R; ++k) {
-        ref[k] = -INFINITY;
-        total[k] = 0.f;
+        for (int k = 0; k < R; ++k) {
+            ref[k] = -INFINITY;
+            total[k] = 0.f;
 #pragma unroll
-        for (int i = 0; i < TILES; ++i)
-            o[k][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+            for (int i = 0; i < TILES; ++i)
+                o[k][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    };
+    clear();
+    float low = 0.f;   // by which the reference is above the largest score
 
     int at = 0;
     for (int t = t_first; t < end; t += 128) {
@@ -421,10 +425,10 @@ __global__ void __launch_bounds__(256, DIM == 256 ? (GROUP == 32 ? 1 : 2) : 3) q
                 top *= scale;
             }
             // weights up to 2^8 are as good as up to 1: the reference moves seldom
-            if (__builtin_amdgcn_ballot_w64(top > ref[k] + 8.f)) {
+            if (__builtin_amdgcn_ballot_w64(top > ref[k] + (8.f - low))) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
-                const float next = fmaxf(ref[k], top), fade = next == -INFINITY ? 1.f : exp2_fast(ref[k] - next);
+                const float next = fmaxf(ref[k], top + low), fade = next == -INFINITY ? 1.f : exp2_fast(ref[k] - next);
                 ref[k] = next;
                 total[k] *= fade;
 #pragma unroll
@@ -470,6 +474,30 @@ __global__ void __launch_bounds__(256, DIM == 256 ? (GROUP == 32 ? 1 : 2) : 3) q
                 }
             });
         });
+        // bf16: sums of weights up to 2^8 by codes and offsets up to 2^8 can pass the largest number where their values and the result do not
+        // (or do so where waves and parts are added). Then once more, with weights up to 2^-40.
+        if constexpr (!Code<T>::NARROW)
+            if (t + 128 >= end && low == 0.f) {
+                uint32_t largest = 0;   // magnitude; infinity and NaN are above all numbers
+#pragma unroll
+                for (int k = 0; k < R; ++k)
+#pragma unroll
+                    for (int i = 0; i < TILES; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            largest = max(largest, __float_as_uint(o[k][i][e]) & 0x7FFFFFFFu);
+                if (__builtin_amdgcn_ballot_w64(largest >= __float_as_uint(0x1p100f))) {
+                    low = 48.f;
+                    clear();
+                    at = 0;
+                    bads = 0;
+#pragma nounroll
+                    for (int i = 0; i < S::RING; ++i)
+                        if (t_first + 128 * i < end)
+                            bads |= copy(t_first + 128 * i, i) << (2 * i);
+                    t = t_first - 128;
+                }
+            }
     }
 
     // join the waves, 16 rows at a time: [row][DIM] sums, then references and totals

@@ -5,7 +5,7 @@ import pytest
 
 import attention_plain as plain
 from paper_2007_06919_amd import aqd
-from test_gpu_attention import OFFSET, U, check_attention, close, reals, run_attn, run_qattn
+from test_gpu_attention import OFFSET, U, Sequences, check_attention, close, reals, run_attn, run_qattn
 
 pytestmark = pytest.mark.gpu
 
@@ -79,3 +79,30 @@ def test_attn_of_values_next_to_the_largest(size, dim, heads, per, nq, nk):
             for b in range(len(nq)):
                 a, z = slice(qs[b], qs[b + 1]), slice(ks[b], ks[b + 1])
                 check_attention(got[a], q[a].double().numpy(), k[z].double().numpy(), v[z].double().numpy(), dim ** -0.5, causal, t, name=f"sequence {b}")
+
+
+@pytest.mark.parametrize("heads, dim, group, per, lengths, counts", [
+    (2, 128, 32, 4, [500, 3], [1, 1]), (1, 64, 64, 3, [9000], [1]), (1, 64, 32, 8, [700, 40], [9, 5]), (1, 256, 32, 2, [300], [20]), (2, 256, 128, 1, [90], [1]),
+    (1, 128, 64, 16, [40] * 9 + [5000], [1] * 10),
+])
+@pytest.mark.parametrize("size", [1e29, 1e33, 7e37])
+def test_qattn_of_values_next_to_the_largest(size, heads, dim, group, per, lengths, counts):
+    """A result is never larger than its values, whatever the sums before the division by the weights. The last group has values
+    of ordinary size."""
+    import torch
+    page, t = 16, "bf16"
+    s = Sequences(torch, 33, lengths, heads, dim, group, page)
+    for b, v in enumerate(s.v):
+        big = s.rng.uniform(-4.5, 4.5, v.shape) * size
+        if dim > group:
+            big[..., -group:] = s.rng.standard_normal(big[..., -group:].shape)
+        big[len(big) // 2:, ..., 0] = 4.5 * size                      # all of one sign
+        plain.write(s.cache, s.slots(b), s.k[b].astype(np.float32), big.astype(np.float32), *s.shape)
+        s.k[b], s.v[b], s.ks[b], s.vs[b] = plain.read(s.cache, s.slots(b), *s.shape)
+    start = [0] + list(np.cumsum(counts))
+    q = reals(torch, s.rng, start[-1], heads * per, dim, t=t)
+    cache, tables = torch.from_numpy(s.cache).cuda(), torch.from_numpy(s.tables).cuda()
+    for workspace in (aqd.ATTN_WORKSPACE_BYTES, 0):
+        y = torch.zeros_like(q, device="cuda:0")
+        run_qattn(torch, s.c, cache, tables, lengths, q.cuda(), start, max(counts), t, y, workspace)
+        s.check(y.double().cpu().numpy(), q, start, t)
