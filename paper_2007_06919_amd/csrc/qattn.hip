@@ -404,8 +404,9 @@ __global__ void __launch_bounds__(256, DIM == 256 ? (GROUP == 32 ? 1 : 2) : 3) q
                         top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, __builtin_bit_cast(u16x2, top)));
                     }
                     const float low = (float)(top >> 8 & 255u), high = (float)(top >> 24), e = G == 1 ? (i & 1 ? high : low) : fmaxf(low, high);
-                    // (weights of values that T rounds to 0 need not be near 1, and their sum has to stay a number)
-                    size[4 * half + i] = __builtin_amdgcn_fmed3f(e - 128.f, -40.f, 100.f);
+                    // (weights of values that T rounds to 0 need not be near 1, and their sum has to stay a number; scales that qcache_write makes
+                    // are below 2^126, and a weight of 2^-127 would be 0)
+                    size[4 * half + i] = __builtin_amdgcn_fmed3f(e - 128.f, -40.f, 125.f);
                 }
         }
 #pragma unroll

@@ -106,3 +106,30 @@ def test_qattn_of_values_next_to_the_largest(size, heads, dim, group, per, lengt
         y = torch.zeros_like(q, device="cuda:0")
         run_qattn(torch, s.c, cache, tables, lengths, q.cuda(), start, max(counts), t, y, workspace)
         s.check(y.double().cpu().numpy(), q, start, t)
+
+
+@pytest.mark.parametrize("count", [1, 20])
+def test_qattn_of_large_values_with_hardly_any_weight_fp16(count):
+    """Two tokens: 2.9e38 with the weight e^-80, and next to nothing with the rest. What is left of the first is a number in fp16. (Products of a weight
+    and a scale: within half a step, or 2^-24 of the row's largest, times a code.)"""
+    import torch
+    dim, page, t = 64, 16, "f16"
+    c = aqd.QcacheDesc(1, dim, 32, page, 2)
+    n = count + 1
+    k, v = np.zeros((n, 1, dim), np.float32), np.full((n, 1, dim), 1e-20, np.float32)
+    k[1:, :, :32] = 2.5
+    v[0] = 2.9e38 * np.linspace(0.5, 1, dim)
+    cache = np.zeros((2, 1, plain.block_bytes(dim, 32, page)), np.uint8)
+    plain.write(cache, np.arange(n), k, v, 1, dim, 32, page)
+    kr, vr, ks, vs = plain.read(cache, np.arange(n), 1, dim, 32, page)
+    q = torch.ones(count, 1, dim).half()
+    y = torch.zeros_like(q, device="cuda:0")
+    run_qattn(torch, c, torch.from_numpy(cache).cuda(), torch.arange(2, dtype=torch.int32, device="cuda:0").view(1, 2), [n], q.cuda(), [0, count], count, t, y,
+              scale=1.0)
+    got = y.double().cpu().numpy()
+    for i in range(count):
+        m, one = i + 2, q[i:i + 1].double().numpy()
+        want, rest, size, most = plain.attention(one, kr[:m], vr[:m], 1.0, False, OFFSET[t] * ks[:m], OFFSET[t] * vs[:m])
+        weights = plain.attention(one, kr[:m], vr[:m], 1.0, False)[2]
+        close(got[i:i + 1], want, (dim / 8 + 2) * 2 * U * most[..., None] * rest + (plain.HALF[t] + 8 * U) * weights + (m / 8 + 8) * 2 * U * size +
+              1.01 * plain.HALF[t] * np.abs(want) + plain.LEAST[t] + m * 2.0 ** -24 * weights.max() * 8)
