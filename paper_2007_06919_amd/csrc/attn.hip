@@ -201,8 +201,8 @@ __global__ void __launch_bounds__(256, DIM == 64 ? 3 : DIM == 128 ? 2 : 1) attn_
                 q[u][e] = w[e] ^ flip;
         }
     }
-    // (a scale of 0 would make -infinity * 0 of hidden scores)
-    const float scale = fmaxf(fabsf(A.scale) * LOG2E, 0x1p-100f);
+    // (a scale of 0 would make -infinity * 0 of hidden scores; the least number above it leaves every finite score below 2^-20)
+    const float scale = fmaxf(fabsf(A.scale) * LOG2E, 0x1p-149f);
 
     f32x16 o[C], s[2];   // sums, and the scores of this step and the next
     u32x4 p[2];          // the last step's weights

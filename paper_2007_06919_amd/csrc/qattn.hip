@@ -267,8 +267,8 @@ __global__ void __launch_bounds__(256, DIM == 256 ? (GROUP == 32 ? 1 : 2) : 3) q
         }
     }
     const int seen_least = seq.length - seq.n + 1 + first_row / per;
-    // (a scale of 0 would make -infinity * 0 of hidden scores)
-    const float scale = fmaxf(fabsf(A.scale) * LOG2E, 0x1p-100f);
+    // (a scale of 0 would make -infinity * 0 of hidden scores; the least number above it leaves every finite score below 2^-20)
+    const float scale = fmaxf(fabsf(A.scale) * LOG2E, 0x1p-149f);
     uint32_t mask = Code<T>::MASK, base = Code<T>::BASE;
     asm("" : "+s"(mask));
     asm("" : "+v"(base));

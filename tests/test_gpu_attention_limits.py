@@ -5,7 +5,7 @@ import pytest
 
 import attention_plain as plain
 from paper_2007_06919_amd import aqd
-from test_gpu_attention import OFFSET, U, Sequences, check_attention, close, reals, run_attn, run_qattn
+from test_gpu_attention import OFFSET, U, Sequences, check_attention, close, reals, run_attn, run_qattn, strides
 
 pytestmark = pytest.mark.gpu
 
@@ -133,3 +133,29 @@ def test_qattn_of_large_values_with_hardly_any_weight_fp16(count):
         weights = plain.attention(one, kr[:m], vr[:m], 1.0, False)[2]
         close(got[i:i + 1], want, (dim / 8 + 2) * 2 * U * most[..., None] * rest + (plain.HALF[t] + 8 * U) * weights + (m / 8 + 8) * 2 * U * size +
               1.01 * plain.HALF[t] * np.abs(want) + plain.LEAST[t] + m * 2.0 ** -24 * weights.max() * 8)
+
+
+@pytest.mark.parametrize("scale", [0.0, 1e-32, -1e-32, 1e-39])
+def test_small_scales_of_large_scores(scale):
+    """Products of queries and keys of about 2^106: a scale of 0 makes every weight the same, smaller ones than 2^-100 count as they are."""
+    import torch
+    dim, page, t = 64, 16, "bf16"
+    rng = np.random.Generator(np.random.PCG64(35))
+    big = 2.0 ** 52
+    q, k = [reals(torch, rng, n, h, dim, t=t, scale=big) for n, h in ((20, 4), (90, 2))]
+    v = reals(torch, rng, 90, 2, dim, t=t)
+    n64 = [x.double().numpy() for x in (q, k, v)]
+    c = aqd.QcacheDesc(2, dim, 32, page, 6)
+    cache = torch.zeros(aqd.qcache_bytes(c), dtype=torch.uint8, device="cuda:0")
+    slots = torch.arange(90, dtype=torch.int32, device="cuda:0")
+    kd, vd = k.cuda(), v.cuda()
+    aqd.qcache_write(c, 90, aqd.BF16, kd, *strides(kd), vd, *strides(vd), slots, cache)
+    kr, vr, ks, vs = plain.read(cache.cpu().numpy().reshape(6, 2, -1), np.arange(90), 2, dim, 32, page)
+    y = torch.zeros_like(q, device="cuda:0")
+    for causal in (True, False):
+        run_attn(torch, q.cuda(), kd, vd, [0, 20], [0, 90], causal, t, y, scale=scale)
+        check_attention(y.double().cpu().numpy(), *n64, scale, causal, t, name=f"prompt {causal}")
+    for count in (20, 1):
+        some = q[:count].cuda()
+        run_qattn(torch, c, cache, slots[:6].view(1, 6), [90], some, [0, count], count, t, y[:count], scale=scale)
+        check_attention(y[:count].double().cpu().numpy(), n64[0][:count], kr, vr, scale, True, t, OFFSET[t] * ks, OFFSET[t] * vs, name=f"cache {count}")
