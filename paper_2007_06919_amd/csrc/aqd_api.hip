@@ -11,6 +11,7 @@
 #include <cstring>
 #include <mutex>
 #include <new>
+#include <numeric>
 #include <string>
 #include <vector>
 
@@ -1776,14 +1777,20 @@ Span span(const void *p, long long rows, long long ld, long long cols, int size)
     return {(uintptr_t)p, ld * size, cols * size, rows};
 }
 
-// whether two matrices may share a byte: their address ranges meet, unless they are
-// disjoint column ranges of rows of one stride
-bool share(const Span &a, const Span &b)
+// whether the address ranges of two matrices meet
+bool ranges_meet(const Span &a, const Span &b)
 {
     if (!a.at || !b.at || !a.rows || !b.rows)
         return false;
     const uintptr_t ea = a.at + (uintptr_t)((a.rows - 1) * a.ld + a.width), eb = b.at + (uintptr_t)((b.rows - 1) * b.ld + b.width);
-    if (a.at >= eb || b.at >= ea)
+    return a.at < eb && b.at < ea;
+}
+
+// whether two matrices may share a byte: their address ranges meet, unless they are
+// disjoint column ranges of rows of one stride
+bool share(const Span &a, const Span &b)
+{
+    if (!ranges_meet(a, b))
         return false;
     if (a.ld != b.ld)
         return true;
@@ -1959,6 +1966,7 @@ namespace {
 struct Rows3 {
     Span outer;
     long long step, width;   // of the smaller stride, and of dim elements, bytes
+    long long count;         // of the smaller stride's dimension
 };
 
 // Strides of a dimension with one entry are ignored (and set to what a packed tensor has); false for strides by which two
@@ -1983,19 +1991,38 @@ Rows3 rows3(const void *p, long long token, long long head, long long tokens, lo
 {
     const bool by_token = token >= head;
     const long long inner = by_token ? head : token, outer = by_token ? token : head, n = by_token ? heads : tokens;
-    return {{(uintptr_t)p, outer * size, ((n - 1) * inner + dim) * size, by_token ? tokens : heads}, inner * size, dim * size};
+    return {{(uintptr_t)p, outer * size, ((n - 1) * inner + dim) * size, by_token ? tokens : heads}, inner * size, dim * size, n};
 }
 
+// whether a row of a and one of b that begins `gap` bytes behind it share a byte (rows of unlike steps: whether they may)
+bool rows_meet(const Rows3 &a, const Rows3 &b, long long gap)
+{
+    if (gap >= a.outer.width || -gap >= b.outer.width)
+        return false;
+    if (a.count == 1 && b.count == 1)
+        return true;
+    const long long step = a.count == 1 ? b.step : b.count == 1 ? a.step : std::gcd(a.step, b.step);
+    const long long phase = (gap % step + step) % step;   // of b's elements behind a's, within a step
+    return phase < a.width || phase + b.width > step;
+}
+
+// rows of unlike strides are taken to share a byte where their ranges meet
 bool share(const Rows3 &a, const Rows3 &b)
 {
-    if (!share(a.outer, b.outer))
+    if (!ranges_meet(a.outer, b.outer))
         return false;
-    // rows of one make whose heads (or tokens) lie between one another
-    if (a.step != b.step || a.outer.ld != b.outer.ld || a.outer.ld % a.step)
+    if (a.outer.rows > 1 && b.outer.rows > 1 && a.outer.ld != b.outer.ld)
         return true;
-    const uintptr_t step = (uintptr_t)a.step, x = a.outer.at, y = b.outer.at;
-    const long long gap = (long long)(y >= x ? (y - x) % step : (step - (x - y) % step) % step);   // b's first element, within a step of a
-    return gap < a.width || gap + b.width > a.step;
+    // rows i of a and i + k of b, as far as they are near enough
+    const long long ld = a.outer.rows > 1 ? a.outer.ld : b.outer.ld, gap = (long long)(b.outer.at - a.outer.at);
+    long long k = std::max(1 - a.outer.rows, (1 - b.outer.width - gap) / ld - 1);
+    const long long last = std::min(b.outer.rows - 1, (a.outer.width - 1 - gap) / ld + 1);
+    if (last - k > 64)
+        return true;
+    for (; k <= last; ++k)
+        if (rows_meet(a, b, gap + k * ld))
+            return true;
+    return false;
 }
 
 bool share(const Rows3 &a, const Span &b) { return share(a.outer, b); }
