@@ -398,7 +398,7 @@ aqd_status_t qlin_run(const qlin_desc_t *desc, const int8_t *x, const float *x_s
  * and values are tensors [tokens][heads][dim] of a real type whose channels are contiguous; each has a
  * token stride and a head stride in elements, so they may be slices of one joint projection's rows, or
  * [heads][tokens][dim]. Of the two strides the smaller is at least dim, and the larger at least what
- * the other dimension spans (a stride is ignored where its dimension has one entry): no element twice.
+ * the other dimension spans (a stride is ignored where its dimension has one entry, both are where there are no tokens): no element twice.
  * Pointers need the alignment of their elements only. What lies between rows is never written. An output must share no
  * element with an input or another output, but for aqd_heads_run's. A count of 0 (tokens, queries,
  * batch) is a no-op. The calls allocate nothing and may be recorded into a graph; device

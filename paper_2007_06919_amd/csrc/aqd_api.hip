@@ -1969,12 +1969,12 @@ struct Rows3 {
     long long count;         // of the smaller stride's dimension
 };
 
-// Strides of a dimension with one entry are ignored (and set to what a packed tensor has); false for strides by which two
+// Strides of a dimension with one entry, and of tensors without tokens, are ignored (and set to what a packed tensor has); false for strides by which two
 // elements could be one, or the tensor leave the address space.
 bool strides_ok(long long &token, long long &head, long long tokens, long long heads, long long dim)
 {
     const auto fits = [](long long stride, long long count) { return stride <= (INT64_C(1) << 56) / std::max(count, 1LL); };
-    if (heads <= 1)
+    if (heads <= 1 || !tokens)
         head = dim;
     if (!fits(head, heads))
         return false;

@@ -11,9 +11,9 @@ NO_GPU = pytest.mark.skipif(torch.cuda.device_count() > 0, reason="addresses of 
 AT = 1 << 40
 
 
-def status(call, *args):
+def status(call, *args, **kw):
     try:
-        call(*args)
+        call(*args, **kw)
     except aqd.AqdError as e:
         return e.status
     return aqd.AQD_OK
@@ -88,3 +88,16 @@ def test_tensors_that_meet_are_refused_and_others_are_not():
             assert taken(got), what
             free += 1
     assert met > 500 and free > 500
+
+
+@NO_GPU
+@pytest.mark.parametrize("token, head", [(0, 0), (1, 1), (-5, 1 << 62)])
+def test_tensors_without_tokens_have_no_strides(token, head):
+    """As torch's of an empty numpy array, whose strides are 0."""
+    c, none = aqd.QcacheDesc(2, 64, 32, 16, 4), (None, token, head)
+    for batch in (0, 1):
+        assert status(aqd.attn_run, batch, 4, 2, 64, 0, 10, 0, 10, True, aqd.BF16, 0.1, *none, AT, 128, 64, AT, 128, 64, AT, AT, *none, stream=0) == aqd.AQD_OK
+        assert status(aqd.qattn_run, c, batch, 4, 0, 0, 10, aqd.BF16, 0.1, *none, AT, AT, AT, 1, AT, *none, stream=0) == aqd.AQD_OK
+    # queries without a key have zeros
+    q, y, start = AT, 2 * AT, 3 * AT
+    assert taken(status(aqd.attn_run, 1, 4, 2, 64, 2, 0, 2, 0, True, aqd.BF16, 0.1, q, 256, 64, *none, *none, start, start, y, 256, 64, stream=0))
