@@ -2137,8 +2137,8 @@ aqd_status_t attn_args(const aqd_attn_desc_t *d, AttnArgs &a)
     REQUIRE(strides_ok(a.q_token, a.q_head, a.queries, a.q_heads, a.dim) && strides_ok(a.k_token, a.k_head, a.keys, a.heads, a.dim) &&
                 strides_ok(a.v_token, a.v_head, a.keys, a.heads, a.dim) && strides_ok(a.y_token, a.y_head, a.queries, a.q_heads, a.dim),
             "strides by which elements could share memory, or too large");
-    // offsets of the 32 rows of a tile are 32-bit numbers
-    if (a.k_token > 1 << 26 || a.v_token > 1 << 26)
+    // offsets of the 32 rows of a tile are 32-bit numbers (one row has none, whatever its stride)
+    if (a.keys > 1 && (a.k_token > 1 << 26 || a.v_token > 1 << 26))
         return fail(AQD_ERR_UNSUPPORTED, "token strides of k and v must be at most 2^26");
     return AQD_OK;
 }

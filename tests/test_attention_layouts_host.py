@@ -1,5 +1,6 @@
 """Layouts of heads and tokens that the attention calls take or refuse: the checks come from the host before any launch. What they take is
 launched, so where there is a GPU, calls with addresses of nothing are left out (test_gpu_attention_layouts.py has them with memory)."""
+import ctypes
 import random
 
 import pytest
@@ -101,3 +102,20 @@ def test_tensors_without_tokens_have_no_strides(token, head):
     # queries without a key have zeros
     q, y, start = AT, 2 * AT, 3 * AT
     assert taken(status(aqd.attn_run, 1, 4, 2, 64, 2, 0, 2, 0, True, aqd.BF16, 0.1, q, 256, 64, *none, *none, start, start, y, 256, 64, stream=0))
+
+
+@pytest.mark.parametrize("keys", [0, 1, 2, 3])
+def test_few_keys_of_a_large_buffer(keys):
+    """[heads][131072 tokens][128] with hardly any token in it: the heads are far apart, the tokens are not."""
+    token, head = 128, 131072 * 128
+    d = aqd.AttnDesc(1, 8, 8, 128, 1, keys, 1, keys, 1, aqd.BF16, 0.1, 8 * 128, 128, token, head, token, head, 8 * 128, 128)
+    size = ctypes.c_size_t(7)
+    assert aqd.lib().aqd_attn_workspace(ctypes.byref(d), ctypes.byref(size)) == aqd.AQD_OK and size.value == 0
+
+
+@pytest.mark.parametrize("keys", [0, 1])
+def test_a_single_key_has_no_token_stride(keys):
+    for token in (0, -1, 1, (1 << 26) + 1, 1 << 60):
+        d = aqd.AttnDesc(1, 8, 8, 128, 1, keys, 1, keys, 1, aqd.BF16, 0.1, 8 * 128, 128, token, 1 << 27, token, 128, 8 * 128, 128)
+        size = ctypes.c_size_t(7)
+        assert aqd.lib().aqd_attn_workspace(ctypes.byref(d), ctypes.byref(size)) == aqd.AQD_OK and size.value == 0

@@ -56,3 +56,21 @@ def test_heads_that_alternate(heads, dim, tokens, pad, t):
         aqd.qcache_read(c, tokens, TYPES[t], caches[0], position, a, *strides(a), b, *strides(b))
     assert torch.equal(k, packed[1]) and torch.equal(v, packed[2])
     unchanged([1, 2])
+
+
+@pytest.mark.parametrize("t, dim", [("bf16", 128), ("f16", 64), ("bf16", 200)])
+def test_first_tokens_of_a_large_buffer(t, dim):
+    """Keys and values [heads][tokens][dim] with room for so many that the heads are more than 2^26 elements apart, and none, one and two tokens in
+    it."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(dim))
+    heads, room = 3, -(-((1 << 26) + 4096) // dim)
+    k, v = [torch.full((heads, room, dim), float("nan"), dtype=DTYPE[t], device="cuda:0") for _ in range(2)]
+    for n in (0, 1, 2):
+        q, a, b = [torch.from_numpy(rng.standard_normal((m, h, dim))).to(DTYPE[t]).cuda() for m, h in ((2, 6), (n, heads), (n, heads))]
+        k[:, :n], v[:, :n] = a.transpose(0, 1), b.transpose(0, 1)
+        want, y = torch.full_like(q, 7), torch.full_like(q, 7)
+        for causal in (True, False):
+            run_attn(torch, q, a, b, [0, 2], [0, n], causal, t, want)
+            run_attn(torch, q, k[:, :n].transpose(0, 1), v[:, :n].transpose(0, 1), [0, 2], [0, n], causal, t, y)
+            assert torch.equal(y, want), (n, causal)
