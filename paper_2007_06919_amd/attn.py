@@ -88,9 +88,19 @@ class PagedCache:
         self.free += reversed(self.pages_of.pop(i))
         del self.lengths[i]
 
+    def shorten(self, i, length):
+        """Takes a sequence's tokens from `length` on back (drafts that were refused, a step whose pass failed), and the pages that only
+        they had. Steps of those tokens have no more passes; as for `remove`, passes that read their pages have ended."""
+        if not 0 <= length <= self.lengths[i]:
+            raise ValueError(f"a sequence of {self.lengths[i]} tokens cannot be shortened to {length}")
+        pages, keep = self.pages_of[i], -(-length // self.page)
+        self.free += reversed(pages[keep:])
+        del pages[keep:]
+        self.lengths[i] = length
+
     def step(self, ids, counts):
         """A Step of counts[j] new tokens of sequence ids[j]; takes the pages that they need. The tokens belong to their sequences from
-        now on: every layer's pass of this step comes before the next step's."""
+        now on (until `shorten` takes them back): every layer's pass of this step comes before the next step's."""
         ids, counts = list(ids), [int(n) for n in counts]
         if len(ids) != len(counts) or len(set(ids)) != len(ids) or any(i not in self.lengths for i in ids):
             raise ValueError("a step names sequences of the cache, each once, and a count for each")

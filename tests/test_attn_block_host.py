@@ -178,3 +178,45 @@ def test_a_step_that_fails_leaves_its_pages_for_the_next(calls, monkeypatch):
         c.step([a, b], [1, 32])
     step = c.step([a, b], [30, 16])
     assert step.rows == 46 and not c.free
+
+
+def test_tokens_are_taken_back(calls):
+    """Drafts that were refused, and a step whose pass failed: the sequence is what it was before them."""
+    c = cache(6)
+    a, b = c.add(), c.add()
+    c.step([a, b], [20, 3])
+    kept = list(c.pages_of[a])
+    c.step([a], [40])                                    # four pages, where two are kept
+    assert len(c.pages_of[a]) == 4 and len(c.free) == 1
+    c.shorten(a, 22)
+    assert c.lengths == {a: 22, b: 3} and c.pages_of[a] == kept and len(c.free) == 3
+    step = c.step([a], [1])
+    assert step.position.tolist() == [22] and step.slots.tolist() == [kept[1] * PAGE + 6] and step.lengths.tolist() == [23]
+    c.shorten(a, 23)
+    c.shorten(a, 16)                                     # a page's end
+    assert c.pages_of[a] == kept[:1]
+    c.shorten(a, 0)
+    assert c.pages_of[a] == [] and c.step([a], [5]).prompts
+    assert sorted(c.free + c.pages_of[a] + c.pages_of[b]) == list(range(6))
+    for length in (-1, 6):
+        with pytest.raises(ValueError):
+            c.shorten(a, length)
+    c.remove(a)
+    with pytest.raises(KeyError):
+        c.shorten(a, 0)
+
+
+def test_a_step_whose_pass_fails_is_taken_back(calls):
+    c = cache()
+    block = attn.CachedAttention(c, max_rows=10, **weights())
+    a = c.add()
+    c.step([a], [9])
+    before = c.lengths[a]
+    step = c.step([a], [11])
+    with pytest.raises(ValueError):
+        block.forward(rows_of(11), None, rows_of(11), None, step)   # more rows than buffers
+    c.shorten(a, before)
+    for n in (6, 5):
+        step = c.step([a], [n])
+        block.forward(rows_of(n), None, rows_of(n), None, step)
+    assert step.position.tolist() == list(range(15, 20))

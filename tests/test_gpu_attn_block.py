@@ -184,3 +184,31 @@ def test_recorded_steps_of_one_token():
     finally:
         torch.cuda.synchronize()
         aqd.graph_destroy(graph)
+
+
+def test_refused_drafts_leave_nothing():
+    """Four drafts a step, of which some stay: the next step's rows have the bits that they have behind the accepted tokens alone."""
+    import torch
+    rng, w, weights, cache, block = make(torch, "bf16", seed=5)
+    _, _, _, plain_cache, plain_block = make(torch, "bf16", seed=5)
+    one, other = cache.add(), plain_cache.add()
+
+    def run(block, cache, sequence, x):
+        y = torch.empty_like(x)
+        block.forward(x, None, y, None, cache.step([sequence], [len(x)]))
+        torch.cuda.synchronize()
+        return y
+
+    x = w(30, HIDDEN, scale=1.0)
+    assert torch.equal(run(block, cache, one, x), run(plain_block, plain_cache, other, x))
+    for stay in (1, 3, 4, 0, 2):                           # 30 to 40 tokens: over a page's end and back
+        drafts, length = w(4, HIDDEN, scale=1.0), cache.lengths[one]
+        run(block, cache, one, drafts)
+        cache.shorten(one, length + stay)
+        if stay:
+            run(plain_block, plain_cache, other, drafts[:stay])
+        x = w(4, HIDDEN, scale=1.0)
+        got, want = run(block, cache, one, x), run(plain_block, plain_cache, other, x)
+        assert torch.equal(got, want), stay
+        cache.shorten(one, length + stay)
+        plain_cache.shorten(other, length + stay)
