@@ -22,7 +22,7 @@ from __future__ import annotations
 import sys
 
 from . import aqd
-from .ffn import DEVICE, _finish, _meet, quantize_rows
+from .ffn import DEVICE, _finish, _meet, _streams_of, quantize_rows
 
 
 class Step:
@@ -53,7 +53,7 @@ class Step:
 
         self.tensors = tuple(put(v) for v in (position, slots, start, after, tables))
         self.position, self.slots, self.start, self.lengths, self.tables = self.tensors
-        self.streams = {aqd._stream(None)}   # handles of those that torch keeps the tensors for
+        self.streams = _streams_of(cache.device)   # handles of those that torch keeps the tensors for
         _finish(cache.device)
 
 
@@ -164,7 +164,7 @@ class CachedAttention:
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
         self._buffers = (self.norm_weight, self.table, self.w1, self.s1, self.w2, self.s2, self.data, self.c1, self.q1, self.c2, self.q2,
                          self.qkv, self.h, self.workspace) + tuple(w for w in (self.q_norm, self.k_norm) if w is not None)
-        self._streams = {aqd._stream(None)}   # handles of those that torch keeps the buffers for
+        self._streams = _streams_of(dev)   # handles of those that torch keeps the buffers for
         _finish(dev)
 
     def forward(self, x, residual, y, total, step, stream=None):

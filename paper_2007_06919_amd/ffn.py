@@ -65,6 +65,13 @@ def _finish(device, all=False):
     torch.cuda.synchronize(device) if all else torch.cuda.current_stream(device).synchronize()
 
 
+def _streams_of(device):
+    """Handles of the streams for which torch keeps tensors that are made now on `device` anyway: its current one, where the device is the
+    current one too (the default streams of two devices have one handle)."""
+    import torch
+    return {aqd._stream(None)} if device.index is None or device.index == torch.cuda.current_device() else set()
+
+
 class GatedFfn:
     """norm_weight [hidden], gate and up [units][hidden], down [hidden][units]: device tensors of one real type, that of
     the block's inputs and outputs too. The set-up has ended on the GPU when the constructor returns, so passes may run on any
@@ -108,7 +115,7 @@ class GatedFfn:
         self._graph = self._recorded = None
         self._buffers = (self.norm_weight, self.w1, self.s1, self.w2, self.s2, self.c1, self.q1, self.h, self.c2, self.q2,
                          self.workspace)
-        self._streams = {aqd._stream(None)}   # handles of those that torch keeps the buffers for
+        self._streams = _streams_of(dev)   # handles of those that torch keeps the buffers for
         _finish(dev)
 
     def _use_on(self, stream):

@@ -220,3 +220,20 @@ def test_a_step_whose_pass_fails_is_taken_back(calls):
         step = c.step([a], [n])
         block.forward(rows_of(n), None, rows_of(n), None, step)
     assert step.position.tolist() == list(range(15, 20))
+
+
+def test_memory_of_another_device_is_kept_for_every_stream(calls, monkeypatch):
+    """Made while another device is the current one, whose default stream has the handle 0 too: the first pass on the memory's own device
+    has to be recorded."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    assert ffn._streams_of(torch.device("cuda", 0)) == set()
+    assert ffn._streams_of(torch.device("cuda", 1)) == {0} == ffn._streams_of(torch.device("cpu"))
+    made = []
+    monkeypatch.setattr(ffn, "_streams_of", lambda device: made.append(device) or set())
+    monkeypatch.setattr(attn, "_streams_of", ffn._streams_of)
+    c = cache()
+    block = attn.CachedAttention(c, max_rows=4, **weights())
+    step = c.step([c.add()], [1])
+    dense = torch.ones(HIDDEN, HIDDEN, dtype=torch.bfloat16)
+    other = ffn.GatedFfn(torch.ones(HIDDEN, dtype=torch.bfloat16), dense, dense, dense, max_rows=4)
+    assert block._streams == step.streams == other._streams == set() and made == [c.device] * 3
