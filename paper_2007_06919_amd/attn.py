@@ -8,7 +8,7 @@
     codes, scales        = qrows(h)
     y                    = qlin(codes)
 
-It takes and gives what the feed-forward block of ``ffn.py`` does, so the two make a layer. ``PagedCache`` keeps which
+In float16 and bfloat16 it takes and gives what the feed-forward block of ``ffn.py`` does, so the two make a layer. ``PagedCache`` keeps which
 pages a sequence has; one of its steps (``Step``) serves every layer that has a cache of its shape. PyTorch provides
 device memory and the stream; all arithmetic is in ``libaqd.so``.
 
@@ -121,7 +121,8 @@ class CachedAttention:
     """norm_weight [hidden], wq [q_heads * dim][hidden], wk and wv [heads * dim][hidden], wo [hidden][q_heads * dim], q_norm and
     k_norm [dim] or None: device tensors of one real type, float16 or bfloat16, that of the block's inputs and outputs too. table:
     cosines and sines [positions][rot] (aqd.h; rotary_table). cache: the PagedCache whose steps it takes. The set-up has ended on the
-    GPU when the constructor returns, so passes may run on any stream, one at a time (see GatedFfn)."""
+    GPU when the constructor returns, so passes may run on any stream, one at a time (see GatedFfn). A step of new sequences alone attends
+    to its own keys and values; where others are among them, all of its rows go through the cache and have its 4 bits' error."""
 
     def __init__(self, cache, norm_weight, wq, wk, wv, wo, table, q_norm=None, k_norm=None, pairs=aqd.PAIRS_HALVES, eps=1e-5, max_rows=4096):
         import torch

@@ -8,13 +8,15 @@
 //
 // A code becomes an operand by one shift and one and-or for two: c is put below the leading bit of 128 (bf16) or 64
 // (fp16), which makes 128 + c or 64 + c. Products with a constant -136 or -72 take the offset, 8 included, out again
-// before it is scaled, so that the sums are those of c - 8, exactly. A key's scale multiplies its
-// scores of the group in fp32, a value's scale its weights before they are rounded to T.
+// before it is scaled, which leaves the sums of c - 8 with the roundings of sums up to 35 (fp16: 19) times as large: up to five of fp32's 24
+// bits. A key's scale multiplies its scores of the group in fp32. A value's scale multiplies its weights, and the products are rounded to T:
+// the matrix cores take no more bits at this rate, and the result has no more. Against 64 bits that leaves the error which fp32 weights have
+// (64 of 700 to 8192, bf16: 0.0017 of the result's norm with either, nearly all of it the rounding of the result).
 //
 // Bound by the vector units, and by how even the workgroups are: 64 sequences of 700 to 8192 tokens, 32 query heads on 8, dim 128, groups of 32
-// take 82 us, 334 MB at 4.0 TB/s; 368 vector instructions a step of 32 tokens (112 of them make operands of codes, 150 apply scales) are 54%
+// take 82 to 84 us, 334 MB at 4.0 TB/s; 368 vector instructions a step of 32 tokens (112 of them make operands of codes, 150 apply scales) are 54%
 // of the cycles, the matrix cores 14%. With groups of 128 and 3 of 120000 (64 heads on 8) 74 us and 8 for the second launch.
-// 64 of 8192 with groups of 64 take 111 us, 5.1 TB/s. One sequence of 1500: 9.2 us, two launches of 5.2 and 4.2.
+// 64 of 8192 with groups of 64 take 113 to 117 us, 5.0 TB/s. One sequence of 1500: 9.2 us, two launches of 5.2 and 4.2.
 //
 // fp16 weights have few exponents: there the softmax's reference is the largest sum of a score and the exponent of its value's
 // scales, so that the largest product of weight and scale is near 1 whatever the values' sizes.
