@@ -468,13 +468,14 @@ aqd_status_t qcache_read(const qcache_rows_desc_t *desc, const void *cache, cons
  * lengths[b] - n + 1 + i tokens, and
  *   y = sum over those of softmax(scale * q . k) v
  * for query head h with key head h / (q_heads / heads). A query that sees no token (an empty sequence) has zeros. Rows of
- * q outside of every sequence are left as they were. fp32 scores and sums, of which the codes' offset takes up to five bits; the weights times the values' scales are rounded to
- * `type` for the matrix product: each term within half a unit of its last place (fp16: or 2^-24 of the row's largest; bf16: where the cache
- * holds values of 2^90 and more, those below 2^-75 may count as 0).
+ * q outside of every sequence are left as they were. fp32 scores and sums, of which the codes' offset takes up to five bits;
+ * the weights times the values' scales are rounded to `type` for the matrix product: each term within half a unit of its
+ * last place (fp16: or 2^-24 of the row's largest; bf16: where the cache holds values of 2^90 and more, those below 2^-75 may
+ * count as 0).
  * max_queries and max_keys bound the sequences' queries and lengths, which sizes the launch; of a longer sequence
- * the first max_queries queries and max_keys tokens count, as if it had no more (and no more than ld_table pages). Queries that see a token whose page
- * number is outside of 0 .. pages - 1 are NaN. What lies in a page past a sequence's end does not matter. No row of q may be
- * two sequences'.
+ * the first max_queries queries and max_keys tokens count, as if it had no more (and no more than ld_table pages). Queries that
+ * see a token whose page number is outside of 0 .. pages - 1 are NaN. What lies in a page past a sequence's end does not matter.
+ * No row of q may be two sequences'.
  * q, y: AQD_F16 or AQD_BF16 (UNSUPPORTED: AQD_F32), [queries][q_heads][dim].
  *
  * workspace (device, 16-byte aligned, ws_bytes): with it, the tokens of long sequences are split between workgroups, which
@@ -500,10 +501,10 @@ aqd_status_t qattn_run(const qattn_desc_t *desc, const void *q, const int32_t *q
  * with n queries and m keys the i-th query sees all m keys, or with causal set the first m - n + 1 + i (prompts that continue
  * what was read before have more keys than queries). Scores, heads, zeros, rows outside and rounding as qattn_run's; the weights are
  * rounded to `type` for the product with v (fp16: within half a unit, or 2^-24 of the row's largest). What a query does not see has
- * no part in its result, infinities and NaN included (32 rows that see such, or a hidden one near what they see, take hundreds of times as long:
- * a prompt of 2048 30 ms for 72 us). max_queries and max_keys bound the sequences' rows, which sizes the launch;
- * of a longer sequence the first max_queries queries and all keys count, as if it had no more queries. Starts are taken as if within 0 .. queries and 0 .. keys,
- * and a sequence whose start lies behind its end as empty; no row of q may be two sequences'.
+ * no part in its result, infinities and NaN included (32 rows that see such, or a hidden one near what they see, take hundreds
+ * of times as long: a prompt of 2048 30 ms for 72 us). max_queries and max_keys bound the sequences' rows, which sizes the
+ * launch; of a longer sequence the first max_queries queries and all keys count, as if it had no more queries. Starts are taken as
+ * if within 0 .. queries and 0 .. keys, and a sequence whose start lies behind its end as empty; no row of q may be two sequences'.
  * dim: a multiple of 8 up to 256 (UNSUPPORTED above); AQD_F16 or AQD_BF16 (UNSUPPORTED: AQD_F32); k_token and v_token
  * at most 2^26 elements (UNSUPPORTED above).
  * workspace as qattn_run's (aqd_attn_workspace): few queries over many keys are split. */

@@ -14,7 +14,7 @@
 // (64 of 700 to 8192, bf16: 0.0017 of the result's norm with either, nearly all of it the rounding of the result).
 //
 // Bound by the vector units, and by how even the workgroups are: 64 sequences of 700 to 8192 tokens, 32 query heads on 8, dim 128, groups of 32
-// take 82 to 84 us, 334 MB at 4.0 TB/s; 368 vector instructions a step of 32 tokens (112 of them make operands of codes, 150 apply scales) are 54%
+// take 82 to 84 us, 334 MB at 4.0 TB/s; 375 vector instructions a step of 32 tokens (112 of them make operands of codes, 150 apply scales) are 54%
 // of the cycles, the matrix cores 14%. With groups of 128 and 3 of 120000 (64 heads on 8) 74 us and 8 for the second launch.
 // 64 of 8192 with groups of 64 take 113 to 117 us, 5.0 TB/s. One sequence of 1500: 9.2 us, two launches of 5.2 and 4.2.
 //
